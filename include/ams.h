@@ -268,6 +268,87 @@ int ams_linear_static_ws(const void* W_packed, const uint16_t* scales, const uin
  */
 int ams_read_probe(const void* buf, size_t bytes, uint32_t* sink, void* stream);
 
+/*
+ * The 4-bit KV cache and the attention over it: what a decode step reads beside the weights.  Not part of the
+ * paper; its number format (e2m1, Sec. 2.2), its scales (Eq. 1 on runs of channels, Sec. 5) and its readings are
+ * those of ams_pack_grouped and ams_dequant_grouped for AMS_FMT_FP4_E2M1.
+ *
+ * For a run of scale_group channels x of one token and kv head:
+ *   s = fp16(max|x| / 6), 1 where that is 0, at most 10912 (so that 6 s is an fp16 value);
+ *   code = x / s rounded to the nearest e2m1 value, ties to the even code, saturating;  the cache stands for
+ *   fp16(code * s).  A run that holds an inf or a NaN stands for NaN in every channel.
+ *
+ * Pages.  `pages` is [n_pages][kv_heads][block], block = ams_kv_block_bytes() bytes that hold page_size tokens of
+ * one kv head (D / 2 bytes of codes and 2 D / scale_group bytes of scales for each of K and V and token).  Inside a
+ * block the layout is the library's own.  Position p of sequence b lies in page
+ * block_table[b * table_stride + p / page_size].  Entries outside [0, n_pages) name no page: rows there are not written,
+ * read back as zeros and are left out of attention.  Sequences may share pages that they only read.
+ *
+ * Rows.  Sequence b has kv_lens[b] tokens, those of the present call among them (a length is taken as at most
+ * table_width * page_size, a negative one as 0).  Rows q_starts[b] .. q_starts[b + 1] - 1 of the call's tensors are
+ * its LAST rows: with n of them row i has position kv_lens[b] - n + i.  q_starts is ascending, [batch + 1]; NULL: one
+ * row per sequence (rows = batch).  Rows that no sequence has are left alone.  Rows with a negative position are
+ * not written, read back as zeros, and see no key.
+ *
+ * block_table, kv_lens and q_starts are device memory and are read by the kernels only: a captured call follows
+ * them from replay to replay, and no entry point waits for the device.  Whatever they hold, nothing outside of the
+ * pages and tensors is touched.
+ */
+typedef struct ams_kv_cache {
+  void* pages;                /* device, 16-byte aligned */
+  const int32_t* block_table; /* device, [batch][table_width], rows table_stride apart */
+  const int32_t* kv_lens;     /* device, [batch] */
+  const int32_t* q_starts;    /* device, [batch + 1], or NULL */
+  int64_t n_pages, table_stride;
+  int32_t table_width, batch, kv_heads;
+  int32_t head_dim;           /* D: 64, 128 or 256 */
+  int32_t page_size;          /* tokens: a multiple of 16, up to AMS_KV_MAX_PAGE */
+  int32_t scale_group;        /* channels of a run: 32, 64 or 128, up to D */
+} ams_kv_cache;
+
+#define AMS_KV_MAX_PAGE 1024
+#define AMS_KV_MAX_HEADS 1024
+#define AMS_KV_MAX_BATCH 65536
+#define AMS_KV_MAX_TOKENS (1 << 28) /* of a sequence (table_width * page_size), and rows of a call (times heads / kv_heads) */
+
+/* Bytes of one head's block of a page. */
+int ams_kv_block_bytes(int head_dim, int page_size, int scale_group, size_t* bytes);
+
+/*
+ * ams_kv_write  quantizes rows of K and V, [rows][kv_heads][D] fp16 with the given strides (in values; the channels of
+ *               a head lie together), into the cache.
+ * ams_kv_read   the reverse: what the cache stands for at the rows' positions.
+ * Any strides and any 2-byte alignment; 16-byte aligned rows are faster.  Two rows of a call that have the same place
+ * race; nothing is written outside of the rows' own places, so writes of other tokens of a page may overlap in time.
+ * Errors: NULL, SHAPE, ALIGN, DEVICE, LAUNCH.
+ */
+int ams_kv_write(const ams_kv_cache* cache, const uint16_t* K, const uint16_t* V, int64_t rows, int64_t k_stride,
+                 int64_t k_head_stride, int64_t v_stride, int64_t v_head_stride, void* stream);
+int ams_kv_read(const ams_kv_cache* cache, uint16_t* K, uint16_t* V, int64_t rows, int64_t k_stride, int64_t k_head_stride,
+                int64_t v_stride, int64_t v_head_stride, void* stream);
+
+/*
+ * Attention of rows of Q, [rows][heads][D] fp16, over the cache: head h reads kv head h / (heads / kv_heads),
+ *   O[r, h] = sum_j softmax_j(softmax_scale * Q[r, h] . K[j]) V[j],   lse[r, h] = log sum_j exp(softmax_scale * Q[r, h] . K[j])
+ * over the keys j < kv_lens[b] that the row sees: with `causal` those up to its own position, with window > 0 (causal only)
+ * the last `window` of these.  fp32 sums and statistics; the weights are rounded to fp16 for the matrix cores, their sum is
+ * not.  A row that sees no key gives O = 0, lse = -inf.  A masked key has no effect, whatever it holds.
+ *   lse          device [rows][heads] fp32 with rows lse_stride apart, or NULL
+ *   max_q_len    the most rows that any sequence has, as far as the caller knows (0: unknown): it chooses between
+ *                kernels, results hold whatever it says
+ *   workspace    device, 16-byte aligned, or NULL.  With it long sequences are cut into pieces that several workgroups
+ *                take.  ams_kv_attention_workspace_bytes says how much is used at most for such a call (never more
+ *                than AMS_KV_WORKSPACE_BYTES); with less, fewer pieces.  Its content is of no account before and after.
+ *                Calls that overlap in time must not share it.
+ * Deterministic.  Errors: NULL, SHAPE (softmax_scale not above 0 or not finite among them), ALIGN, DEVICE, LAUNCH.
+ */
+#define AMS_KV_WORKSPACE_BYTES (64 << 20)
+int ams_kv_attention_workspace_bytes(const ams_kv_cache* cache, int64_t rows, int heads, int64_t max_q_len, size_t* bytes);
+int ams_kv_attention(const ams_kv_cache* cache, const uint16_t* Q, uint16_t* O, float* lse, int64_t rows, int heads,
+                     int64_t q_stride, int64_t q_head_stride, int64_t o_stride, int64_t o_head_stride, int64_t lse_stride,
+                     float softmax_scale, int causal, int64_t window, int64_t max_q_len, void* workspace,
+                     size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -27,6 +27,7 @@ FP4 = 6  # AMS_FMT_FP4_E2M1
 SEARCH_SET_BIT = 0  # AMS_SEARCH_SET_BIT
 SEARCH_REROUND = 1  # AMS_SEARCH_REROUND
 MAX_M = 32
+KV_WORKSPACE_BYTES = 64 << 20  # AMS_KV_WORKSPACE_BYTES
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libams.so")
 _lib = None
@@ -36,6 +37,15 @@ _i64, _int, _vp = ctypes.c_int64, ctypes.c_int, ctypes.c_void_p
 
 class AmsError(RuntimeError):
     pass
+
+
+class _KvCache(ctypes.Structure):
+    """ams_kv_cache of include/ams.h."""
+
+    _fields_ = [
+        ("pages", _vp), ("block_table", _vp), ("kv_lens", _vp), ("q_starts", _vp), ("n_pages", _i64), ("table_stride", _i64),
+        *((name, ctypes.c_int32) for name in ("table_width", "batch", "kv_heads", "head_dim", "page_size", "scale_group")),
+    ]
 
 
 def load_library():
@@ -71,6 +81,10 @@ def load_library():
     lib.ams_linear_ws.argtypes = [_vp, _vp, _vp, _vp, _int, _i64, _i64, _int, _vp, ctypes.c_size_t, _vp]
     lib.ams_fp16_linear_ws.argtypes = [_vp, _vp, _vp, _int, _i64, _i64, _vp, ctypes.c_size_t, _vp]
     lib.ams_linear_plan.argtypes = [_int, _int, _i64, _i64, _int, ctypes.c_char_p, ctypes.c_size_t]
+    lib.ams_kv_block_bytes.argtypes = [_int, _int, _int, ctypes.POINTER(ctypes.c_size_t)]
+    lib.ams_kv_write.argtypes = lib.ams_kv_read.argtypes = [ctypes.POINTER(_KvCache), _vp, _vp, *[_i64] * 5, _vp]
+    lib.ams_kv_attention_workspace_bytes.argtypes = [ctypes.POINTER(_KvCache), _i64, _int, _i64, ctypes.POINTER(ctypes.c_size_t)]
+    lib.ams_kv_attention.argtypes = [ctypes.POINTER(_KvCache), _vp, _vp, _vp, _i64, _int, *[_i64] * 5, ctypes.c_float, _int, _i64, _i64, _vp, ctypes.c_size_t, _vp]
     lib.ams_read_probe.argtypes = [_vp, ctypes.c_size_t, _vp, _vp]
     _lib = lib
     return lib
@@ -468,3 +482,136 @@ def ams_pack_per_tensor(fmt: int, W: np.ndarray, search: int = SEARCH_SET_BIT, r
     rc = load_library().ams_pack_per_tensor(fmt, search, _np_ptr(W), N, K, K, _np_ptr(packed), _np_ptr(scales), _np_ptr(codes) if return_codes else None)
     _check(rc, "ams_pack_per_tensor")
     return (packed, scales, codes) if return_codes else (packed, scales)
+
+
+def ams_kv_block_bytes(head_dim: int, page_size: int, scale_group: int) -> int:
+    """Bytes that page_size tokens of one kv head take in a 4-bit cache."""
+    out = ctypes.c_size_t(0)
+    _check(load_library().ams_kv_block_bytes(head_dim, page_size, scale_group, ctypes.byref(out)), "ams_kv_block_bytes")
+    return out.value
+
+
+def ams_kv_cache(n_pages: int, kv_heads: int, head_dim: int, page_size: int = 64, scale_group: int = 32, device="cuda"):
+    """An empty 4-bit KV cache: uint8 [n_pages, kv_heads, block], a block holding page_size tokens of a head."""
+    import torch
+
+    return torch.zeros((n_pages, kv_heads, ams_kv_block_bytes(head_dim, page_size, scale_group)), dtype=torch.uint8, device=device)
+
+
+def _kv_rows(t, name, heads, head_dim):
+    # [rows, heads, head_dim] with the channels of a head side by side
+    import torch
+
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != head_dim:
+        raise ValueError(f"{name} must be [rows, {heads}, {head_dim}], it is {list(t.shape)}")
+    if t.dtype != torch.float16:
+        raise TypeError(f"expected {torch.float16}, got {t.dtype}")
+    if not t.is_cuda or t.stride(2) != 1:
+        raise ValueError(f"{name} must be a CUDA tensor whose last dimension is contiguous")
+    if _devices != 1:
+        _check_device(t)
+    return t.data_ptr()
+
+
+def _kv_view(cache, block_table, kv_lens, q_starts, head_dim, scale_group):
+    import torch
+
+    if cache.dim() != 3 or block_table.dim() != 2 or kv_lens.dim() != 1:
+        raise ValueError("expected cache [pages, kv_heads, block], block_table [batch, pages of a sequence] and kv_lens [batch]")
+    batch, width = block_table.shape
+    if kv_lens.shape[0] != batch:
+        raise ValueError(f"block_table has {batch} sequences, kv_lens {kv_lens.shape[0]}")
+    if q_starts is not None and tuple(q_starts.shape) != (batch + 1,):
+        raise ValueError(f"q_starts must have {batch + 1} entries")
+    token = ams_kv_block_bytes(head_dim, 16, scale_group) // 16
+    page_size, rest = divmod(cache.shape[2], token)
+    if rest:
+        raise ValueError(f"a block of {cache.shape[2]} bytes holds no whole number of tokens of {token} bytes")
+    if block_table.dtype != torch.int32:
+        raise TypeError(f"expected {torch.int32}, got {block_table.dtype}")
+    if not block_table.is_cuda or (width > 1 and block_table.stride(1) != 1):
+        raise ValueError("block_table must be a CUDA tensor whose last dimension is contiguous")
+    if _devices != 1:
+        _check_device(block_table)
+    return _KvCache(
+        _dev_ptr(cache, torch.uint8), block_table.data_ptr(), _dev_ptr(kv_lens, torch.int32), None if q_starts is None else _dev_ptr(q_starts, torch.int32), cache.shape[0],
+        block_table.stride(0) if batch > 1 else width, width, batch, cache.shape[1], head_dim, page_size, scale_group
+    )
+
+
+def ams_kv_write(cache, k, v, block_table, kv_lens, scale_group: int = 32, q_starts=None):
+    """Quantize rows of k and v, fp16 [rows, kv_heads, head_dim] (views too), into the cache as the last rows of their sequences.
+
+    Sequence b has kv_lens[b] tokens, the new ones among them, in the pages block_table[b] (int32 [batch, pages]); its rows of k and v
+    are q_starts[b] .. q_starts[b + 1] - 1 (int32 [batch + 1]; None: one row per sequence).  Returns the cache."""
+    view = _kv_view(cache, block_table, kv_lens, q_starts, k.shape[-1], scale_group)
+    kp, vp = _kv_rows(k, "k", cache.shape[1], k.shape[-1]), _kv_rows(v, "v", cache.shape[1], k.shape[-1])
+    if v.shape[0] != k.shape[0]:
+        raise ValueError(f"k has {k.shape[0]} rows, v {v.shape[0]}")
+    rc = load_library().ams_kv_write(ctypes.byref(view), kp, vp, k.shape[0], k.stride(0), k.stride(1), v.stride(0), v.stride(1), _stream())
+    _check(rc, "ams_kv_write")
+    return cache
+
+
+def ams_kv_read(cache, block_table, kv_lens, scale_group: int = 32, head_dim: int = 128, q_starts=None, rows: int = None, out=None):
+    """The values that the cache holds for the last rows of each sequence: (k, v), fp16 [rows, kv_heads, head_dim].
+
+    Rows as in ams_kv_write: with q_starts = the cumulated kv_lens whole sequences are read.  `rows` is q_starts[-1] (one per
+    sequence without q_starts); with out=(k, v) it is theirs."""
+    import torch
+
+    view = _kv_view(cache, block_table, kv_lens, q_starts, head_dim, scale_group)
+    if out is None:
+        if rows is None:
+            if q_starts is not None:
+                raise ValueError("rows or out must be given with q_starts")
+            rows = block_table.shape[0]
+        out = tuple(torch.empty((rows, cache.shape[1], head_dim), dtype=torch.float16, device=cache.device) for _ in range(2))
+    k, v = out
+    kp, vp = _kv_rows(k, "out", cache.shape[1], head_dim), _kv_rows(v, "out", cache.shape[1], head_dim)
+    if v.shape[0] != k.shape[0] or (rows is not None and rows != k.shape[0]):
+        raise ValueError(f"out must hold {k.shape[0] if rows is None else rows} rows, it has {k.shape[0]} and {v.shape[0]}")
+    rc = load_library().ams_kv_read(ctypes.byref(view), kp, vp, k.shape[0], k.stride(0), k.stride(1), v.stride(0), v.stride(1), _stream())
+    _check(rc, "ams_kv_read")
+    return k, v
+
+
+def ams_kv_attention_workspace_bytes(q, cache, block_table, kv_lens, scale_group: int = 32, q_starts=None, max_q_len: int = None) -> int:
+    """Bytes of workspace that ams_kv_attention uses at most for such a call (never more than KV_WORKSPACE_BYTES)."""
+    out = ctypes.c_size_t(0)
+    view = _kv_view(cache, block_table, kv_lens, q_starts, q.shape[-1], scale_group)
+    _check(load_library().ams_kv_attention_workspace_bytes(ctypes.byref(view), q.shape[0], q.shape[1], max_q_len or 0, ctypes.byref(out)), "ams_kv_attention_workspace_bytes")
+    return out.value
+
+
+def ams_kv_attention(q, cache, block_table, kv_lens, scale_group: int = 32, q_starts=None, max_q_len: int = None, softmax_scale: float = None, causal: bool = True, window: int = 0,
+                     workspace=None, out=None, lse=None):
+    """softmax(softmax_scale * q k^T) v over the cache, fp16 [rows, heads, head_dim] like q (a view too); heads / kv_heads of them share a kv head.
+
+    q's rows are the last rows of their sequences, as in ams_kv_write: a row sees the keys up to its own (causal), of these the last
+    `window` if that is not 0.  softmax_scale: head_dim ** -0.5 by default.  max_q_len: the most rows of a sequence, if known.
+    workspace: a uint8 CUDA tensor that calls may share one after the other; without one long sequences are not cut into pieces.
+    lse: fp32 [rows, heads], receives log(sum(exp(scores)))."""
+    import torch
+
+    if q.dim() != 3:
+        raise ValueError("q must be [rows, heads, head_dim]")
+    rows, heads, head_dim = q.shape
+    view = _kv_view(cache, block_table, kv_lens, q_starts, head_dim, scale_group)
+    if out is None:
+        out = torch.empty((rows, heads, head_dim), dtype=torch.float16, device=q.device)
+    elif out.dim() != 3 or out.shape[0] != rows:
+        raise ValueError(f"out must hold {rows} rows of [{heads}, {head_dim}], it is {list(out.shape)}")
+    if lse is not None and (tuple(lse.shape) != (rows, heads) or (heads > 1 and lse.stride(1) != 1)):
+        raise ValueError(f"lse must be [{rows}, {heads}] with a contiguous last dimension")
+    if lse is not None and (lse.dtype != torch.float32 or not lse.is_cuda):
+        raise TypeError("lse must be a float32 CUDA tensor")
+    if lse is not None and _devices != 1:
+        _check_device(lse)
+    rc = load_library().ams_kv_attention(
+        ctypes.byref(view), _kv_rows(q, "q", heads, head_dim), _kv_rows(out, "out", heads, head_dim), lse.data_ptr() if lse is not None else None, rows, heads, q.stride(0), q.stride(1),
+        out.stride(0), out.stride(1), lse.stride(0) if lse is not None else 0, head_dim**-0.5 if softmax_scale is None else softmax_scale, int(causal), window, max_q_len or 0,
+        _dev_ptr(workspace, torch.uint8) if workspace is not None else None, workspace.numel() if workspace is not None else 0, _stream()
+    )
+    _check(rc, "ams_kv_attention")
+    return out

@@ -2053,6 +2053,10 @@ int prepare_format() {
 
 }  // namespace
 
+namespace ams_kv {
+int device_status() { return device_state(); }
+}  // namespace ams_kv
+
 extern "C" {
 
 int ams_init(void) {
