@@ -560,12 +560,11 @@ def ams_kv_read(cache, block_table, kv_lens, scale_group: int = 32, head_dim: in
     sequence without q_starts); with out=(k, v) it is theirs."""
     import torch
 
+    if out is None and rows is None and q_starts is not None:
+        raise ValueError("rows or out must be given with q_starts")
     view = _kv_view(cache, block_table, kv_lens, q_starts, head_dim, scale_group)
     if out is None:
-        if rows is None:
-            if q_starts is not None:
-                raise ValueError("rows or out must be given with q_starts")
-            rows = block_table.shape[0]
+        rows = block_table.shape[0] if rows is None else rows
         out = tuple(torch.empty((rows, cache.shape[1], head_dim), dtype=torch.float16, device=cache.device) for _ in range(2))
     k, v = out
     kp, vp = _kv_rows(k, "out", cache.shape[1], head_dim), _kv_rows(v, "out", cache.shape[1], head_dim)
