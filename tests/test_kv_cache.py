@@ -149,9 +149,10 @@ def test_what_the_binding_refuses_on_the_gpu():
 
 def test_the_oracle_rounds_as_the_definition_says():
     # scale 1: ties to the even code, saturation, signs; a run of zeros; a run that holds an inf
-    x = np.array([6, 0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, -0.25, -0.75, -5.0, 0.2501, 0.7499] + [0] * 19, dtype=np.float16)
+    x = np.array([6, 0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, -0.25, -0.75, -5.0, 0.2501, 0.7499] + [0] * 19, dtype=np.float16)  # the last two are ties once they are fp16
     y = O.held(x[None], 32)[0]
-    assert list(y[:13]) == [6, 0, 1, 1, 2, 2, 4, 4, 0, -1, -4, 0.5, 0.5]
+    assert list(y[:13]) == [6, 0, 1, 1, 2, 2, 4, 4, 0, -1, -4, 0, 1]
+    assert list(O.held(np.array([[6, 0.2505, 0.749] + [0] * 29], dtype=np.float16), 32)[0, :3]) == [6, 0.5, 0.5]
     assert np.signbit(y[8]) and not np.signbit(y[20])
     assert not O.held(np.zeros((1, 64), np.float16), 32).any()
     z = np.ones((1, 64), np.float16)
