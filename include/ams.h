@@ -336,10 +336,11 @@ int ams_kv_read(const ams_kv_cache* cache, uint16_t* K, uint16_t* V, int64_t row
  *   lse          device [rows][heads] fp32 with rows lse_stride apart, or NULL
  *   max_q_len    the most rows that any sequence has, as far as the caller knows (0: unknown): it chooses between
  *                kernels, results hold whatever it says
- *   workspace    device, 16-byte aligned, or NULL.  With it long sequences are cut into pieces that several workgroups
- *                take.  ams_kv_attention_workspace_bytes says how much is used at most for such a call (never more
- *                than AMS_KV_WORKSPACE_BYTES); with less, fewer pieces.  Its content is of no account before and after.
- *                Calls that overlap in time must not share it.
+ *   workspace    device, 16-byte aligned, zero-filled once before its first use (the calls leave it ready for the next one,
+ *                of any shape), or NULL.  With it the keys of a row may be shared out to several workgroups, which exchange
+ *                their parts through it.  ams_kv_attention_workspace_bytes says how much is used at most for such a call
+ *                (never more than AMS_KV_WORKSPACE_BYTES); with less, fewer workgroups.  Calls that overlap in time must
+ *                not share it.
  * Deterministic.  Errors: NULL, SHAPE (softmax_scale not above 0 or not finite among them), ALIGN, DEVICE, LAUNCH.
  */
 #define AMS_KV_WORKSPACE_BYTES (64 << 20)

@@ -23,6 +23,7 @@ namespace ams_kv {
 typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef _Float16 h4 __attribute__((ext_vector_type(4)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef float f2 __attribute__((ext_vector_type(2)));
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
@@ -38,13 +39,25 @@ constexpr Planes planes(int head_dim, int page_size, int scale_group) {
   return {codes, scales, 2 * (codes + scales)};
 }
 
+// Division by a number that the host knows, of anything below 2^31.
+struct Divisor {
+  uint32_t by, mul, shift;
+  __device__ __forceinline__ uint32_t quotient(uint32_t n) const { return (uint32_t)(((uint64_t)n * mul) >> shift); }
+};
+inline Divisor divisor(uint32_t by) {
+  uint32_t bits = 0;
+  while (bits < 31 && (1u << bits) < by) bits++;
+  return {by, (uint32_t)(((1ull << (31 + bits)) + by - 1) / by), 31 + bits};  // rounded up: off by less than n / 2^31 of a unit
+}
+
 // What every kernel of the cache is told of it.  Lengths, tables and row starts are the device's: a captured call follows them.
 struct View {
   uint8_t* pages;
   const int32_t *table, *lens, *starts;  // starts may be null: one row per sequence
   int64_t table_stride, page_bytes;      // page_bytes: of a page's blocks of all heads
   int n_pages, table_width, batch, kv_heads, rows;
-  int page_tiles, page_size, codes, scales, block;
+  int page_size, codes, scales, block;
+  Divisor page_tiles, heads;  // heads: of the cache
 };
 
 __device__ __forceinline__ int lane_id() { return (int)(threadIdx.x & 63); }
@@ -57,9 +70,10 @@ __device__ __forceinline__ int row_start(const View& v, int b) {
 // Tokens of sequence b that the table has places for.
 __device__ __forceinline__ int kv_len(const View& v, int b) { return (int)min((int64_t)max(v.lens[b], 0), (int64_t)v.table_width * v.page_size); }
 
-// The block of tile `tile` (>= 0) of sequence b, or null where the table names no page of the pool.
-__device__ __forceinline__ uint8_t* block_of(const View& v, int b, int tile, int head) {
-  const int page = tile / v.page_tiles;
+// The block of tile `tile` (>= 0) of sequence b, or null where the table names no page of the pool; and where in it the tile is.
+__device__ __forceinline__ uint8_t* block_of(const View& v, int b, int tile, int head, int* in_page) {
+  const int page = (int)v.page_tiles.quotient((uint32_t)tile);
+  *in_page = tile - page * (int)v.page_tiles.by;
   if (page >= v.table_width) return nullptr;
   const int number = v.table[b * v.table_stride + page];
   if (number < 0 || number >= v.n_pages) return nullptr;
@@ -89,18 +103,15 @@ __device__ __forceinline__ h2 two_codes(uint32_t w) {
   return __builtin_bit_cast(h2, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, BYTE));
 }
 // Eight channels of K: a word's codes times their run's scale, each product rounded to fp16 (as ams_dequant rounds it).
-__device__ __forceinline__ h8 restore_k(uint32_t w, _Float16 s) {
-  const h2 ss = {s, s};
-  const h2 a = two_codes<0>(w) * ss, b = two_codes<1>(w) * ss, c = two_codes<2>(w) * ss, d = two_codes<3>(w) * ss;
-  return h8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+__device__ __forceinline__ h8 restore_k(uint32_t w, h2 s) {
+  const h2 a = two_codes<0>(w) * s, b = two_codes<1>(w) * s, c = two_codes<2>(w) * s, d = two_codes<3>(w) * s;
+  return __builtin_bit_cast(h8, u4{bits(a), bits(b), bits(c), bits(d)});
 }
-// Four tokens of V's channels a (32 i + c) and b (32 i + 16 + c), with the scales of the four tokens.
-__device__ __forceinline__ void restore_v(uint32_t w, h4 s, h4* a, h4* b) {
-  const h2 s01 = {s[0], s[1]}, s23 = {s[2], s[3]};
+// Four tokens of V's channels a (32 i + c) and b (32 i + 16 + c), with the scales of tokens 0, 1 and 2, 3.
+__device__ __forceinline__ void restore_v(uint32_t w, uint32_t s01, uint32_t s23, u2* a, u2* b) {
   const uint32_t x = (w & 0x0F0F0F0Fu) | ((w >> 8) & 0xF0F0F0F0u), y = w >> 4;
-  const h2 a0 = two_codes<0>(x) * s01, a1 = two_codes<2>(x) * s23, b0 = two_codes<0>(y) * s01, b1 = two_codes<2>(y) * s23;
-  *a = h4{a0[0], a0[1], a1[0], a1[1]};
-  *b = h4{b0[0], b0[1], b1[0], b1[1]};
+  *a = u2{bits(two_codes<0>(x) * halves(s01)), bits(two_codes<2>(x) * halves(s23))};
+  *b = u2{bits(two_codes<0>(y) * halves(s01)), bits(two_codes<2>(y) * halves(s23))};
 }
 
 // A lane's words of a tile's codes: W of them per block of 256 W bytes.
@@ -108,10 +119,10 @@ template <int D>
 struct Lane {
   static constexpr int kWords = D / 32, W = kWords < 4 ? kWords : 4, kBlocks = kWords / W;
   uint32_t w[kWords];
-  __device__ __forceinline__ void load(const uint8_t* tile, int lane) {
+  __device__ __forceinline__ void load(const uint8_t* tile, uint32_t lane) {
 #pragma unroll
     for (int p = 0; p < kBlocks; p++) {
-      const uint8_t* at = tile + p * 256 * W + lane * 4 * W;
+      const uint8_t* at = tile + (p * 256 * W + lane * 4u * W);
       if constexpr (W == 2) {
         const u2 x = *(const u2*)at;
         w[0] = x[0], w[1] = x[1];
@@ -123,31 +134,62 @@ struct Lane {
   }
 };
 
-// N scales that lie together.
+// The same through a buffer: `at` is the wavefront's offset in it.
+template <int D>
+__device__ __forceinline__ void load_words(Lane<D>& x, __amdgpu_buffer_rsrc_t from, uint32_t lane, int at) {
+  constexpr int W = Lane<D>::W;
+#pragma unroll
+  for (int p = 0; p < Lane<D>::kBlocks; p++) {
+    if constexpr (W == 2) {
+      const u2 w = __builtin_bit_cast(u2, __builtin_amdgcn_raw_buffer_load_b64(from, lane * 8, at, 0));
+      x.w[0] = w[0], x.w[1] = w[1];
+    } else {
+      const u4 w = __builtin_bit_cast(u4, __builtin_amdgcn_raw_buffer_load_b128(from, lane * 16 + p * 1024, at, 0));
+      x.w[4 * p] = w[0], x.w[4 * p + 1] = w[1], x.w[4 * p + 2] = w[2], x.w[4 * p + 3] = w[3];
+    }
+  }
+}
+
+// N scales that lie together, two to a word.
 template <int N>
 struct Scales {
-  _Float16 s[N];
+  static constexpr int WORDS = (N + 1) / 2;
+  uint32_t w[WORDS];
   __device__ __forceinline__ void load(const uint8_t* at) {
     if constexpr (N == 1) {
-      s[0] = *(const _Float16*)at;
-    } else if constexpr (N == 2) {
-      const h2 x = *(const h2*)at;
-      s[0] = x[0], s[1] = x[1];
-    } else if constexpr (N % 8 == 0) {
+      w[0] = *(const uint16_t*)at;
+    } else if constexpr (WORDS % 4 == 0) {
 #pragma unroll
-      for (int i = 0; i < N; i += 8) {
-        const h8 x = *(const h8*)(at + 2 * i);
-#pragma unroll
-        for (int j = 0; j < 8; j++) s[i + j] = x[j];
+      for (int i = 0; i < WORDS; i += 4) {
+        const u4 x = *(const u4*)(at + 4 * i);
+        w[i] = x[0], w[i + 1] = x[1], w[i + 2] = x[2], w[i + 3] = x[3];
       }
+    } else if constexpr (WORDS == 2) {
+      const u2 x = *(const u2*)at;
+      w[0] = x[0], w[1] = x[1];
     } else {
-#pragma unroll
-      for (int i = 0; i < N; i += 4) {
-        const h4 x = *(const h4*)(at + 2 * i);
-#pragma unroll
-        for (int j = 0; j < 4; j++) s[i + j] = x[j];
-      }
+      static_assert(WORDS == 1, "1, 2, 4 or a multiple of 8 scales");
+      w[0] = *(const uint32_t*)at;
     }
+  }
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t from, uint32_t offset, int at) {
+    static_assert(N <= 8, "up to 16 bytes");
+    if constexpr (N == 1) {
+      w[0] = __builtin_amdgcn_raw_buffer_load_b16(from, offset, at, 0);
+    } else if constexpr (N == 2) {
+      w[0] = __builtin_amdgcn_raw_buffer_load_b32(from, offset, at, 0);
+    } else if constexpr (N == 4) {
+      const u2 x = __builtin_bit_cast(u2, __builtin_amdgcn_raw_buffer_load_b64(from, offset, at, 0));
+      w[0] = x[0], w[1] = x[1];
+    } else {
+      const u4 x = __builtin_bit_cast(u4, __builtin_amdgcn_raw_buffer_load_b128(from, offset, at, 0));
+      w[0] = x[0], w[1] = x[1], w[2] = x[2], w[3] = x[3];
+    }
+  }
+  // scale i twice
+  __device__ __forceinline__ h2 twice(int i) const {
+    const h2 x = halves(w[i / 2]);
+    return i % 2 ? h2{x[1], x[1]} : h2{x[0], x[0]};
   }
 };
 

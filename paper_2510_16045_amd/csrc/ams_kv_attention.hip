@@ -10,9 +10,11 @@
 // operand of O^T = V^T P^T wants it (a lane has the same four keys of a tile in both), V's words become its A operand.  No LDS, no
 // barrier before the end, where the wavefronts' partial sums are joined.
 //
-// Pieces: the host knows neither lengths nor (with row starts) how many rows a sequence has, so every workgroup works out the same
-// split from them: the steps of all sequences over the workgroups that fill the chip, rounded up, is the length of a piece.  A piece
-// of a sequence that has several leaves (max, sum, O) in the workspace, and join_kernel adds those up in the order of the pieces.
+// Split of the work: the host knows neither lengths nor (with row starts) how many rows a sequence has, so every workgroup works it
+// out from them: the steps of all row tiles of a kv head, one tile after the other, are cut into equal shares, as many as there are
+// workgroups that fit on the chip at once.  A share may begin and end inside a tile.  Of a tile that lies in several shares every
+// workgroup leaves its part (max, sum, O) in the workspace and counts itself in; the one that comes last adds all of them up, always in
+// the same order, and clears the count.  Nobody waits for anybody.
 #include "ams_kv.h"
 
 #include <float.h>
@@ -21,9 +23,9 @@
 
 namespace ams_kv {
 
+constexpr int kDeviceScope = 16;  // cache policy (sc1) of a buffer load or store that the whole device sees
 constexpr int kStep = 32;         // keys of a wavefront's step
-constexpr int kStreamWaves = 4;
-constexpr int kMinPiece = 4;      // steps of a piece: one for each wavefront
+constexpr int kMinShare = 4;      // steps of a share: one for each wavefront
 constexpr float kLift = 8.0f;     // exponents of P are raised by this: below it P keeps fp16's full precision over 2^-22 of the largest
 constexpr float kSlack = 7.0f;    // how far (log2) a score may pass the running maximum before that is raised: 2^(8 + 7) is in fp16
 
@@ -31,11 +33,15 @@ struct AttentionArgs {
   View v;
   const uint16_t* q;
   uint16_t* out;
-  float *lse, *part;  // part: [slot][kv head][row of the tile][D + 2]
+  float* lse;
+  uint32_t* counts;  // [kv head][share in which the tile begins]
+  float* parts;      // [kv head][2 share + (the tile begins in it)][row of the tile][max, sum, -, -, D values]
   int64_t q_stride, q_head, out_stride, out_head, lse_stride;
   float scale2;  // softmax_scale * log2(e)
   int group;     // R
-  int heads_pieces;  // pieces that the sequences of one kv head are cut into, about; 0: none is cut
+  Divisor by_group;
+  int shares;        // of the steps of one kv head; 0: no tile is cut, a workgroup takes one
+  int part_rows;     // rows of a tile in `parts`
   int causal, window, vec;
 };
 
@@ -45,14 +51,15 @@ struct Extent {
 };
 template <int ROWS>
 __device__ __forceinline__ Extent extent_of(const AttentionArgs& a, int b) {
-  Extent e;
+  Extent e = {0, 0, 0, 0, 0, 0};
+  if (b >= a.v.batch) return e;
   e.start = row_start(a.v, b);
   e.n = max(row_start(a.v, b + 1) - e.start, 0);
   e.len = kv_len(a.v, b);
   const int first = e.len - e.n;  // position of the first row
   e.lo = a.window > 0 ? max(first + 1 - a.window, 0) & ~(kStep - 1) : 0;
-  e.row_tiles = (int)(((int64_t)e.n * a.group + ROWS - 1) / ROWS);
-  e.steps = e.row_tiles > 0 ? max((e.len - e.lo + kStep - 1) / kStep, 0) : 0;
+  e.row_tiles = (int)(((uint32_t)e.n * (uint32_t)a.group + ROWS - 1) / ROWS);
+  e.steps = max((e.len - e.lo + kStep - 1) / kStep, 1);  // one also where there is no key: somebody has to say so
   return e;
 }
 
@@ -69,356 +76,505 @@ __device__ __forceinline__ int wave_prefix(int x) {  // inclusive
   }
   return x;
 }
+// x, of which the compiler knows nothing: what follows from it is not worked out before it is needed and kept in registers.
+__device__ __forceinline__ int hidden(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int of_lane(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
 
-// Steps of a piece: the same for every workgroup of a call.
+// Steps of a share, and of all row tiles together; without shares both count tiles.
+struct Split {
+  uint32_t per, total;
+};
 template <int ROWS>
-__device__ __forceinline__ int piece_steps(const AttentionArgs& a) {
-  if (a.heads_pieces == 0) return 0x7FFFFFFF;
-  int64_t total = 0;
-  for (int b = 0; b < a.v.batch; b += 64)
-    if (b + lane_id() < a.v.batch) {
-      const Extent e = extent_of<ROWS>(a, b + lane_id());
-      total += (int64_t)e.row_tiles * e.steps;
-    }
-  total = wave_sum(total);
-  const int64_t piece = (total + a.heads_pieces - 1) / a.heads_pieces;
-  return (int)min(max((piece + kMinPiece - 1) / kMinPiece * kMinPiece, (int64_t)kMinPiece), (int64_t)0x7FFFFF00);
+__device__ __forceinline__ Split split_of(const AttentionArgs& a, const Extent& first) {  // first: of the first 64 sequences
+  uint64_t total = (uint64_t)first.row_tiles * (a.shares > 0 ? first.steps : 1);
+  for (int b0 = 64; b0 < a.v.batch; b0 += 64) {
+    const Extent x = extent_of<ROWS>(a, b0 + lane_id());
+    total += (uint64_t)x.row_tiles * (a.shares > 0 ? x.steps : 1);
+  }
+  total = min((uint64_t)wave_sum((int64_t)total), (uint64_t)0x7FFFFFFF);  // the host sees to it
+  if (a.shares == 0) return {1, (uint32_t)total};
+  const uint32_t share = ((uint32_t)total + a.shares - 1) / a.shares;
+  return {max((share + kMinShare - 1) / kMinShare * kMinShare, (uint32_t)kMinShare), (uint32_t)total};
 }
 
-// A piece of work: rows of tile `row_tile` of sequence b, piece `piece` of `pieces`; slot: where the first piece of the tile leaves its
-// result.  With JOIN an item is a row tile.
-struct Item {
-  int b, row_tile, piece, pieces, slot;
+// Where step `at` of the whole lies: `step` of a row tile whose first one is step `first` of the whole.
+struct Place {
+  Extent e;
+  int b, row_tile, step;
+  uint32_t first;
 };
-template <int ROWS, bool JOIN>
-__device__ __forceinline__ bool find_item(const AttentionArgs& a, int per_piece, int item, Item* out) {
-  int items = 0, slots = 0;
+template <int ROWS>
+__device__ __forceinline__ bool place_of(const AttentionArgs& a, Extent e, uint32_t at, Place* out) {  // e: of the first 64 sequences
+  uint32_t before = 0;
   for (int b0 = 0; b0 < a.v.batch; b0 += 64) {
-    const int b = b0 + lane_id();
-    int pieces = 0, tiles = 0;
-    if (b < a.v.batch) {
-      const Extent e = extent_of<ROWS>(a, b);
-      tiles = e.row_tiles;
-      pieces = tiles > 0 ? max(1, (int)(((int64_t)e.steps + per_piece - 1) / per_piece)) : 0;
-    }
-    const int mine = JOIN ? tiles : tiles * pieces, taken = pieces > 1 ? tiles * pieces : 0;
-    const int end = wave_prefix(mine) + items, slot_end = wave_prefix(taken) + slots;
-    const unsigned long long past = __ballot(end > item);
+    if (b0 > 0) e = extent_of<ROWS>(a, b0 + lane_id());
+    const uint32_t each = a.shares > 0 ? e.steps : 1, mine = e.row_tiles * each;
+    const uint32_t end = wave_prefix(mine) + before;
+    const unsigned long long past = __ballot(end > at);
     if (past) {
-      const int at = __builtin_ctzll(past);
-      const int local = item - (__shfl(end, at, 64) - __shfl(mine, at, 64));
-      pieces = __shfl(pieces, at, 64);
-      out->b = b0 + at;
-      out->pieces = pieces;
-      out->row_tile = JOIN ? local : local / pieces;
-      out->piece = JOIN ? 0 : local % pieces;
-      out->slot = __shfl(slot_end, at, 64) - __shfl(taken, at, 64) + out->row_tile * pieces;
+      const int lane = __builtin_ctzll(past);
+      const uint32_t tile_steps = of_lane(each, lane), first = of_lane(end - mine, lane);
+      out->b = b0 + lane;
+      out->row_tile = (at - first) / tile_steps;
+      out->first = first + out->row_tile * tile_steps;
+      out->step = at - out->first;
+      out->e = {of_lane(e.start, lane), of_lane(e.n, lane), of_lane(e.len, lane), of_lane(e.lo, lane), of_lane(e.row_tiles, lane), of_lane(e.steps, lane)};
       return true;
     }
-    items = __shfl(end, 63, 64);
-    slots = __shfl(slot_end, 63, 64);
+    before = of_lane(end, 63);
   }
   return false;
 }
 
-__device__ __forceinline__ h8 join_halves(h4 a, h4 b) { return h8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}; }
+__device__ __forceinline__ h8 join_halves(u2 a, u2 b) { return __builtin_bit_cast(h8, u4{a[0], a[1], b[0], b[1]}); }
+
+// Eight halfs; where rows are not 16-byte aligned half by half.
+__device__ __forceinline__ u4 load_half8(const uint16_t* p, bool vec) {
+  if (vec) return *(const u4*)p;
+  u4 x;
+#pragma unroll
+  for (int i = 0; i < 4; i++) x[i] = p[2 * i] | (uint32_t)p[2 * i + 1] << 16;
+  return x;
+}
 
 // The lowest and highest key (one past) that the row at `position` may see.
 __device__ __forceinline__ int key_end(const AttentionArgs& a, int len, int position) { return a.causal ? min(len, position + 1) : len; }
 __device__ __forceinline__ int key_begin(const AttentionArgs& a, int position) { return a.window > 0 ? max(position + 1 - a.window, 0) : 0; }
 
-// Words and scales of two tiles of a step.
-template <int D, int G>
-struct StepData {
-  Lane<D> k[2], v[2];
-  Scales<D / G> sk[2];
-  Scales<4 * D / G> sv[2];
-  bool held[2];  // the table names a page for the tile
-  __device__ __forceinline__ void load(const AttentionArgs& a, int b, int head, int step, int lane) {
-    constexpr int RUNS = D / G, CODES = 8 * D, SCALES = kTile * RUNS * 2;
+// The pages of 64 steps of a wavefront, one step to a lane: looked up together, read lane by lane.
+struct Pages {
+  int number[2];  // of each tile of the step: -1 where the table names no page
+  __device__ __forceinline__ void look_up(const AttentionArgs& a, int b, int step, int to) {
 #pragma unroll
     for (int t = 0; t < 2; t++) {
-      const int tile = 2 * step + t;
-      const uint8_t* block = block_of(a.v, b, tile, head);
-      held[t] = block != nullptr;
-      if (!block) block = a.v.pages;  // read, and left out
-      const uint8_t* const kc = block + tile % a.v.page_tiles * CODES;
-      const uint8_t* const ks = block + 2 * a.v.codes + tile % a.v.page_tiles * SCALES;
-      k[t].load(kc, lane);
-      v[t].load(kc + a.v.codes, lane);
-      sk[t].load(ks + (lane & 15) * RUNS * 2);
-      sv[t].load(ks + a.v.scales + (lane >> 4) * RUNS * 8);
+      const uint32_t page = a.v.page_tiles.quotient((uint32_t)(2 * step + t));
+      int found = -1;
+      if (step < to && page < (uint32_t)a.v.table_width) found = a.v.table[b * a.v.table_stride + page];
+      number[t] = (uint32_t)found < (uint32_t)a.v.n_pages ? found : -1;
     }
   }
 };
 
-__device__ __forceinline__ bool not_finite(_Float16 x) { return (__builtin_bit_cast(uint16_t, x) & 0x7C00) == 0x7C00; }
+// A tile's block as a buffer; of a page that is not there nothing is read.
+struct Tile {
+  __amdgpu_buffer_rsrc_t block;
+  int tile;   // in its page
+  bool held;  // there is a page
+  __device__ __forceinline__ Tile(const AttentionArgs& a, const Pages& pages, int head, int step, int t, int at) {
+    const int number = of_lane(pages.number[t], at);
+    held = number >= 0;
+    const uint64_t begin = (uint64_t)a.v.pages + (uint64_t)(held ? number : 0) * (uint64_t)a.v.page_bytes + (uint64_t)(uint32_t)head * (uint32_t)a.v.block;
+    block = __builtin_amdgcn_make_buffer_rsrc((void*)begin, 0, held ? a.v.block : 0, 0x00020000);
+    const uint32_t index = 2 * step + t;
+    tile = (int)(index - a.v.page_tiles.quotient(index) * a.v.page_tiles.by);
+  }
+};
 
-// Runs of V that stand for NaN take part in a step's products as zeros where not every row sees every key of the step; here the rows
-// that do see one get the NaN.
-template <int D, int G, int QT>
-__device__ __forceinline__ void nan_of_seen_keys(const StepData<D, G>& x, int first_key, const int (&begin)[QT], const int (&end)[QT], f4 (&o)[D / 16][QT]) {
-  bool any = false;
+// A lane's words of the two tiles of a step and their scales.  V's scales are asked for once by the lanes together, 8 RUNS words of
+// 32 bits of a tile.
+template <int D, int G>
+struct StepK {
+  static constexpr int RUNS = D / G;
+  Lane<D> w[2];
+  Scales<RUNS> s[2];
+  __device__ __forceinline__ void load(const AttentionArgs& a, const Tile& from, int t, uint32_t lane) {
+    load_words<D>(w[t], from.block, lane, from.tile * 8 * D);
+    s[t].load(from.block, (lane & 15) * (RUNS * 2u), 2 * a.v.codes + from.tile * kTile * RUNS * 2);
+  }
+};
+template <int D, int G>
+struct StepV {
+  static constexpr int RUNS = D / G;
+  Lane<D> w[2];
+  uint32_t s[2];
+  __device__ __forceinline__ void load(const AttentionArgs& a, const Tile& from, int t, uint32_t lane) {
+    load_words<D>(w[t], from.block, lane, a.v.codes + from.tile * 8 * D);
+    s[t] = __builtin_amdgcn_raw_buffer_load_b32(from.block, lane < 8 * RUNS ? lane * 4 : 0x7FFE0000, 2 * a.v.codes + a.v.scales + from.tile * kTile * RUNS * 2, 0);
+  }
+};
+
+// Runs of V that stand for NaN take part in a step's products as zeros where not every row sees every key of the step, and the rows
+// that do see one get the NaN here.  stage: the scales of the step's two tiles; begin, end: the keys that a lane's row sees.
+template <int RUNS, int G, int QT, int DT>
+__device__ __forceinline__ void nan_of_seen_keys(uint8_t* stage, int lane, int first_key, const int (&begin)[QT], const int (&end)[QT], f4 (&o)[DT][QT]) {
+  const int g = lane >> 4;
+  uint32_t bad[RUNS], any = 0;  // of the step's 32 keys those whose run stands for NaN; first a lane's eight
 #pragma unroll
-  for (int i = 0; i < 4 * D / G; i++) any |= not_finite(x.sv[0].s[i]) || not_finite(x.sv[1].s[i]);
-  if (!__ballot(any)) return;
-#pragma unroll
-  for (int run = 0; run < D / G; run++) {
-    uint32_t keys = 0;  // of the step, whose run stands for NaN
+  for (int run = 0; run < RUNS; run++) {
+    bad[run] = 0;
 #pragma unroll
     for (int u = 0; u < 2; u++)
 #pragma unroll
-      for (int j = 0; j < 4; j++) {
-        const unsigned long long lanes = __ballot(x.held[u] && not_finite(x.sv[u].s[4 * run + j]));
+      for (int j = 0; j < 4; j++)
+        if ((*(const uint16_t*)(stage + ((u * 4 + g) * RUNS + run) * 8 + 2 * j) & 0x7C00) == 0x7C00) bad[run] |= 1u << (16 * u + 4 * g + j);
+    any |= bad[run];
+  }
+  if (!__ballot(any != 0)) return;
 #pragma unroll
-        for (int g = 0; g < 4; g++) keys |= (uint32_t)(lanes >> 16 * g & 1) << (16 * u + 4 * g + j);
-      }
+  for (int run = 0; run < RUNS; run++) {
+    bad[run] |= (uint32_t)__shfl_xor((int)bad[run], 16, 64);
+    bad[run] |= (uint32_t)__shfl_xor((int)bad[run], 32, 64);
+#pragma unroll
+    for (int u = 0; u < 2; u++)
+#pragma unroll
+      for (int j = 0; j < 4; j++)
+        if (bad[run] >> (16 * u + 4 * g + j) & 1) *(uint16_t*)(stage + ((u * 4 + g) * RUNS + run) * 8 + 2 * j) = 0;
 #pragma unroll
     for (int t = 0; t < QT; t++) {
       const int from = min(max(begin[t] - first_key, 0), 32), to = min(max(end[t] - first_key, 0), 32);
       const uint32_t seen = (uint32_t)((1ull << to) - 1) & ~(uint32_t)((1ull << from) - 1);
-      if (keys & seen) {
+      if (bad[run] & seen) {
 #pragma unroll
         for (int d = run * G / 16; d < (run + 1) * G / 16; d++) o[d][t] = f4{NAN, NAN, NAN, NAN};
       }
     }
   }
+  wave_sync();
 }
 
-template <int D, int G, int QT>
-__global__ __launch_bounds__(64 * kStreamWaves) void stream_kernel(AttentionArgs a) {
-  constexpr int ROWS = 16 * QT, RUNS = D / G, DT = D / 16, KB = D / 32;
-  const int tid = threadIdx.x, wave = tid >> 6, lane = lane_id(), g = lane >> 4, col = lane & 15;
-  const int head = blockIdx.x % a.v.kv_heads;
-  Item it;
-  const int per_piece = piece_steps<ROWS>(a);
-  if (!find_item<ROWS, false>(a, per_piece, blockIdx.x / a.v.kv_heads, &it)) return;
-  const Extent e = extent_of<ROWS>(a, it.b);
-  const int rows = e.n * a.group, row0 = it.row_tile * ROWS;
-  // this lane's rows: one in each column tile
-  h8 q[KB][QT];
-  int begin[QT], end[QT];
+__device__ __forceinline__ void store_out(const AttentionArgs& a, const Extent& e, int head, int r, int channel, f4 x) {
+  const int token = (int)a.by_group.quotient((uint32_t)r);
+  _Float16* const dst = (_Float16*)a.out + (int64_t)(e.start + token) * a.out_stride + (int64_t)(head * a.group + r - token * a.group) * a.out_head + channel;
+  const h4 y = {(_Float16)x[0], (_Float16)x[1], (_Float16)x[2], (_Float16)x[3]};
+  if (a.vec) {
+    *(h4*)dst = y;
+  } else {
 #pragma unroll
-  for (int t = 0; t < QT; t++) {
-    const int r = row0 + 16 * t + col;
-    const bool there = r < rows;
-    const int token = there ? r / a.group : 0, position = e.len - e.n + token;
-    begin[t] = there ? key_begin(a, position) : 0;
-    end[t] = there ? key_end(a, e.len, position) : 0;
-    const uint16_t* src = a.q + (int64_t)(e.start + token) * a.q_stride + (int64_t)(head * a.group + (there ? r % a.group : 0)) * a.q_head + 8 * g;
-#pragma unroll
-    for (int i = 0; i < KB; i++) {
-      u4 x = {0, 0, 0, 0};
-      if (there) {
-        if (a.vec) {
-          x = *(const u4*)(src + 32 * i);
-        } else {
-#pragma unroll
-          for (int j = 0; j < 4; j++) x[j] = src[32 * i + 2 * j] | (uint32_t)src[32 * i + 2 * j + 1] << 16;
-        }
-      }
-      q[i][t] = __builtin_bit_cast(h8, x);
-    }
+    for (int j = 0; j < 4; j++) dst[j] = y[j];
   }
-  // the piece's steps that some row of the tile sees, and those in which every row sees every key
-  const int first_token = row0 / a.group, last_token = min(row0 + ROWS, rows) - 1;
-  const int p_first = e.len - e.n + first_token, p_last = e.len - e.n + last_token / a.group;
-  const int step_end = (key_end(a, e.len, p_last) + kStep - 1) / kStep, step_begin = key_begin(a, p_first) / kStep;
-  const int from = max((int)min((int64_t)it.piece * per_piece, (int64_t)0x7FFFFFF) + e.lo / kStep, step_begin);
-  const int to = min((int)min((int64_t)(it.piece + 1) * per_piece, (int64_t)0x7FFFFFF) + e.lo / kStep, step_end);
-  const int whole_begin = key_begin(a, p_last), whole_end = key_end(a, e.len, p_first);
+}
+__device__ __forceinline__ void store_lse(const AttentionArgs& a, const Extent& e, int head, int r, float top, float sum) {
+  if (!a.lse) return;
+  const int token = (int)a.by_group.quotient((uint32_t)r);
+  a.lse[(int64_t)(e.start + token) * a.lse_stride + head * a.group + r - token * a.group] = sum > 0 || sum != sum ? (top - kLift + __log2f(sum)) * 0.69314718056f : -INFINITY;
+}
 
-  f4 o[DT][QT];
-  float m[QT], l[QT];
+// Adds up `count` parts of a row tile, from share `first` on.  D / 4 lanes take a row, four channels each; of the workgroup's groups of
+// lanes as many take the rows as there are (a power of two), and the others share the parts of a row; 8 parts are asked for before the
+// first is used.
+template <int D, int THREADS>
+__device__ __forceinline__ void join_parts(const AttentionArgs& a, const Extent& e, __amdgpu_buffer_rsrc_t left, int head, int row0, int rows, int first, int count, float* lds) {
+  constexpr int LANES = D / 4, GROUPS = THREADS / LANES, AHEAD = 8;
+  f4* const xs = (f4*)lds;             // [group][lane]
+  f2* const stats = (f2*)(xs + THREADS);  // [group]
+  const int group = threadIdx.x / LANES, c = threadIdx.x % LANES;
+  int takers = 1;  // groups that take rows
+  while (takers < rows && takers < GROUPS) takers *= 2;
+  const int sharers = GROUPS / takers, mine = group / takers;
+  for (int i0 = 0; i0 < rows; i0 += takers) {
+    const int i = i0 + group % takers;
+    float top = -INFINITY, sum = 0;
+    f4 x = {0, 0, 0, 0};
+    for (int s0 = mine; s0 < count; s0 += sharers * AHEAD) {
+      f4 from[AHEAD];
+      f2 stat[AHEAD];
 #pragma unroll
-  for (int t = 0; t < QT; t++) {
-    m[t] = -INFINITY, l[t] = 0;
+      for (int j = 0; j < AHEAD; j++) {
+        const int s = s0 + j * sharers;
+        const int at = s < count && i < rows ? ((2 * (first + s) + (s == 0)) * a.part_rows + i) * (D + 4) * 4 : 0x7FFE0000;  // nothing is read there
+        from[j] = __builtin_bit_cast(f4, __builtin_amdgcn_raw_buffer_load_b128(left, at + 16 + 16 * c, 0, kDeviceScope));
+        stat[j] = __builtin_bit_cast(f2, __builtin_amdgcn_raw_buffer_load_b64(left, at, 0, kDeviceScope));
+        if (s >= count) stat[j] = f2{-INFINITY, 0};
+      }
+      float most = top;
 #pragma unroll
-    for (int d = 0; d < DT; d++) o[d][t] = f4{0, 0, 0, 0};
-  }
-  for (int step = from + wave; step < to; step += kStreamWaves) {
-    StepData<D, G> x;
-    x.load(a, it.b, head, step, lane);
-    f4 s[2][QT];
+      for (int j = 0; j < AHEAD; j++) most = fmaxf(most, stat[j][0]);
+      const float less = top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top - most);
+      top = most;
+      sum *= less, x *= less;
 #pragma unroll
-    for (int u = 0; u < 2; u++) {
-#pragma unroll
-      for (int t = 0; t < QT; t++) s[u][t] = f4{0, 0, 0, 0};
-#pragma unroll
-      for (int i = 0; i < KB; i++) {
-        const h8 k = restore_k(x.k[u].w[i], x.sk[u].s[32 * i / G]);
-#pragma unroll
-        for (int t = 0; t < QT; t++) s[u][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[i][t], s[u][t], 0, 0, 0);
+      for (int j = 0; j < AHEAD; j++) {
+        const float by = stat[j][0] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(stat[j][0] - top);
+        sum += stat[j][1] * by;
+        x += from[j] * by;
       }
     }
-    const bool whole = step * kStep >= whole_begin && (step + 1) * kStep <= whole_end && x.held[0] && x.held[1];
-    h8 p[QT];
+    __syncthreads();  // what was in LDS has been read
+    xs[threadIdx.x] = x;
+    if (c == 0) stats[group] = f2{top, sum};
+    __syncthreads();
+    if (mine == 0 && i < rows) {
+      top = -INFINITY, sum = 0;
+      x = f4{0, 0, 0, 0};
+      for (int j = 0; j < sharers; j++) top = fmaxf(top, stats[j * takers + group][0]);
+      for (int j = 0; j < sharers; j++) {
+        const f2 stat = stats[j * takers + group];
+        const float by = stat[0] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(stat[0] - top);
+        sum += stat[1] * by;
+        x += xs[(j * takers + group) * LANES + c] * by;
+      }
+      store_out(a, e, head, row0 + i, 4 * c, x * (sum > 0 || sum != sum ? 1.0f / sum : 0.0f));
+      if (c == 0) store_lse(a, e, head, row0 + i, top, sum);
+    }
+  }
+}
+
+// Wavefronts of a workgroup, and workgroups of a compute unit: what the registers allow.
+constexpr int stream_waves(int, int) { return 4; }
+constexpr int stream_groups(int d, int qt) { return d * qt <= 128 ? 3 : d * qt < 512 ? 2 : 1; }
+
+template <int D, int G, int QT>
+__global__ __launch_bounds__(64 * stream_waves(D, QT), stream_groups(D, QT) * stream_waves(D, QT) / 4) void stream_kernel(AttentionArgs a) {
+  constexpr int kStreamWaves = stream_waves(D, QT), ROWS = 16 * QT, RUNS = D / G, DT = D / 16, KB = D / 32, AT_ONCE = DT < 8 ? DT : 8;
+  const int wave = uniform((int)threadIdx.x >> 6), lane = lane_id();
+  const int share = (int)a.v.heads.quotient(blockIdx.x), head = blockIdx.x - share * a.v.kv_heads;
+  // While keys are read: the rows of q as the matrix instructions take them, and V's scales of each wavefront's step.  Then the
+  // wavefronts' results, eight d-tiles of a column tile at a time.
+  constexpr int Q_BYTES = KB * QT * 1024, STAGE = 64 * RUNS, PARTS = kStreamWaves * AT_ONCE * 1024;
+  __shared__ __align__(16) uint8_t shared[Q_BYTES + kStreamWaves * STAGE > PARTS ? Q_BYTES + kStreamWaves * STAGE : PARTS];
+  __shared__ float tops[kStreamWaves][ROWS], sums[kStreamWaves][ROWS];
+  __shared__ bool all_there;
+  h8* const q_rows = (h8*)shared;
+  uint8_t* const stage = shared + Q_BYTES + wave * STAGE;
+  f4* const parts = (f4*)shared;
+
+  const Extent first_64 = extent_of<ROWS>(a, lane);
+  const Split split = split_of<ROWS>(a, first_64);
+  uint32_t now = share * split.per;
+  const uint32_t stop = min(now + split.per, split.total);
+  Place place;
+  while (now < stop && place_of<ROWS>(a, first_64, now, &place)) {
+    const Extent& e = place.e;
+    const int rows = e.n * a.group, row0 = place.row_tile * ROWS;
+    // the share's steps of the tile that some row sees, and the keys that every row sees
+    const int steps = (int)min((uint32_t)(e.steps - place.step), stop - now);
+    const bool alone = a.shares == 0 || steps == e.steps;
+    const int last_row = min(row0 + ROWS, rows) - 1;
+    const int p_first = e.len - e.n + (int)a.by_group.quotient((uint32_t)row0), p_last = e.len - e.n + (int)a.by_group.quotient((uint32_t)last_row);
+    const int from = uniform(max(e.lo / kStep + place.step, key_begin(a, p_first) / kStep));
+    const int to = uniform(min(e.lo / kStep + (alone ? e.steps : place.step + steps), (key_end(a, e.len, p_last) + kStep - 1) / kStep));
+    const int whole_begin = uniform(key_begin(a, p_last)), whole_end = uniform(key_end(a, e.len, p_first));
+    Pages pages;
+    pages.look_up(a, place.b, from + wave + kStreamWaves * hidden(lane), to);
+    // the tile's rows: a lane has one of each column tile
+    const int load_lane = hidden(lane);
 #pragma unroll
     for (int t = 0; t < QT; t++) {
-      if (!whole) {
+      const int r = row0 + 16 * t + (load_lane & 15), token = (int)a.by_group.quotient((uint32_t)r);
+      const uint16_t* src = a.q + (int64_t)(e.start + token) * a.q_stride + (int64_t)(head * a.group + r - token * a.group) * a.q_head + 8 * (load_lane >> 4);
+#pragma unroll
+      for (int i0 = 0; i0 < KB; i0 += kStreamWaves) {
+        const int i = i0 + wave;
+        if (KB < kStreamWaves && i >= KB) break;
+        u4 x = {0, 0, 0, 0};
+        if (r < rows) x = load_half8(src + 32 * i, a.vec);
+        q_rows[(i * QT + t) * 64 + lane] = __builtin_bit_cast(h8, x);
+      }
+    }
+    __syncthreads();
+
+    f4 o[DT][QT];
+    float m[QT], l[QT];
+#pragma unroll
+    for (int t = 0; t < QT; t++) {
+      m[t] = -INFINITY, l[t] = 0;
+#pragma unroll
+      for (int d = 0; d < DT; d++) o[d][t] = f4{0, 0, 0, 0};
+    }
+    // S^T of the two tiles of a step: a lane has four keys of each and its row.
+    auto scores = [&](const StepK<D, G>& k, f4(&s)[2][QT]) {
+#pragma unroll
+      for (int i = 0; i < KB; i++) {
+        const h8 k0 = restore_k(k.w[0].w[i], k.s[0].twice(32 * i / G)), k1 = restore_k(k.w[1].w[i], k.s[1].twice(32 * i / G));
+#pragma unroll
+        for (int t = 0; t < QT; t++) {
+          const h8 q = q_rows[(i * QT + t) * 64 + lane];
+          s[0][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, q, i ? s[0][t] : f4{0, 0, 0, 0}, 0, 0, 0);
+          s[1][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, q, i ? s[1][t] : f4{0, 0, 0, 0}, 0, 0, 0);
+        }
+      }
+    };
+    // P from S, and the statistics.  The maximum is raised only where a score passes it by more than the slack, then for all lanes that
+    // share the row.
+    auto weights = [&](f4(&s)[2][QT], h8(&p)[QT]) {
+#pragma unroll
+      for (int t = 0; t < QT; t++) {
+        float top = s[0][t][0];
+#pragma unroll
+        for (int i = 1; i < 8; i++) top = fmaxf(top, s[i / 4][t][i % 4]);
+        top *= a.scale2;
+        if (__ballot(top > m[t] + kSlack)) {
+          top = fmaxf(top, m[t]);
+          top = fmaxf(top, __shfl_xor(top, 16, 64));
+          top = fmaxf(top, __shfl_xor(top, 32, 64));
+          const float less = top > m[t] ? __builtin_amdgcn_exp2f(m[t] - top) : 1.0f;
+          m[t] = top;
+          l[t] *= less;
+#pragma unroll
+          for (int d = 0; d < DT; d++) o[d][t] *= less;
+        }
+        const float sub = m[t] == -INFINITY ? 0.0f : m[t] - kLift;
 #pragma unroll
         for (int u = 0; u < 2; u++)
 #pragma unroll
           for (int i = 0; i < 4; i++) {
-            const int key = step * kStep + 16 * u + 4 * g + i;
-            if (key < begin[t] || key >= end[t] || !x.held[u]) s[u][t][i] = -INFINITY;
+            const float v = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][t][i], a.scale2, -sub));
+            l[t] += v;
+            p[t][4 * u + i] = (_Float16)v;
           }
       }
-      float top = m[t];
+    };
+    // O^T += V^T P^T; scale(tile, word): a word of the tile's scales, two tokens of a run
+    auto multiply = [&](const StepV<D, G>& v, const h8(&p)[QT], auto scale) {
 #pragma unroll
-      for (int u = 0; u < 2; u++)
+      for (int i = 0; i < KB; i++) {
+        u2 va[2], vb[2];
 #pragma unroll
-        for (int i = 0; i < 4; i++) top = fmaxf(top, s[u][t][i] * a.scale2);
-      // the maximum is raised only where a score passes it by more than the slack: then for all lanes that share the row
-      if (__ballot(top > m[t] + kSlack)) {
-        top = fmaxf(top, __shfl_xor(top, 16, 64));
-        top = fmaxf(top, __shfl_xor(top, 32, 64));
-        const float less = top > m[t] ? __builtin_amdgcn_exp2f(m[t] - top) : 1.0f;
-        m[t] = top;
-        l[t] *= less;
-#pragma unroll
-        for (int d = 0; d < DT; d++) o[d][t] *= less;
-      }
-      const float sub = m[t] == -INFINITY ? 0.0f : m[t] - kLift;
-#pragma unroll
-      for (int u = 0; u < 2; u++)
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-          const float v = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][t][i], a.scale2, -sub));
-          l[t] += v;
-          p[t][4 * u + i] = (_Float16)v;
+        for (int u = 0; u < 2; u++) {
+          const u2 s = scale(u, 32 * i / G);
+          restore_v(v.w[u].w[i], s[0], s[1], &va[u], &vb[u]);
         }
-    }
 #pragma unroll
-    for (int i = 0; i < KB; i++) {
-      const int run = 32 * i / G * 4;
-      h4 va[2], vb[2];
+        for (int t = 0; t < QT; t++) {
+          o[2 * i][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(join_halves(va[0], va[1]), p[t], o[2 * i][t], 0, 0, 0);
+          o[2 * i + 1][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(join_halves(vb[0], vb[1]), p[t], o[2 * i + 1][t], 0, 0, 0);
+        }
+      }
+    };
+    auto put_scales = [&](const StepV<D, G>& v) {
+      wave_sync();  // the last step's have been read
+#pragma unroll
+      for (int u = 0; u < 2; u++)
+        if (lane < 8 * RUNS) *(uint32_t*)(stage + 32 * RUNS * u + 4 * lane) = v.s[u];
+      wave_sync();
+    };
+    // The next step's keys are asked for as soon as this one's have been used, and its values then; behind the last step that one's
+    // again, so that what is waited for is always the older request.
+    int step = from + wave, at = 0;
+    if (step < to) {
+      StepK<D, G> k;
+      StepV<D, G> v;
 #pragma unroll
       for (int u = 0; u < 2; u++) {
-        h4 sv = {x.sv[u].s[run], x.sv[u].s[run + 1], x.sv[u].s[run + 2], x.sv[u].s[run + 3]};
-        if (!whole) {  // a masked key's P is 0, and 0 times what it holds has to be
-#pragma unroll
-          for (int j = 0; j < 4; j++)
-            if (not_finite(sv[j])) sv[j] = (_Float16)0;
+        const Tile tile(a, pages, head, step, u, 0);
+        k.load(a, tile, u, lane), v.load(a, tile, u, lane);
+      }
+      for (;;) {
+        f4 s[2][QT];
+        h8 p[QT];
+        scores(k, s);
+        const bool held[2] = {of_lane(pages.number[0], at) >= 0, of_lane(pages.number[1], at) >= 0};
+        const bool whole = step * kStep >= whole_begin && (step + 1) * kStep <= whole_end && held[0] && held[1];  // every row sees every key
+        const bool more = step + kStreamWaves < to;
+        if (more && ++at == 64) {
+          at = 0;
+          pages.look_up(a, place.b, step + kStreamWaves + kStreamWaves * hidden(lane), to);
         }
-        restore_v(x.v[u].w[i], sv, &va[u], &vb[u]);
-      }
+        const int next = more ? step + kStreamWaves : step;
+        const Tile t0(a, pages, head, next, 0, at), t1(a, pages, head, next, 1, at);
+        k.load(a, t0, 0, lane), k.load(a, t1, 1, lane);
+        int begin[QT], end[QT];
+        if (!whole) {
+          const int mine = hidden(lane), key = step * kStep + 4 * (mine >> 4);
 #pragma unroll
-      for (int t = 0; t < QT; t++) {
-        o[2 * i][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(join_halves(va[0], va[1]), p[t], o[2 * i][t], 0, 0, 0);
-        o[2 * i + 1][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(join_halves(vb[0], vb[1]), p[t], o[2 * i + 1][t], 0, 0, 0);
-      }
-    }
-    if (!whole) nan_of_seen_keys<D, G, QT>(x, step * kStep, begin, end, o);
-  }
-
-  // The wavefronts' results are joined in their order; eight d-tiles of one column tile at a time go through LDS.
-  constexpr int AT_ONCE = DT < 8 ? DT : 8;
-  __shared__ __align__(16) f4 parts[kStreamWaves][AT_ONCE][64];
-  __shared__ float tops[kStreamWaves][ROWS], sums[kStreamWaves][ROWS];
+          for (int t = 0; t < QT; t++) {
+            const int r = row0 + 16 * t + (mine & 15), position = e.len - e.n + (int)a.by_group.quotient((uint32_t)r);
+            begin[t] = r < rows ? key_begin(a, position) : 0;
+            end[t] = r < rows ? key_end(a, e.len, position) : 0;
 #pragma unroll
-  for (int t = 0; t < QT; t++) {
-    l[t] += __shfl_xor(l[t], 16, 64);
-    l[t] += __shfl_xor(l[t], 32, 64);
-    if (g == 0) tops[wave][16 * t + col] = m[t], sums[wave][16 * t + col] = l[t];
-  }
-  __syncthreads();
-  const bool alone = it.pieces == 1;
-  float* const part = a.part + ((int64_t)(it.slot + it.piece) * a.v.kv_heads + head) * ROWS * (D + 2);
+            for (int u = 0; u < 2; u++)
 #pragma unroll
-  for (int t = 0; t < QT; t++) {
-    const int r = row0 + 16 * t + col;
-    float top = -INFINITY, sum = 0, by[kStreamWaves];
-#pragma unroll
-    for (int w = 0; w < kStreamWaves; w++) top = fmaxf(top, tops[w][16 * t + col]);
-#pragma unroll
-    for (int w = 0; w < kStreamWaves; w++) {
-      const float mine = tops[w][16 * t + col];
-      by[w] = mine == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mine - top);
-      sum += sums[w][16 * t + col] * by[w];
-    }
-    const float scale = alone ? (sum > 0 || sum != sum ? 1.0f / sum : 0.0f) : 1.0f;
-#pragma unroll
-    for (int d0 = 0; d0 < DT; d0 += AT_ONCE) {
-      __syncthreads();
-#pragma unroll
-      for (int d = 0; d < AT_ONCE; d++) parts[wave][d][lane] = o[d0 + d][t];
-      __syncthreads();
-      for (int d = wave; d < AT_ONCE; d += kStreamWaves) {
-        f4 x = {0, 0, 0, 0};
-#pragma unroll
-        for (int w = 0; w < kStreamWaves; w++) x += parts[w][d][lane] * by[w];
-        if (r >= rows) continue;
-        x *= scale;
-        const int channel = 16 * (d0 + d) + 4 * g;
-        if (alone) {
-          uint16_t* const dst = a.out + (int64_t)(e.start + r / a.group) * a.out_stride + (int64_t)(head * a.group + r % a.group) * a.out_head + channel;
-          const h4 y = {(_Float16)x[0], (_Float16)x[1], (_Float16)x[2], (_Float16)x[3]};
-          if (a.vec) {
-            *(h4*)dst = y;
-          } else {
-#pragma unroll
-            for (int j = 0; j < 4; j++) ((_Float16*)dst)[j] = y[j];
+              for (int i = 0; i < 4; i++)
+                if (key + 16 * u + i < begin[t] || key + 16 * u + i >= end[t] || !held[u]) s[u][t][i] = -INFINITY;
           }
-        } else {
-          float* const dst = part + (16 * t + col) * (D + 2) + 2 + channel;
+        }
+        weights(s, p);
+        put_scales(v);
+        if (!whole) nan_of_seen_keys<RUNS, G, QT, DT>(stage, hidden(lane), step * kStep, begin, end, o);
+        multiply(v, p, [&](int u, int run) { return *(const u2*)(stage + ((u * 4 + (lane >> 4)) * RUNS + run) * 8); });
+        v.load(a, t0, 0, lane), v.load(a, t1, 1, lane);
+        if (!more) break;
+        step = next;
+      }
+    }
+
+    // The wavefronts' results are joined in their order.
+    const int done = hidden(lane), g = done >> 4, col = done & 15;
 #pragma unroll
-          for (int j = 0; j < 4; j++) dst[j] = x[j];
+    for (int t = 0; t < QT; t++) {
+      l[t] += __shfl_xor(l[t], 16, 64);
+      l[t] += __shfl_xor(l[t], 32, 64);
+      if (g == 0) tops[wave][16 * t + col] = m[t], sums[wave][16 * t + col] = l[t];
+    }
+    const int left_size = uniform(alone ? 0 : 2 * a.shares * a.part_rows * (D + 4) * 4);  // of this head
+    const __amdgpu_buffer_rsrc_t left = __builtin_amdgcn_make_buffer_rsrc((void*)(a.parts + (int64_t)uniform(head) * 2 * a.shares * a.part_rows * (D + 4)), 0, left_size, 0x00020000);
+    const int part = (2 * share + (place.step == 0)) * a.part_rows;
+#pragma unroll
+    for (int t = 0; t < QT; t++) {
+      const int r = row0 + 16 * t + col;
+      float top = -INFINITY, sum = 0, by[kStreamWaves], scale = 0;
+#pragma unroll
+      for (int d0 = 0; d0 < DT; d0 += AT_ONCE) {
+        __syncthreads();
+#pragma unroll
+        for (int d = 0; d < AT_ONCE; d++) parts[(wave * AT_ONCE + d) * 64 + done] = o[d0 + d][t];
+        __syncthreads();
+        if (d0 == 0) {
+#pragma unroll
+          for (int w = 0; w < kStreamWaves; w++) top = fmaxf(top, tops[w][16 * t + col]);
+#pragma unroll
+          for (int w = 0; w < kStreamWaves; w++) {
+            const float mine = tops[w][16 * t + col];
+            by[w] = mine == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mine - top);
+            sum += sums[w][16 * t + col] * by[w];
+          }
+          scale = alone ? (sum > 0 || sum != sum ? 1.0f / sum : 0.0f) : 1.0f;
+        }
+        for (int d = wave; d < AT_ONCE; d += kStreamWaves) {
+          f4 x = {0, 0, 0, 0};
+#pragma unroll
+          for (int w = 0; w < kStreamWaves; w++) x += parts[(w * AT_ONCE + d) * 64 + done] * by[w];
+          if (r >= rows) continue;
+          const int channel = 16 * (d0 + d) + 4 * g;
+          if (alone)
+            store_out(a, e, head, r, channel, x * scale);
+          else
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4, x), left, ((part + 16 * t + col) * (D + 4) + 4 + channel) * 4, 0, kDeviceScope);
         }
       }
-    }
-    if (wave == 0 && g == 0 && r < rows) {
-      if (!alone) {
-        part[(16 * t + col) * (D + 2)] = top;
-        part[(16 * t + col) * (D + 2) + 1] = sum;
-      } else if (a.lse) {
-        a.lse[(int64_t)(e.start + r / a.group) * a.lse_stride + head * a.group + r % a.group] = sum > 0 || sum != sum ? (top - kLift + __log2f(sum)) * 0.69314718056f : -INFINITY;
+      if (wave == 0 && g == 0 && r < rows) {
+        if (alone)
+          store_lse(a, e, head, r, top, sum);
+        else
+          __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u2, f2{top, sum}), left, (part + 16 * t + col) * (D + 4) * 4, 0, kDeviceScope);
       }
     }
-  }
-}
-
-// Adds up the pieces of a row tile that has several.  A wavefront takes rows of the tile, its lanes the channels.
-template <int D, int ROWS>
-__global__ __launch_bounds__(256) void join_kernel(AttentionArgs a) {
-  const int wave = threadIdx.x >> 6, lane = lane_id(), head = blockIdx.x % a.v.kv_heads;
-  Item it;
-  const int per_piece = piece_steps<ROWS>(a);
-  if (!find_item<ROWS, true>(a, per_piece, blockIdx.x / a.v.kv_heads, &it) || it.pieces == 1) return;
-  const Extent e = extent_of<ROWS>(a, it.b);
-  const int rows = min(e.n * a.group - it.row_tile * ROWS, ROWS);
-  const int64_t stride = (int64_t)a.v.kv_heads * ROWS * (D + 2);
-  for (int i = wave; i < rows; i += 4) {
-    const float* const part = a.part + ((int64_t)it.slot * a.v.kv_heads + head) * ROWS * (D + 2) + i * (D + 2);
-    float top = -INFINITY, sum = 0, x[D / 64];
-#pragma unroll
-    for (int j = 0; j < D / 64; j++) x[j] = 0;
-    for (int s = 0; s < it.pieces; s++) top = fmaxf(top, part[s * stride]);
-    for (int s = 0; s < it.pieces; s++) {
-      const float mine = part[s * stride], by = mine == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mine - top);
-      sum += part[s * stride + 1] * by;
-#pragma unroll
-      for (int j = 0; j < D / 64; j++) x[j] += part[s * stride + 2 + 64 * j + lane] * by;
+    if (!alone) {
+      const uint32_t first = place.first / split.per;
+      const int count = (int)((place.first + e.steps - 1) / split.per - first) + 1;
+      // every wavefront's stores have been acknowledged before the workgroup is counted in, and the parts are asked for after the count
+      // has come back; they go to the level of the memory system that all compute units share
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+      if (threadIdx.x == 0) {
+        uint32_t* const counter = a.counts + head * a.shares + first;
+        const bool last = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)count - 1;
+        if (last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        all_there = last;
+      }
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+      if (all_there) join_parts<D, 64 * kStreamWaves>(a, e, left, head, row0, min(rows - row0, ROWS), (int)first, count, (float*)shared);
     }
-    const int r = it.row_tile * ROWS + i;
-    const float scale = sum > 0 || sum != sum ? 1.0f / sum : 0.0f;
-    uint16_t* const dst = a.out + (int64_t)(e.start + r / a.group) * a.out_stride + (int64_t)(head * a.group + r % a.group) * a.out_head;
-#pragma unroll
-    for (int j = 0; j < D / 64; j++) dst[64 * j + lane] = __builtin_bit_cast(uint16_t, (_Float16)(x[j] * scale));
-    if (a.lse && lane == 0)
-      a.lse[(int64_t)(e.start + r / a.group) * a.lse_stride + head * a.group + r % a.group] = sum > 0 || sum != sum ? (top - kLift + __log2f(sum)) * 0.69314718056f : -INFINITY;
+    now += a.shares > 0 ? steps : 1;
+    __syncthreads();  // what the tile left in LDS has been read
   }
 }
 
 // ---- launch ------------------------------------------------------------------------------------------
-constexpr int kTargetGroups = 1024;  // workgroups that fill the chip
+constexpr int kComputeUnits = 256;
+constexpr size_t kCountBytes = 64 * 1024;  // of a workspace: counts of any call (kv_heads x shares of them), at its front
+static_assert(4 * kComputeUnits * sizeof(uint32_t) <= kCountBytes && AMS_KV_MAX_HEADS * sizeof(uint32_t) <= kCountBytes, "one for each share of each head");
 
 struct Plan {
-  int qt, rows;
-  int64_t row_tiles;    // at most so many over all sequences
-  int64_t tile_steps;   // at most so many steps of one row tile
-  int64_t pieces;       // heads_pieces
-  size_t workspace;     // bytes that this many pieces need
+  int qt, rows, part_rows;
+  int64_t row_tiles;  // at most so many over all sequences
+  int64_t shares;
+  size_t workspace;   // bytes that this many shares need
 };
 Plan make_plan(const ams_kv_cache* c, int64_t rows, int heads, int64_t max_q_len, size_t workspace) {
   Plan p;
@@ -427,13 +583,14 @@ Plan make_plan(const ams_kv_cache* c, int64_t rows, int heads, int64_t max_q_len
   p.qt = most <= 16 ? 1 : most <= 32 || c->head_dim == 256 ? 2 : 4;
   p.rows = 16 * p.qt;
   p.row_tiles = c->q_starts ? rows * R / p.rows + c->batch : c->batch * (int64_t)((R + p.rows - 1) / p.rows);
-  p.tile_steps = ((int64_t)c->table_width * c->page_size + kStep - 1) / kStep;
-  const size_t slot = (size_t)c->kv_heads * p.rows * (c->head_dim + 2) * sizeof(float);
-  p.pieces = std::max<int64_t>(kTargetGroups / c->kv_heads, 1);
-  // sequences that are cut have fewer than twice as many pieces as all have on average
-  if (p.tile_steps <= kMinPiece) p.pieces = 0;
-  p.pieces = std::min<int64_t>(p.pieces, (int64_t)(std::min<size_t>(workspace, AMS_KV_WORKSPACE_BYTES) / slot / 2));
-  p.workspace = 2 * (size_t)p.pieces * slot;
+  const int64_t tile_steps = std::max<int64_t>(((int64_t)c->table_width * c->page_size + kStep - 1) / kStep, 1);
+  p.part_rows = (int)std::min<int64_t>(c->q_starts ? rows * R : R, p.rows);
+  const size_t part = (size_t)c->kv_heads * p.part_rows * (c->head_dim + 4) * sizeof(float);
+  p.shares = std::max<int64_t>(stream_groups(c->head_dim, p.qt) * kComputeUnits / c->kv_heads, 1);
+  if (tile_steps <= kMinShare || p.row_tiles * tile_steps > 0x7FFFFFFF) p.shares = 0;
+  const size_t room = std::min<size_t>(workspace, AMS_KV_WORKSPACE_BYTES);
+  p.shares = std::min<int64_t>(p.shares, room < kCountBytes ? 0 : (int64_t)((room - kCountBytes) / part / 2));
+  p.workspace = p.shares > 0 ? kCountBytes + 2 * (size_t)p.shares * part : 0;
   return p;
 }
 
@@ -463,31 +620,24 @@ int ams_kv_attention(const ams_kv_cache* cache, const uint16_t* Q, uint16_t* O, 
   if (!aligned(Q, 2) || !aligned(O, 2) || !aligned(lse, 4) || !aligned(workspace, 16)) return AMS_ERR_ALIGN;
   if (const int rc = device_status(); rc != AMS_OK) return rc;
   if (rows == 0 || cache->batch == 0) return AMS_OK;
-  a.q = Q, a.out = O, a.lse = lse, a.part = (float*)workspace;
+  a.q = Q, a.out = O, a.lse = lse, a.counts = (uint32_t*)workspace, a.parts = (float*)((uint8_t*)workspace + kCountBytes);
   a.q_stride = q_stride, a.q_head = q_head_stride, a.out_stride = o_stride, a.out_head = o_head_stride, a.lse_stride = lse_stride;
   a.scale2 = softmax_scale * 1.44269504089f;
-  a.group = heads / cache->kv_heads;
+  a.group = heads / cache->kv_heads, a.by_group = divisor((uint32_t)a.group);
   a.causal = causal != 0, a.window = (int)std::min<int64_t>(window, 0x3FFFFFFF);
   a.vec = aligned(Q, 16) && aligned(O, 8) && (q_stride | q_head_stride) % 8 == 0 && (o_stride | o_head_stride) % 4 == 0;
   const Plan p = make_plan(cache, rows, heads, max_q_len, workspace ? workspace_bytes : 0);
-  a.heads_pieces = (int)p.pieces;
-  const int64_t items = std::min(p.row_tiles + p.pieces, p.row_tiles * ((p.tile_steps + kMinPiece - 1) / kMinPiece + 1));
-  const int64_t grid = items * cache->kv_heads, joins = p.row_tiles * cache->kv_heads;
+  a.shares = (int)p.shares, a.part_rows = p.part_rows;
+  const int64_t grid = (p.shares > 0 ? p.shares : p.row_tiles) * cache->kv_heads;
   if (grid > 0x7FFFFFFF) return AMS_ERR_SHAPE;
-  auto launch = [&](auto kernel, int64_t n) { hipLaunchKernelGGL(kernel, dim3((unsigned)n), dim3(256), 0, (hipStream_t)stream, a); };
   dispatch(cache->head_dim, cache->scale_group, [&](auto d, auto g) {
     constexpr int D = decltype(d)::value, G = decltype(g)::value;
+    auto launch = [&](auto kernel, int qt) { hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * stream_waves(D, qt)), 0, (hipStream_t)stream, a); };
     switch (p.qt) {
-      case 1: launch(stream_kernel<D, G, 1>, grid); break;
-      case 2: launch(stream_kernel<D, G, 2>, grid); break;
+      case 1: launch(stream_kernel<D, G, 1>, 1); break;
+      case 2: launch(stream_kernel<D, G, 2>, 2); break;
       default:
-        if constexpr (D < 256) launch(stream_kernel<D, G, 4>, grid);  // 256 accumulators do not fit beside the rows
-    }
-    if (p.pieces == 0) return;
-    switch (p.qt) {
-      case 1: launch(join_kernel<D, 16>, joins); break;
-      case 2: launch(join_kernel<D, 32>, joins); break;
-      default: launch(join_kernel<D, 64>, joins); break;
+        if constexpr (D < 256) launch(stream_kernel<D, G, 4>, 4);  // 256 accumulators do not fit beside the rows
     }
   });
   return hipGetLastError() == hipSuccess ? AMS_OK : AMS_ERR_LAUNCH;

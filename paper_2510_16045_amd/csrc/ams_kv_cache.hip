@@ -90,10 +90,11 @@ __global__ __launch_bounds__(64 * kWaves) void write_kernel(RowsArgs a) {
   constexpr int RUNS = D / G, CHUNKS = D / 8, W = Lane<D>::W, CODES = 8 * D, SCALES = kTile * RUNS * 2;
   __shared__ __align__(16) uint8_t image[kWaves][2 * (CODES + SCALES)];
   const int wave = threadIdx.x >> 6, lane = lane_id();
-  const int head = blockIdx.x % a.v.kv_heads, item = (blockIdx.x / a.v.kv_heads) * kWaves + wave;
+  const int group = (int)a.v.heads.quotient(blockIdx.x), head = blockIdx.x - group * a.v.kv_heads, item = group * kWaves + wave;
   TileRows t;
   if (!tile_rows(a.v, item, &t) || t.tile < 0) return;
-  uint8_t* const block = block_of(a.v, t.b, t.tile, head);
+  int in_page;
+  uint8_t* const block = block_of(a.v, t.b, t.tile, head, &in_page);
   if (!block) return;
   uint8_t* const img = image[wave];
   for (int u = lane; u < kTile * CHUNKS; u += 64) {
@@ -130,7 +131,6 @@ __global__ __launch_bounds__(64 * kWaves) void write_kernel(RowsArgs a) {
     }
   }
   wave_sync();
-  const int in_page = t.tile % a.v.page_tiles;
   uint8_t* const kc = block + in_page * CODES;
   uint8_t* const vc = kc + a.v.codes;
   uint8_t* const ks = block + 2 * a.v.codes + in_page * SCALES;
@@ -168,10 +168,11 @@ __global__ __launch_bounds__(64 * kWaves) void read_kernel(RowsArgs a) {
   constexpr int RUNS = D / G, W = Lane<D>::W, CODES = 8 * D, SCALES = kTile * RUNS * 2, ROW = D + 8;
   __shared__ __align__(16) _Float16 image[kWaves][kTile * ROW];
   const int wave = threadIdx.x >> 6, lane = lane_id();
-  const int head = blockIdx.x % a.v.kv_heads, item = (blockIdx.x / a.v.kv_heads) * kWaves + wave;
+  const int group = (int)a.v.heads.quotient(blockIdx.x), head = blockIdx.x - group * a.v.kv_heads, item = group * kWaves + wave;
   TileRows t;
   if (!tile_rows(a.v, item, &t)) return;
-  const uint8_t* const block = t.tile < 0 ? nullptr : block_of(a.v, t.b, t.tile, head);
+  int in_page = 0;
+  const uint8_t* const block = t.tile < 0 ? nullptr : block_of(a.v, t.b, t.tile, head, &in_page);
   auto there = [&](int token) { return token >= t.first && token < t.end; };
   auto row_of = [&](uint16_t* p, int64_t stride, int64_t h, int token) { return p + (int64_t)(t.row + token) * stride + head * h; };
   if (!block) {
@@ -183,7 +184,7 @@ __global__ __launch_bounds__(64 * kWaves) void read_kernel(RowsArgs a) {
     }
     return;
   }
-  const int in_page = t.tile % a.v.page_tiles, g = lane >> 4, c = lane & 15;
+  const int g = lane >> 4, c = lane & 15;
   const uint8_t* const kc = block + in_page * CODES;
   const uint8_t* const ks = block + 2 * a.v.codes + in_page * SCALES;
   Lane<D> kw, vw;
@@ -196,18 +197,19 @@ __global__ __launch_bounds__(64 * kWaves) void read_kernel(RowsArgs a) {
   if (there(c)) {
 #pragma unroll
     for (int i = 0; i < Lane<D>::kWords; i++)
-      store8(row_of(a.k, a.k_stride, a.k_head, c) + 32 * i + 8 * g, __builtin_bit_cast(u4, restore_k(kw.w[i], sk.s[32 * i / G])), a.vec);
+      store8(row_of(a.k, a.k_stride, a.k_head, c) + 32 * i + 8 * g, __builtin_bit_cast(u4, restore_k(kw.w[i], sk.twice(32 * i / G))), a.vec);
   }
   _Float16* const img = image[wave];
 #pragma unroll
   for (int i = 0; i < Lane<D>::kWords; i++) {
-    const int run = 32 * i / G * 4;
-    h4 x, y;
-    restore_v(vw.w[i], h4{sv.s[run], sv.s[run + 1], sv.s[run + 2], sv.s[run + 3]}, &x, &y);
+    const int run = 32 * i / G * 2;
+    u2 x, y;
+    restore_v(vw.w[i], sv.w[run], sv.w[run + 1], &x, &y);
+    const h4 xs = __builtin_bit_cast(h4, x), ys = __builtin_bit_cast(h4, y);
 #pragma unroll
     for (int j = 0; j < 4; j++) {
-      img[(4 * g + j) * ROW + 32 * i + c] = x[j];
-      img[(4 * g + j) * ROW + 32 * i + 16 + c] = y[j];
+      img[(4 * g + j) * ROW + 32 * i + c] = xs[j];
+      img[(4 * g + j) * ROW + 32 * i + 16 + c] = ys[j];
     }
   }
   wave_sync();
@@ -260,7 +262,7 @@ int make_view(const ams_kv_cache* c, int64_t rows, View* v) {
   v->pages = (uint8_t*)c->pages, v->table = c->block_table, v->lens = c->kv_lens, v->starts = c->q_starts;
   v->table_stride = c->table_stride, v->page_bytes = (int64_t)c->kv_heads * p.block;
   v->n_pages = (int)c->n_pages, v->table_width = c->table_width, v->batch = c->batch, v->kv_heads = c->kv_heads, v->rows = (int)rows;
-  v->page_tiles = c->page_size / kTile, v->page_size = c->page_size, v->codes = p.codes, v->scales = p.scales, v->block = p.block;
+  v->page_tiles = divisor((uint32_t)(c->page_size / kTile)), v->heads = divisor((uint32_t)c->kv_heads), v->page_size = c->page_size, v->codes = p.codes, v->scales = p.scales, v->block = p.block;
   return AMS_OK;
 }
 

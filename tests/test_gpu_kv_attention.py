@@ -13,6 +13,22 @@ from tests.test_gpu_kv_cache import SIZES, dev, host, rows_of, starts_of, table_
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
+WORKSPACE = None
+
+
+@pytest.fixture(autouse=True, scope="module")
+def workspace():
+    """One for all calls of this file, whatever their shapes; its counts are zero after each test."""
+    global WORKSPACE
+    WORKSPACE = torch.zeros(16 << 20, dtype=torch.uint8, device="cuda")
+    yield
+    WORKSPACE = None
+
+
+@pytest.fixture(autouse=True)
+def counts_are_zero():
+    yield
+    assert not bool(WORKSPACE[:65536].any())
 
 
 def near(out, want, size, keys):
@@ -37,7 +53,7 @@ class Case:
 
     def run(self, workspace="own", q=None, out=None, lse=None, **more):
         if workspace == "own":
-            workspace = torch.empty(16 << 20, dtype=torch.uint8, device="cuda").fill_(255)  # its content is of no account
+            workspace = WORKSPACE
         return ams.ams_kv_attention(dev(self.q) if q is None else q, self.cache, self.table, self.kv_lens, self.G, q_starts=self.starts, causal=self.causal, window=self.window,
                                     workspace=workspace, out=out, lse=lse, **more)
 
@@ -110,7 +126,7 @@ def test_rows_without_a_key():
 @pytest.mark.parametrize("workspace", ["own", None, 200000, 16])
 def test_pieces(workspace):
     c = Case([3000, 5, 1111, 0, 260], [1] * 5, heads=8, kv_heads=1)
-    ws = workspace if workspace in ("own", None) else torch.empty(workspace, dtype=torch.uint8, device="cuda")
+    ws = workspace if workspace in ("own", None) else torch.zeros(workspace, dtype=torch.uint8, device="cuda")
     c.check(workspace=ws)
     a = c.run(workspace=ws)
     for _ in range(3):
@@ -237,7 +253,7 @@ def test_on_another_stream():
     c = Case([500, 40], [1, 1])
     want, q = c.run(), dev(c.q)
     side = torch.cuda.Stream()
-    ws, out = torch.empty(1 << 20, dtype=torch.uint8, device="cuda"), torch.zeros_like(want)
+    ws, out = torch.zeros(1 << 20, dtype=torch.uint8, device="cuda"), torch.zeros_like(want)
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):
         q2 = q * 1  # made on that stream
@@ -259,7 +275,7 @@ def test_a_captured_step_follows_the_lengths():
         write_all(x, table, seqs, G)
     k, v, q = (torch.zeros((B, n, D), dtype=torch.float16, device="cuda") for n in (kv_heads, kv_heads, heads))
     lens, out = dev(first), torch.zeros((B, heads, D), dtype=torch.float16, device="cuda")
-    ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    ws = torch.zeros(1 << 20, dtype=torch.uint8, device="cuda")
     ams.ams_init()
 
     def step(x, o):
