@@ -12,7 +12,8 @@
 //
 // Split of the work: the host knows neither lengths nor (with row starts) how many rows a sequence has, so every workgroup works it
 // out from them: the steps of all row tiles of a kv head, one tile after the other, are cut into equal shares, as many as there are
-// workgroups that fit on the chip at once.  A share may begin and end inside a tile.  Of a tile that lies in several shares every
+// workgroups that fit on the chip at once.  A share may begin and end inside a tile; that a workgroup begins a tile counts as much as
+// kTileSteps steps.  Where no tile has more than kUncutSteps, shares are made of whole tiles.  Of a tile that lies in several shares every
 // workgroup leaves its part (max, sum, O) in the workspace and counts itself in; the one that comes last adds all of them up, always in
 // the same order, and clears the count.  Nobody waits for anybody.
 #include "ams_kv.h"
@@ -25,7 +26,10 @@ namespace ams_kv {
 
 constexpr int kDeviceScope = 16;  // cache policy (sc1) of a buffer load or store that the whole device sees
 constexpr int kStep = 32;         // keys of a wavefront's step
-constexpr int kMinShare = 4;      // steps of a share: one for each wavefront
+constexpr int kMinShare = 16;     // steps of a share: four for each wavefront
+constexpr int kTileSteps = 14;    // what it takes to begin a tile and to leave its result, in steps
+constexpr int kUncutSteps = 32;   // a tile of so many is not cut: joining its parts takes longer than its steps
+constexpr int kMaxParts = 64;     // a tile in more parts costs its last workgroup more than the others gain
 constexpr float kLift = 8.0f;     // exponents of P are raised by this: below it P keeps fp16's full precision over 2^-22 of the largest
 constexpr float kSlack = 7.0f;    // how far (log2) a score may pass the running maximum before that is raised: 2^(8 + 7) is in fp16
 
@@ -40,7 +44,8 @@ struct AttentionArgs {
   float scale2;  // softmax_scale * log2(e)
   int group;     // R
   Divisor by_group;
-  int shares;        // of the steps of one kv head; 0: no tile is cut, a workgroup takes one
+  int shares;        // workgroups of one kv head
+  int cut;           // whether a tile may lie in several
   int part_rows;     // rows of a tile in `parts`
   int causal, window, vec;
 };
@@ -63,10 +68,10 @@ __device__ __forceinline__ Extent extent_of(const AttentionArgs& a, int b) {
   return e;
 }
 
-__device__ __forceinline__ int64_t wave_sum(int64_t x) {
+__device__ __forceinline__ uint32_t wave_sum(uint32_t x) {
 #pragma unroll
-  for (int i = 1; i < 64; i *= 2) x += __shfl_xor(x, i, 64);
-  return x;
+  for (int i = 1; i < 64; i *= 2) x += (uint32_t)__shfl_xor((int)x, i, 64);
+  return (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
 }
 __device__ __forceinline__ int wave_prefix(int x) {  // inclusive
 #pragma unroll
@@ -84,44 +89,48 @@ __device__ __forceinline__ int hidden(int x) {
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ int of_lane(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
 
-// Steps of a share, and of all row tiles together; without shares both count tiles.
+// How much a share is, and all row tiles together: in steps with kTileSteps more for each tile, or in tiles that are not cut.
 struct Split {
   uint32_t per, total;
+  bool cut;
 };
+__device__ __forceinline__ uint32_t tile_cost(const Extent& e, bool cut) { return cut ? e.steps + kTileSteps : 1; }
 template <int ROWS>
 __device__ __forceinline__ Split split_of(const AttentionArgs& a, const Extent& first) {  // first: of the first 64 sequences
-  uint64_t total = (uint64_t)first.row_tiles * (a.shares > 0 ? first.steps : 1);
+  uint32_t tiles = first.row_tiles, cost = first.row_tiles * tile_cost(first, true), most = first.row_tiles > 0 ? first.steps : 0;
   for (int b0 = 64; b0 < a.v.batch; b0 += 64) {
     const Extent x = extent_of<ROWS>(a, b0 + lane_id());
-    total += (uint64_t)x.row_tiles * (a.shares > 0 ? x.steps : 1);
+    tiles += x.row_tiles, cost += x.row_tiles * tile_cost(x, true), most = max(most, x.row_tiles > 0 ? (uint32_t)x.steps : 0);
   }
-  total = min((uint64_t)wave_sum((int64_t)total), (uint64_t)0x7FFFFFFF);  // the host sees to it
-  if (a.shares == 0) return {1, (uint32_t)total};
-  const uint32_t share = ((uint32_t)total + a.shares - 1) / a.shares;
-  return {max((share + kMinShare - 1) / kMinShare * kMinShare, (uint32_t)kMinShare), (uint32_t)total};
+  Split split;
+  split.cut = a.cut && __ballot(most > (uint32_t)kUncutSteps) != 0;
+  split.total = wave_sum(split.cut ? cost : tiles);
+  split.per = (split.total + a.shares - 1) / (uint32_t)a.shares;
+  if (split.cut) split.per = max(split.per, (uint32_t)kMinShare);
+  return split;
 }
 
-// Where step `at` of the whole lies: `step` of a row tile whose first one is step `first` of the whole.
+// The row tile that the cost `at` of the whole falls on, where its own begins and how much it is.
 struct Place {
   Extent e;
-  int b, row_tile, step;
-  uint32_t first;
+  int b, row_tile;
+  uint32_t first, cost;
 };
 template <int ROWS>
-__device__ __forceinline__ bool place_of(const AttentionArgs& a, Extent e, uint32_t at, Place* out) {  // e: of the first 64 sequences
+__device__ __forceinline__ bool place_of(const AttentionArgs& a, Extent e, bool cut, uint32_t at, Place* out) {  // e: of the first 64 sequences
   uint32_t before = 0;
   for (int b0 = 0; b0 < a.v.batch; b0 += 64) {
     if (b0 > 0) e = extent_of<ROWS>(a, b0 + lane_id());
-    const uint32_t each = a.shares > 0 ? e.steps : 1, mine = e.row_tiles * each;
+    const uint32_t each = tile_cost(e, cut), mine = e.row_tiles * each;
     const uint32_t end = wave_prefix(mine) + before;
     const unsigned long long past = __ballot(end > at);
     if (past) {
       const int lane = __builtin_ctzll(past);
-      const uint32_t tile_steps = of_lane(each, lane), first = of_lane(end - mine, lane);
+      const uint32_t first = of_lane(end - mine, lane);
       out->b = b0 + lane;
-      out->row_tile = (at - first) / tile_steps;
-      out->first = first + out->row_tile * tile_steps;
-      out->step = at - out->first;
+      out->cost = of_lane(each, lane);
+      out->row_tile = (at - first) / out->cost;
+      out->first = first + out->row_tile * out->cost;
       out->e = {of_lane(e.start, lane), of_lane(e.n, lane), of_lane(e.len, lane), of_lane(e.lo, lane), of_lane(e.row_tiles, lane), of_lane(e.steps, lane)};
       return true;
     }
@@ -236,9 +245,14 @@ __device__ __forceinline__ void nan_of_seen_keys(uint8_t* stage, int lane, int f
   wave_sync();
 }
 
-__device__ __forceinline__ void store_out(const AttentionArgs& a, const Extent& e, int head, int r, int channel, f4 x) {
+// A row tile that lies in several shares.
+struct Pending {
+  int start, row0, rows, first, count;  // start: its sequence's first row; first: the first of the shares
+};
+
+__device__ __forceinline__ void store_out(const AttentionArgs& a, int start, int head, int r, int channel, f4 x) {
   const int token = (int)a.by_group.quotient((uint32_t)r);
-  _Float16* const dst = (_Float16*)a.out + (int64_t)(e.start + token) * a.out_stride + (int64_t)(head * a.group + r - token * a.group) * a.out_head + channel;
+  _Float16* const dst = (_Float16*)a.out + (int64_t)(start + token) * a.out_stride + (int64_t)(head * a.group + r - token * a.group) * a.out_head + channel;
   const h4 y = {(_Float16)x[0], (_Float16)x[1], (_Float16)x[2], (_Float16)x[3]};
   if (a.vec) {
     *(h4*)dst = y;
@@ -247,21 +261,22 @@ __device__ __forceinline__ void store_out(const AttentionArgs& a, const Extent& 
     for (int j = 0; j < 4; j++) dst[j] = y[j];
   }
 }
-__device__ __forceinline__ void store_lse(const AttentionArgs& a, const Extent& e, int head, int r, float top, float sum) {
+__device__ __forceinline__ void store_lse(const AttentionArgs& a, int start, int head, int r, float top, float sum) {
   if (!a.lse) return;
   const int token = (int)a.by_group.quotient((uint32_t)r);
-  a.lse[(int64_t)(e.start + token) * a.lse_stride + head * a.group + r - token * a.group] = sum > 0 || sum != sum ? (top - kLift + __log2f(sum)) * 0.69314718056f : -INFINITY;
+  a.lse[(int64_t)(start + token) * a.lse_stride + head * a.group + r - token * a.group] = sum > 0 || sum != sum ? (top - kLift + __log2f(sum)) * 0.69314718056f : -INFINITY;
 }
 
-// Adds up `count` parts of a row tile, from share `first` on.  D / 4 lanes take a row, four channels each; of the workgroup's groups of
+// Adds up the parts of a row tile.  D / 4 lanes take a row, four channels each; of the workgroup's groups of
 // lanes as many take the rows as there are (a power of two), and the others share the parts of a row; 8 parts are asked for before the
 // first is used.
 template <int D, int THREADS>
-__device__ __forceinline__ void join_parts(const AttentionArgs& a, const Extent& e, __amdgpu_buffer_rsrc_t left, int head, int row0, int rows, int first, int count, float* lds) {
+__device__ __forceinline__ void join_parts(const AttentionArgs& a, const Pending& tile, __amdgpu_buffer_rsrc_t left, int head, float* lds) {
   constexpr int LANES = D / 4, GROUPS = THREADS / LANES, AHEAD = 8;
   f4* const xs = (f4*)lds;             // [group][lane]
   f2* const stats = (f2*)(xs + THREADS);  // [group]
   const int group = threadIdx.x / LANES, c = threadIdx.x % LANES;
+  const int rows = tile.rows, first = tile.first, count = tile.count;
   int takers = 1;  // groups that take rows
   while (takers < rows && takers < GROUPS) takers *= 2;
   const int sharers = GROUPS / takers, mine = group / takers;
@@ -307,8 +322,8 @@ __device__ __forceinline__ void join_parts(const AttentionArgs& a, const Extent&
         sum += stat[1] * by;
         x += xs[(j * takers + group) * LANES + c] * by;
       }
-      store_out(a, e, head, row0 + i, 4 * c, x * (sum > 0 || sum != sum ? 1.0f / sum : 0.0f));
-      if (c == 0) store_lse(a, e, head, row0 + i, top, sum);
+      store_out(a, tile.start, head, tile.row0 + i, 4 * c, x * (sum > 0 || sum != sum ? 1.0f / sum : 0.0f));
+      if (c == 0) store_lse(a, tile.start, head, tile.row0 + i, top, sum);
     }
   }
 }
@@ -327,7 +342,7 @@ __global__ __launch_bounds__(64 * stream_waves(D, QT), stream_groups(D, QT) * st
   constexpr int Q_BYTES = KB * QT * 1024, STAGE = 64 * RUNS, PARTS = kStreamWaves * AT_ONCE * 1024;
   __shared__ __align__(16) uint8_t shared[Q_BYTES + kStreamWaves * STAGE > PARTS ? Q_BYTES + kStreamWaves * STAGE : PARTS];
   __shared__ float tops[kStreamWaves][ROWS], sums[kStreamWaves][ROWS];
-  __shared__ bool all_there;
+  __shared__ bool all_there[2];
   h8* const q_rows = (h8*)shared;
   uint8_t* const stage = shared + Q_BYTES + wave * STAGE;
   f4* const parts = (f4*)shared;
@@ -336,17 +351,24 @@ __global__ __launch_bounds__(64 * stream_waves(D, QT), stream_groups(D, QT) * st
   const Split split = split_of<ROWS>(a, first_64);
   uint32_t now = share * split.per;
   const uint32_t stop = min(now + split.per, split.total);
+  const __amdgpu_buffer_rsrc_t left = __builtin_amdgcn_make_buffer_rsrc((void*)(a.parts + (int64_t)uniform(head) * 2 * a.shares * a.part_rows * (D + 4)), 0,
+                                                                        a.cut ? 2 * a.shares * a.part_rows * (D + 4) * 4 : 0, 0x00020000);  // this head's parts
   Place place;
-  while (now < stop && place_of<ROWS>(a, first_64, now, &place)) {
+  Pending left_first = {}, left_last = {};
+  int pending = 0;
+  while (now < stop && place_of<ROWS>(a, first_64, split.cut, now, &place)) {
     const Extent& e = place.e;
     const int rows = e.n * a.group, row0 = place.row_tile * ROWS;
     // the share's steps of the tile that some row sees, and the keys that every row sees
-    const int steps = (int)min((uint32_t)(e.steps - place.step), stop - now);
-    const bool alone = a.shares == 0 || steps == e.steps;
+    const uint32_t then = min(place.first + place.cost, stop);
+    const int begin_step = split.cut ? max((int)(now - place.first) - kTileSteps, 0) : 0, end_step = split.cut ? (int)(then - place.first) - kTileSteps : e.steps;
+    now = then;
+    if (end_step <= 0) break;  // the tile begins in the next share
+    const bool alone = begin_step == 0 && end_step == e.steps;
     const int last_row = min(row0 + ROWS, rows) - 1;
     const int p_first = e.len - e.n + (int)a.by_group.quotient((uint32_t)row0), p_last = e.len - e.n + (int)a.by_group.quotient((uint32_t)last_row);
-    const int from = uniform(max(e.lo / kStep + place.step, key_begin(a, p_first) / kStep));
-    const int to = uniform(min(e.lo / kStep + (alone ? e.steps : place.step + steps), (key_end(a, e.len, p_last) + kStep - 1) / kStep));
+    const int from = uniform(max(e.lo / kStep + begin_step, key_begin(a, p_first) / kStep));
+    const int to = uniform(min(e.lo / kStep + end_step, (key_end(a, e.len, p_last) + kStep - 1) / kStep));
     const int whole_begin = uniform(key_begin(a, p_last)), whole_end = uniform(key_end(a, e.len, p_first));
     Pages pages;
     pages.look_up(a, place.b, from + wave + kStreamWaves * hidden(lane), to);
@@ -500,9 +522,7 @@ __global__ __launch_bounds__(64 * stream_waves(D, QT), stream_groups(D, QT) * st
       l[t] += __shfl_xor(l[t], 32, 64);
       if (g == 0) tops[wave][16 * t + col] = m[t], sums[wave][16 * t + col] = l[t];
     }
-    const int left_size = uniform(alone ? 0 : 2 * a.shares * a.part_rows * (D + 4) * 4);  // of this head
-    const __amdgpu_buffer_rsrc_t left = __builtin_amdgcn_make_buffer_rsrc((void*)(a.parts + (int64_t)uniform(head) * 2 * a.shares * a.part_rows * (D + 4)), 0, left_size, 0x00020000);
-    const int part = (2 * share + (place.step == 0)) * a.part_rows;
+    const int part = (2 * share + (begin_step == 0)) * a.part_rows;
 #pragma unroll
     for (int t = 0; t < QT; t++) {
       const int r = row0 + 16 * t + col;
@@ -531,38 +551,44 @@ __global__ __launch_bounds__(64 * stream_waves(D, QT), stream_groups(D, QT) * st
           if (r >= rows) continue;
           const int channel = 16 * (d0 + d) + 4 * g;
           if (alone)
-            store_out(a, e, head, r, channel, x * scale);
+            store_out(a, e.start, head, r, channel, x * scale);
           else
             __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4, x), left, ((part + 16 * t + col) * (D + 4) + 4 + channel) * 4, 0, kDeviceScope);
         }
       }
       if (wave == 0 && g == 0 && r < rows) {
         if (alone)
-          store_lse(a, e, head, r, top, sum);
+          store_lse(a, e.start, head, r, top, sum);
         else
           __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u2, f2{top, sum}), left, (part + 16 * t + col) * (D + 4) * 4, 0, kDeviceScope);
       }
     }
     if (!alone) {
-      const uint32_t first = place.first / split.per;
-      const int count = (int)((place.first + e.steps - 1) / split.per - first) + 1;
-      // every wavefront's stores have been acknowledged before the workgroup is counted in, and the parts are asked for after the count
-      // has come back; they go to the level of the memory system that all compute units share
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      __syncthreads();
-      if (threadIdx.x == 0) {
-        uint32_t* const counter = a.counts + head * a.shares + first;
-        const bool last = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)count - 1;
-        if (last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        all_there = last;
-      }
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      __syncthreads();
-      if (all_there) join_parts<D, 64 * kStreamWaves>(a, e, left, head, row0, min(rows - row0, ROWS), (int)first, count, (float*)shared);
+      const int first = (int)((place.first + kTileSteps) / split.per), last = (int)((place.first + kTileSteps + e.steps - 1) / split.per);
+      left_first = pending == 0 ? Pending{e.start, row0, min(rows - row0, ROWS), first, last - first + 1} : left_first;
+      left_last = Pending{e.start, row0, min(rows - row0, ROWS), first, last - first + 1};
+      pending++;
     }
-    now += a.shares > 0 ? steps : 1;
     __syncthreads();  // what the tile left in LDS has been read
   }
+  // Only the first and the last tile of a share may lie in others too.  Every wavefront's stores have been acknowledged before the
+  // workgroup is counted in, and the parts are asked for after the count has come back; they go to the level of the memory system that
+  // all compute units share.
+  if (pending == 0) return;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (threadIdx.x < (unsigned)pending) {
+    const Pending mine = threadIdx.x == 0 ? left_first : left_last;
+    uint32_t* const counter = a.counts + head * a.shares + mine.first;
+    const bool last = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)mine.count - 1;
+    if (last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    all_there[threadIdx.x] = last;
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+#pragma unroll 1
+  for (int i = 0; i < pending; i++)
+    if (all_there[i]) join_parts<D, 64 * kStreamWaves>(a, i == 0 ? left_first : left_last, left, head, (float*)shared);
 }
 
 // ---- launch ------------------------------------------------------------------------------------------
@@ -574,6 +600,7 @@ struct Plan {
   int qt, rows, part_rows;
   int64_t row_tiles;  // at most so many over all sequences
   int64_t shares;
+  bool cut;
   size_t workspace;   // bytes that this many shares need
 };
 Plan make_plan(const ams_kv_cache* c, int64_t rows, int heads, int64_t max_q_len, size_t workspace) {
@@ -586,11 +613,12 @@ Plan make_plan(const ams_kv_cache* c, int64_t rows, int heads, int64_t max_q_len
   const int64_t tile_steps = std::max<int64_t>(((int64_t)c->table_width * c->page_size + kStep - 1) / kStep, 1);
   p.part_rows = (int)std::min<int64_t>(c->q_starts ? rows * R : R, p.rows);
   const size_t part = (size_t)c->kv_heads * p.part_rows * (c->head_dim + 4) * sizeof(float);
-  p.shares = std::max<int64_t>(stream_groups(c->head_dim, p.qt) * kComputeUnits / c->kv_heads, 1);
-  if (tile_steps <= kMinShare || p.row_tiles * tile_steps > 0x7FFFFFFF) p.shares = 0;
   const size_t room = std::min<size_t>(workspace, AMS_KV_WORKSPACE_BYTES);
-  p.shares = std::min<int64_t>(p.shares, room < kCountBytes ? 0 : (int64_t)((room - kCountBytes) / part / 2));
-  p.workspace = p.shares > 0 ? kCountBytes + 2 * (size_t)p.shares * part : 0;
+  const int64_t fit = std::max<int64_t>(stream_groups(c->head_dim, p.qt) * kComputeUnits / c->kv_heads, 1);
+  p.shares = std::min(std::min(fit, p.row_tiles * kMaxParts), room < kCountBytes ? 0 : (int64_t)((room - kCountBytes) / part / 2));
+  p.cut = p.shares > 1 && tile_steps > kUncutSteps && p.row_tiles * (tile_steps + kTileSteps) <= 0x7FFFFFFF;
+  p.workspace = p.cut ? kCountBytes + 2 * (size_t)p.shares * part : 0;
+  if (!p.cut) p.shares = p.row_tiles;
   return p;
 }
 
@@ -627,8 +655,8 @@ int ams_kv_attention(const ams_kv_cache* cache, const uint16_t* Q, uint16_t* O, 
   a.causal = causal != 0, a.window = (int)std::min<int64_t>(window, 0x3FFFFFFF);
   a.vec = aligned(Q, 16) && aligned(O, 8) && (q_stride | q_head_stride) % 8 == 0 && (o_stride | o_head_stride) % 4 == 0;
   const Plan p = make_plan(cache, rows, heads, max_q_len, workspace ? workspace_bytes : 0);
-  a.shares = (int)p.shares, a.part_rows = p.part_rows;
-  const int64_t grid = (p.shares > 0 ? p.shares : p.row_tiles) * cache->kv_heads;
+  a.shares = (int)p.shares, a.cut = p.cut, a.part_rows = p.part_rows;
+  const int64_t grid = p.shares * cache->kv_heads;
   if (grid > 0x7FFFFFFF) return AMS_ERR_SHAPE;
   dispatch(cache->head_dim, cache->scale_group, [&](auto d, auto g) {
     constexpr int D = decltype(d)::value, G = decltype(g)::value;
