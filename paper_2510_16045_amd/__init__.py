@@ -212,9 +212,19 @@ def _first_call(*args):
 _call = _first_call
 
 
+def _first_kv_call(*args):
+    """The same for the calls of the KV cache: (entry, cache, block_table, kv_lens, scale_group, q_starts, ...)."""
+    _bind_call()
+    return _kv_call(*args)
+
+
+_kv_call = _first_kv_call
+_KV_WRITE, _KV_READ, _KV_ATTENTION = range(3)  # of csrc/ams_binding.cpp
+
+
 def _bind_call():
-    global _call
-    _call = lambda *args: None  # the long way
+    global _call, _kv_call
+    _call = _kv_call = lambda *args: None  # the long way
     try:
         import torch  # its libraries first
     except ImportError:
@@ -232,7 +242,8 @@ def _bind_call():
         return
     lib = load_library()
     _binding.bind(*(ctypes.cast(f, _vp).value for f in (lib.ams_packed_bytes, lib.ams_group_scales_count, lib.ams_linear, lib.ams_linear_ws, lib.ams_linear_static_ws, lib.ams_linear_grouped)))
-    _call = _binding.linear
+    _binding.bind_kv(*(ctypes.cast(f, _vp).value for f in (lib.ams_kv_block_bytes, lib.ams_kv_write, lib.ams_kv_read, lib.ams_kv_attention)))
+    _call, _kv_call = _binding.linear, _binding.kv
 
 
 _PLAIN, _WORKSPACE, _STATIC, _GROUPED = range(4)  # of csrc/ams_binding.cpp
@@ -544,6 +555,8 @@ def ams_kv_write(cache, k, v, block_table, kv_lens, scale_group: int = 32, q_sta
 
     Sequence b has kv_lens[b] tokens, the new ones among them, in the pages block_table[b] (int32 [batch, pages]); its rows of k and v
     are q_starts[b] .. q_starts[b + 1] - 1 (int32 [batch + 1]; None: one row per sequence).  Returns the cache."""
+    if _kv_call(_KV_WRITE, cache, block_table, kv_lens, scale_group, q_starts, k, v):
+        return cache
     view = _kv_view(cache, block_table, kv_lens, q_starts, k.shape[-1], scale_group)
     kp, vp = _kv_rows(k, "k", cache.shape[1], k.shape[-1]), _kv_rows(v, "v", cache.shape[1], k.shape[-1])
     if v.shape[0] != k.shape[0]:
@@ -558,6 +571,8 @@ def ams_kv_read(cache, block_table, kv_lens, scale_group: int = 32, head_dim: in
 
     Rows as in ams_kv_write: with q_starts = the cumulated kv_lens whole sequences are read.  `rows` is q_starts[-1] (one per
     sequence without q_starts); with out=(k, v) it is theirs."""
+    if out is not None and rows is None and _kv_call(_KV_READ, cache, block_table, kv_lens, scale_group, q_starts, head_dim, *out):
+        return out
     import torch
 
     if out is None and rows is None and q_starts is not None:
@@ -592,6 +607,8 @@ def ams_kv_attention(q, cache, block_table, kv_lens, scale_group: int = 32, q_st
     workspace: a uint8 CUDA tensor, zero-filled once, that calls may share one after the other; without one a row's keys are not shared out
     to several workgroups.
     lse: fp32 [rows, heads], receives log(sum(exp(scores)))."""
+    if out is not None and _kv_call(_KV_ATTENTION, cache, block_table, kv_lens, scale_group, q_starts, q, out, max_q_len, softmax_scale, causal, window, workspace, lse):
+        return out
     import torch
 
     if q.dim() != 3:
