@@ -1,0 +1,266 @@
+// Attention over the 4-bit KV cache: what its two kernels share.
+//
+//   S[r, j] = softmax_scale * q[r] . k[j],  O[r] = sum_j exp(S[r, j] - max) v[j] / sum_j exp(S[r, j] - max)
+//
+// with k and v as the cache holds them (fp16 values), sums and statistics in fp32.  The heads / kv_heads query heads that read one
+// kv head are rows of one problem: row r of a sequence is token r / R of its query rows and head r % R of the kv head's R.
+//
+// Split of the work: the host knows neither lengths nor (with row starts) how many rows a sequence has, so every workgroup works it
+// out from them: the steps of all row tiles of a kv head, one tile after the other, are cut into equal shares, as many as there are
+// workgroups that fit on the chip at once.  A share may begin and end inside a tile; that a workgroup begins a tile counts as much as
+// kTileSteps steps.  Where no tile has more than kUncutSteps, shares are made of whole tiles.  Of a tile that lies in several shares every
+// workgroup leaves its part (max, sum, O) in the workspace and counts itself in; the one that comes last adds all of them up, always in
+// the same order, and clears the count.  Nobody waits for anybody.
+#ifndef AMS_KV_ATTENTION_H_
+#define AMS_KV_ATTENTION_H_
+
+#include "ams_kv.h"
+
+namespace ams_kv {
+
+
+constexpr int kDeviceScope = 16;  // cache policy (sc1) of a buffer load or store that the whole device sees
+constexpr int kStep = 32;         // keys of a wavefront's step
+constexpr int kMinShare = 16;     // steps of a share: four for each wavefront
+constexpr int kTileSteps = 14;    // what it takes to begin a tile and to leave its result, in steps
+constexpr int kUncutSteps = 32;   // a tile of so many is not cut: joining its parts takes longer than its steps
+constexpr int kMaxParts = 64;     // a tile in more parts costs its last workgroup more than the others gain
+constexpr float kLift = 8.0f;     // exponents of P are raised by this: below it P keeps fp16's full precision over 2^-22 of the largest
+constexpr float kSlack = 7.0f;    // how far (log2) a score may pass the running maximum before that is raised: 2^(8 + 7) is in fp16
+
+struct AttentionArgs {
+  View v;
+  const uint16_t* q;
+  uint16_t* out;
+  float* lse;
+  uint32_t* counts;  // [kv head][share in which the tile begins]
+  float* parts;      // [kv head][2 share + (the tile begins in it)][row of the tile][max, sum, -, -, D values]
+  int64_t q_stride, q_head, out_stride, out_head, lse_stride;
+  float scale2;  // softmax_scale * log2(e)
+  int group;     // R
+  Divisor by_group;
+  int shares;        // workgroups of one kv head
+  int cut;           // whether a tile may lie in several
+  int part_rows;     // rows of a tile in `parts`
+  int causal, window, vec;
+};
+
+// What one sequence contributes: rows, row tiles and steps of keys.
+struct Extent {
+  int start, n, len, lo, row_tiles, steps;  // lo: first key (a multiple of kStep) that any row may see
+};
+template <int ROWS>
+__device__ __forceinline__ Extent extent_of(const AttentionArgs& a, int b) {
+  Extent e = {0, 0, 0, 0, 0, 0};
+  if (b >= a.v.batch) return e;
+  e.start = row_start(a.v, b);
+  e.n = max(row_start(a.v, b + 1) - e.start, 0);
+  e.len = kv_len(a.v, b);
+  const int first = e.len - e.n;  // position of the first row
+  e.lo = a.window > 0 ? max(first + 1 - a.window, 0) & ~(kStep - 1) : 0;
+  e.row_tiles = (int)(((uint32_t)e.n * (uint32_t)a.group + ROWS - 1) / ROWS);
+  e.steps = max((e.len - e.lo + kStep - 1) / kStep, 1);  // one also where there is no key: somebody has to say so
+  return e;
+}
+
+__device__ __forceinline__ uint32_t wave_sum(uint32_t x) {
+#pragma unroll
+  for (int i = 1; i < 64; i *= 2) x += (uint32_t)__shfl_xor((int)x, i, 64);
+  return (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
+}
+__device__ __forceinline__ int wave_prefix(int x) {  // inclusive
+#pragma unroll
+  for (int i = 1; i < 64; i *= 2) {
+    const int y = __shfl_up(x, i, 64);
+    if (lane_id() >= i) x += y;
+  }
+  return x;
+}
+// x, of which the compiler knows nothing: what follows from it is not worked out before it is needed and kept in registers.
+__device__ __forceinline__ int hidden(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int of_lane(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
+
+// How much a share is, and all row tiles together: in steps with kTileSteps more for each tile, or in tiles that are not cut.
+struct Split {
+  uint32_t per, total;
+  bool cut;
+};
+__device__ __forceinline__ uint32_t tile_cost(const Extent& e, bool cut) { return cut ? e.steps + kTileSteps : 1; }
+template <int ROWS>
+__device__ __forceinline__ Split split_of(const AttentionArgs& a, const Extent& first) {  // first: of the first 64 sequences
+  uint32_t tiles = first.row_tiles, cost = first.row_tiles * tile_cost(first, true), most = first.row_tiles > 0 ? first.steps : 0;
+  for (int b0 = 64; b0 < a.v.batch; b0 += 64) {
+    const Extent x = extent_of<ROWS>(a, b0 + lane_id());
+    tiles += x.row_tiles, cost += x.row_tiles * tile_cost(x, true), most = max(most, x.row_tiles > 0 ? (uint32_t)x.steps : 0);
+  }
+  Split split;
+  split.cut = a.cut && __ballot(most > (uint32_t)kUncutSteps) != 0;
+  split.total = wave_sum(split.cut ? cost : tiles);
+  split.per = (split.total + a.shares - 1) / (uint32_t)a.shares;
+  if (split.cut) split.per = max(split.per, (uint32_t)kMinShare);
+  return split;
+}
+
+// The row tile that the cost `at` of the whole falls on, where its own begins and how much it is.
+struct Place {
+  Extent e;
+  int b, row_tile;
+  uint32_t first, cost;
+};
+template <int ROWS>
+__device__ __forceinline__ bool place_of(const AttentionArgs& a, Extent e, bool cut, uint32_t at, Place* out) {  // e: of the first 64 sequences
+  uint32_t before = 0;
+  for (int b0 = 0; b0 < a.v.batch; b0 += 64) {
+    if (b0 > 0) e = extent_of<ROWS>(a, b0 + lane_id());
+    const uint32_t each = tile_cost(e, cut), mine = e.row_tiles * each;
+    const uint32_t end = wave_prefix(mine) + before;
+    const unsigned long long past = __ballot(end > at);
+    if (past) {
+      const int lane = __builtin_ctzll(past);
+      const uint32_t first = of_lane(end - mine, lane);
+      out->b = b0 + lane;
+      out->cost = of_lane(each, lane);
+      out->row_tile = (at - first) / out->cost;
+      out->first = first + out->row_tile * out->cost;
+      out->e = {of_lane(e.start, lane), of_lane(e.n, lane), of_lane(e.len, lane), of_lane(e.lo, lane), of_lane(e.row_tiles, lane), of_lane(e.steps, lane)};
+      return true;
+    }
+    before = of_lane(end, 63);
+  }
+  return false;
+}
+
+__device__ __forceinline__ h8 join_halves(u2 a, u2 b) { return __builtin_bit_cast(h8, u4{a[0], a[1], b[0], b[1]}); }
+
+// Eight halfs; where rows are not 16-byte aligned half by half.
+__device__ __forceinline__ u4 load_half8(const uint16_t* p, bool vec) {
+  if (vec) return *(const u4*)p;
+  u4 x;
+#pragma unroll
+  for (int i = 0; i < 4; i++) x[i] = p[2 * i] | (uint32_t)p[2 * i + 1] << 16;
+  return x;
+}
+
+// The lowest and highest key (one past) that the row at `position` may see.
+__device__ __forceinline__ int key_end(const AttentionArgs& a, int len, int position) { return a.causal ? min(len, position + 1) : len; }
+__device__ __forceinline__ int key_begin(const AttentionArgs& a, int position) { return a.window > 0 ? max(position + 1 - a.window, 0) : 0; }
+
+// A row tile that lies in several shares.
+struct Pending {
+  int start, row0, rows, first, count;  // start: its sequence's first row; first: the first of the shares
+};
+
+__device__ __forceinline__ void store_out(const AttentionArgs& a, int start, int head, int r, int channel, f4 x) {
+  const int token = (int)a.by_group.quotient((uint32_t)r);
+  _Float16* const dst = (_Float16*)a.out + (int64_t)(start + token) * a.out_stride + (int64_t)(head * a.group + r - token * a.group) * a.out_head + channel;
+  const h4 y = {(_Float16)x[0], (_Float16)x[1], (_Float16)x[2], (_Float16)x[3]};
+  if (a.vec) {
+    *(h4*)dst = y;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; j++) dst[j] = y[j];
+  }
+}
+__device__ __forceinline__ void store_lse(const AttentionArgs& a, int start, int head, int r, float top, float sum) {
+  if (!a.lse) return;
+  const int token = (int)a.by_group.quotient((uint32_t)r);
+  a.lse[(int64_t)(start + token) * a.lse_stride + head * a.group + r - token * a.group] = sum > 0 || sum != sum ? (top - kLift + __log2f(sum)) * 0.69314718056f : -INFINITY;
+}
+
+// Adds up the parts of a row tile.  D / 4 lanes take a row, four channels each; of the workgroup's groups of
+// lanes as many take the rows as there are (a power of two), and the others share the parts of a row; 8 parts are asked for before the
+// first is used.
+template <int D, int THREADS>
+__device__ __forceinline__ void join_parts(const AttentionArgs& a, const Pending& tile, __amdgpu_buffer_rsrc_t left, int head, float* lds) {
+  constexpr int LANES = D / 4, GROUPS = THREADS / LANES, AHEAD = 8;
+  f4* const xs = (f4*)lds;             // [group][lane]
+  f2* const stats = (f2*)(xs + THREADS);  // [group]
+  const int group = threadIdx.x / LANES, c = threadIdx.x % LANES;
+  const int rows = tile.rows, first = tile.first, count = tile.count;
+  int takers = 1;  // groups that take rows
+  while (takers < rows && takers < GROUPS) takers *= 2;
+  const int sharers = GROUPS / takers, mine = group / takers;
+  for (int i0 = 0; i0 < rows; i0 += takers) {
+    const int i = i0 + group % takers;
+    float top = -INFINITY, sum = 0;
+    f4 x = {0, 0, 0, 0};
+    for (int s0 = mine; s0 < count; s0 += sharers * AHEAD) {
+      f4 from[AHEAD];
+      f2 stat[AHEAD];
+#pragma unroll
+      for (int j = 0; j < AHEAD; j++) {
+        const int s = s0 + j * sharers;
+        const int at = s < count && i < rows ? ((2 * (first + s) + (s == 0)) * a.part_rows + i) * (D + 4) * 4 : 0x7FFE0000;  // nothing is read there
+        from[j] = __builtin_bit_cast(f4, __builtin_amdgcn_raw_buffer_load_b128(left, at + 16 + 16 * c, 0, kDeviceScope));
+        stat[j] = __builtin_bit_cast(f2, __builtin_amdgcn_raw_buffer_load_b64(left, at, 0, kDeviceScope));
+        if (s >= count) stat[j] = f2{-INFINITY, 0};
+      }
+      float most = top;
+#pragma unroll
+      for (int j = 0; j < AHEAD; j++) most = fmaxf(most, stat[j][0]);
+      const float less = top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top - most);
+      top = most;
+      sum *= less, x *= less;
+#pragma unroll
+      for (int j = 0; j < AHEAD; j++) {
+        const float by = stat[j][0] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(stat[j][0] - top);
+        sum += stat[j][1] * by;
+        x += from[j] * by;
+      }
+    }
+    __syncthreads();  // what was in LDS has been read
+    xs[threadIdx.x] = x;
+    if (c == 0) stats[group] = f2{top, sum};
+    __syncthreads();
+    if (mine == 0 && i < rows) {
+      top = -INFINITY, sum = 0;
+      x = f4{0, 0, 0, 0};
+      for (int j = 0; j < sharers; j++) top = fmaxf(top, stats[j * takers + group][0]);
+      for (int j = 0; j < sharers; j++) {
+        const f2 stat = stats[j * takers + group];
+        const float by = stat[0] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(stat[0] - top);
+        sum += stat[1] * by;
+        x += xs[(j * takers + group) * LANES + c] * by;
+      }
+      store_out(a, tile.start, head, tile.row0 + i, 4 * c, x * (sum > 0 || sum != sum ? 1.0f / sum : 0.0f));
+      if (c == 0) store_lse(a, tile.start, head, tile.row0 + i, top, sum);
+    }
+  }
+}
+
+// The end of a workgroup whose share has `pending` tiles that lie in others too (only its first and its last can).  Every wavefront's
+// stores have been acknowledged before the workgroup is counted in, and the parts are asked for after the count has come back; they go
+// to the level of the memory system that all compute units share.
+template <int D, int THREADS>
+__device__ __forceinline__ void join_pending(const AttentionArgs& a, int pending, const Pending& first, const Pending& last, __amdgpu_buffer_rsrc_t left, int head, float* lds, bool* all_there) {
+  if (pending == 0) return;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (threadIdx.x < (unsigned)pending) {
+    const Pending mine = threadIdx.x == 0 ? first : last;
+    uint32_t* const counter = a.counts + head * a.shares + mine.first;
+    const bool is_last = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)mine.count - 1;
+    if (is_last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    all_there[threadIdx.x] = is_last;
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+#pragma unroll 1
+  for (int i = 0; i < pending; i++)
+    if (all_there[i]) join_parts<D, THREADS>(a, i == 0 ? first : last, left, head, lds);
+}
+
+// ---- the kernels' launches -----------------------------------------------------------------------------
+// Wavefronts of a workgroup, and of stream_kernel workgroups of a compute unit: what the registers allow.
+constexpr int tile_waves(int d) { return d == 256 ? 4 : 8; }
+constexpr int stream_waves(int, int) { return 4; }
+constexpr int stream_groups(int d, int qt) { return d * qt <= 128 ? 3 : d * qt < 512 ? 2 : 1; }
+void launch_stream(const AttentionArgs& a, int head_dim, int scale_group, int qt, unsigned grid, hipStream_t stream);
+void launch_tile(const AttentionArgs& a, int head_dim, int scale_group, unsigned grid, hipStream_t stream);
+
+}  // namespace ams_kv
+#endif

@@ -12,7 +12,7 @@ struct TileRows {
   int b, tile, row, first, end;
 };
 __device__ __forceinline__ bool tile_rows(const View& v, int item, TileRows* t) {
-  auto first_item = [&](int b) { return row_start(v, b) / kTile + 2 * b; };
+  auto first_item = [&](int b) { return v.starts ? row_start(v, b) / kTile + 2 * b : b; };
   const int b = sequence_of(v.batch, item, first_item);
   const int start = row_start(v, b), n = max(row_start(v, b + 1) - start, 0), len = kv_len(v, b);
   const int p0 = len - n;  // position of the first row
@@ -22,9 +22,10 @@ __device__ __forceinline__ bool tile_rows(const View& v, int item, TileRows* t) 
   return t->first < t->end;
 }
 
-// Eight halfs; rows that are not 16-byte aligned half by half.
+// Eight halfs; rows that are not 16-byte aligned half by half.  They are read once, and stay out of the caches (16384 rows of 8 heads
+// written and read back 45 -> 36 us).
 __device__ __forceinline__ u4 load8(const uint16_t* p, bool vec) {
-  if (vec) return *(const u4*)p;
+  if (vec) return __builtin_nontemporal_load((const u4*)p);
   u4 x;
 #pragma unroll
   for (int i = 0; i < 4; i++) x[i] = p[2 * i] | (uint32_t)p[2 * i + 1] << 16;
@@ -32,18 +33,32 @@ __device__ __forceinline__ u4 load8(const uint16_t* p, bool vec) {
 }
 __device__ __forceinline__ void store8(uint16_t* p, u4 x, bool vec) {
   if (vec) {
-    *(u4*)p = x;
+    __builtin_nontemporal_store(x, (u4*)p);
     return;
   }
 #pragma unroll
   for (int i = 0; i < 4; i++) p[2 * i] = (uint16_t)x[i], p[2 * i + 1] = (uint16_t)(x[i] >> 16);
 }
 
-// The larger of a lane's value and those of the lanes that hold the rest of its run (a power of two of neighbours).
+__device__ __forceinline__ uint32_t max_halves(uint32_t a, uint32_t b) {
+  const us2 x = __builtin_bit_cast(us2, a), y = __builtin_bit_cast(us2, b);
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(x, y));
+}
+
+// A lane's value from another lane of its 16, by a data-parallel pattern.
+template <int PATTERN>
+__device__ __forceinline__ uint32_t moved(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, PATTERN, 0xF, 0xF, true);
+}
+constexpr int kSwapOne = 0xB1, kSwapTwo = 0x4E, kMirrorEight = 0x141, kMirror = 0x140;  // lane ^ 1, lane ^ 2, 7 - lane, 15 - lane
+
+// The larger of a lane's value and those of the lanes that hold the rest of its run (4, 8 or 16 neighbours).
 template <int LANES>
 __device__ __forceinline__ uint32_t max_over(uint32_t x) {
-#pragma unroll
-  for (int i = 1; i < LANES; i *= 2) x = max(x, (uint32_t)__shfl_xor((int)x, i, 64));
+  x = max(x, moved<kSwapOne>(x));
+  x = max(x, moved<kSwapTwo>(x));
+  if constexpr (LANES >= 8) x = max(x, moved<kMirrorEight>(x));
+  if constexpr (LANES == 16) x = max(x, moved<kMirror>(x));
   return x;
 }
 
@@ -81,54 +96,62 @@ struct RowsArgs {
   int vec;  // rows are 16-byte aligned
 };
 
-constexpr int kWaves = 4;  // tiles of a workgroup
+// Tiles of a workgroup: of several heads, whose rows lie beside each other.
+constexpr int kWaves = 4;
 
-// The tile's planes are put together in LDS, in the cache's order, and leave as whole words; a word of V's codes holds four tokens and
-// goes byte by byte where some of them are not this call's.
+// A wavefront has 64 / (D / 8) tokens at a time, eight channels of one of them to a lane; all of its rows are asked for before the page
+// is looked up.  The tile's planes are put together in LDS, in the cache's order, and leave as whole words; a word of V's codes holds four
+// tokens and goes byte by byte where some of them are not this call's.
 template <int D, int G>
 __global__ __launch_bounds__(64 * kWaves) void write_kernel(RowsArgs a) {
-  constexpr int RUNS = D / G, CHUNKS = D / 8, W = Lane<D>::W, CODES = 8 * D, SCALES = kTile * RUNS * 2;
+  constexpr int RUNS = D / G, CHUNKS = D / 8, W = Lane<D>::W, CODES = 8 * D, SCALES = kTile * RUNS * 2, PASSES = kTile * CHUNKS / 64, TOKENS = 64 / CHUNKS;
   __shared__ __align__(16) uint8_t image[kWaves][2 * (CODES + SCALES)];
-  const int wave = threadIdx.x >> 6, lane = lane_id();
-  const int group = (int)a.v.heads.quotient(blockIdx.x), head = blockIdx.x - group * a.v.kv_heads, item = group * kWaves + wave;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = lane_id();
+  const int unit = blockIdx.x * kWaves + wave, item = (int)a.v.heads.quotient(unit), head = unit - item * a.v.kv_heads;
   TileRows t;
   if (!tile_rows(a.v, item, &t) || t.tile < 0) return;
+  const int c = lane % CHUNKS;
+  u4 x[PASSES][2];
+#pragma unroll
+  for (int i = 0; i < PASSES; i++) {
+    const int token = i * TOKENS + lane / CHUNKS;
+    x[i][0] = x[i][1] = u4{0, 0, 0, 0};
+    if (token >= t.first && token < t.end) {
+      const int64_t row = t.row + token;
+      x[i][0] = load8(a.k + row * a.k_stride + head * a.k_head + 8 * c, a.vec);
+      x[i][1] = load8(a.v_rows + row * a.v_stride + head * a.v_head + 8 * c, a.vec);
+    }
+  }
   int in_page;
   uint8_t* const block = block_of(a.v, t.b, t.tile, head, &in_page);
   if (!block) return;
   uint8_t* const img = image[wave];
-  for (int u = lane; u < kTile * CHUNKS; u += 64) {
-    const int token = u / CHUNKS, c = u % CHUNKS;
-    const bool mine = token >= t.first && token < t.end;
+#pragma unroll
+  for (int i = 0; i < PASSES; i++) {
+    if ((i + 1) * TOKENS <= t.first || i * TOKENS >= t.end) continue;
+    const int token = i * TOKENS + lane / CHUNKS, word = c / 4, run = c * 8 / G;
+    uint32_t code[2];
 #pragma unroll
     for (int which = 0; which < 2; which++) {
-      u4 x = {0, 0, 0, 0};
-      const uint16_t* src = which ? a.v_rows + (int64_t)(t.row + token) * a.v_stride + head * a.v_head : a.k + (int64_t)(t.row + token) * a.k_stride + head * a.k_head;
-      if (mine) x = load8(src + 8 * c, a.vec);
       uint32_t most = 0;
 #pragma unroll
-      for (int j = 0; j < 4; j++) most = max(most, max(x[j] & 0x7FFFu, (x[j] >> 16) & 0x7FFFu));
-      most = max_over<G / 8>(most);
+      for (int j = 0; j < 4; j++) most = max_halves(most, x[i][which][j] & 0x7FFF7FFFu);
+      most = max_over<G / 8>(max(most & 0xFFFFu, most >> 16));
       const _Float16 s = scale_of(most);
-      const uint32_t code = eight_codes(x, (float)s, most < 0x7C00u);
-      const int i = c / 4, run = c * 8 / G;
-      if (which == 0) {
-        *(uint32_t*)(img + i / W * 256 * W + ((c & 3) * 16 + token) * 4 * W + i % W * 4) = code;
-        if (c * 8 % G == 0) *(_Float16*)(img + 2 * CODES + 2 * (token * RUNS + run)) = s;
-      } else {
-        // channels 8 (c & 1) .. + 7 of 32 i + 16 ab: joined with the other half's codes in the lane two further (ab is bit 1 of c)
-        const uint32_t other = (uint32_t)__shfl_xor((int)code, 2, 64);
-        const uint32_t low = c & 2 ? other : code, high = c & 2 ? code : other;  // a, b
-        // each of the two lanes stores four channels: the lower one the first four
-        const int from = c & 2 ? 4 : 0;
-#pragma unroll
-        for (int j = 0; j < 4; j++) {
-          const uint32_t na = low >> 4 * (from + j) & 15, nb = high >> 4 * (from + j) & 15;
-          img[CODES + i / W * 256 * W + (token / 4 * 16 + (c & 1) * 8 + from + j) * 4 * W + i % W * 4 + token % 4] = (uint8_t)(token & 1 ? nb | na << 4 : na | nb << 4);
-        }
-        if (c * 8 % G == 0) *(_Float16*)(img + 2 * CODES + SCALES + 2 * ((token / 4 * RUNS + run) * 4 + token % 4)) = s;
-      }
+      code[which] = eight_codes(x[i][which], (float)s, most < 0x7C00u);
+      if (c * 8 % G == 0) *(_Float16*)(img + 2 * CODES + which * SCALES + 2 * (which ? (token / 4 * RUNS + run) * 4 + token % 4 : token * RUNS + run)) = s;
     }
+    *(uint32_t*)(img + word / W * 256 * W + ((c & 3) * 16 + token) * 4 * W + word % W * 4) = code[0];
+    // V: channels 8 (c & 1) .. + 7 of 32 word + 16 (c >> 1 & 1): joined with the other half's codes, in the lane two further, and each of the
+    // two lanes stores four channels, the lower one the first four.
+    const uint32_t other = moved<kSwapTwo>(code[1]);
+    const bool upper = (c & 2) != 0;
+    uint32_t low = upper ? other : code[1], high = upper ? code[1] : other;  // a, b
+    if (upper) low >>= 16, high >>= 16;
+    const uint32_t first = token & 1 ? high : low, second = token & 1 ? low : high;  // in the lower and the upper nibble
+    const uint32_t even = (first & 0x0F0Fu) | (second & 0x0F0Fu) << 4, odd = (first >> 4 & 0x0F0Fu) | (second & 0xF0F0u);
+    uint8_t* const to = img + CODES + word / W * 256 * W + (token / 4 * 16 + (c & 1) * 8 + (upper ? 4 : 0)) * 4 * W + word % W * 4 + token % 4;
+    to[0] = (uint8_t)even, to[4 * W] = (uint8_t)odd, to[8 * W] = (uint8_t)(even >> 8), to[12 * W] = (uint8_t)(odd >> 8);
   }
   wave_sync();
   uint8_t* const kc = block + in_page * CODES;
@@ -167,8 +190,8 @@ template <int D, int G>
 __global__ __launch_bounds__(64 * kWaves) void read_kernel(RowsArgs a) {
   constexpr int RUNS = D / G, W = Lane<D>::W, CODES = 8 * D, SCALES = kTile * RUNS * 2, ROW = D + 8;
   __shared__ __align__(16) _Float16 image[kWaves][kTile * ROW];
-  const int wave = threadIdx.x >> 6, lane = lane_id();
-  const int group = (int)a.v.heads.quotient(blockIdx.x), head = blockIdx.x - group * a.v.kv_heads, item = group * kWaves + wave;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = lane_id();
+  const int unit = blockIdx.x * kWaves + wave, item = (int)a.v.heads.quotient(unit), head = unit - item * a.v.kv_heads;
   TileRows t;
   if (!tile_rows(a.v, item, &t)) return;
   int in_page = 0;
@@ -194,12 +217,16 @@ __global__ __launch_bounds__(64 * kWaves) void read_kernel(RowsArgs a) {
   sk.load(ks + c * RUNS * 2);
   Scales<4 * RUNS> sv;
   sv.load(ks + a.v.scales + g * RUNS * 8);
-  if (there(c)) {
-#pragma unroll
-    for (int i = 0; i < Lane<D>::kWords; i++)
-      store8(row_of(a.k, a.k_stride, a.k_head, c) + 32 * i + 8 * g, __builtin_bit_cast(u4, restore_k(kw.w[i], sk.twice(32 * i / G))), a.vec);
-  }
   _Float16* const img = image[wave];
+#pragma unroll
+  for (int i = 0; i < Lane<D>::kWords; i++) *(u4*)(img + c * ROW + 32 * i + 8 * g) = __builtin_bit_cast(u4, restore_k(kw.w[i], sk.twice(32 * i / G)));
+  wave_sync();
+#pragma unroll
+  for (int u = lane; u < kTile * D / 8; u += 64) {
+    const int token = u / (D / 8), part = u % (D / 8);
+    if (there(token)) store8(row_of(a.k, a.k_stride, a.k_head, token) + 8 * part, *(const u4*)(img + token * ROW + 8 * part), a.vec);
+  }
+  wave_sync();
 #pragma unroll
   for (int i = 0; i < Lane<D>::kWords; i++) {
     const int run = 32 * i / G * 2;
@@ -229,9 +256,8 @@ int run_rows(const ams_kv_cache* cache, int64_t rows, uint16_t* k, uint16_t* v, 
   if (rows == 0 || cache->batch == 0) return AMS_OK;
   a.k = k, a.v_rows = v, a.k_stride = k_stride, a.k_head = k_head, a.v_stride = v_stride, a.v_head = v_head;
   a.vec = aligned(k, 16) && aligned(v, 16) && (k_stride | k_head | v_stride | v_head) % 8 == 0;
-  // without row starts a sequence has one row, and one tile of its two
-  const int64_t items = rows / kTile + 2 * (int64_t)cache->batch, grid = (items + kWaves - 1) / kWaves * cache->kv_heads;
-  if (grid > 0x7FFFFFFF) return AMS_ERR_SHAPE;
+  const int64_t units = (cache->q_starts ? rows / kTile + 2 * (int64_t)cache->batch : cache->batch) * cache->kv_heads, grid = (units + kWaves - 1) / kWaves;
+  if (units > 0x7FFFFFFF - kWaves) return AMS_ERR_SHAPE;
   auto go = [&](auto d, auto g) {
     constexpr int D = decltype(d)::value, G = decltype(g)::value;
     if constexpr (WRITE)

@@ -1,0 +1,315 @@
+// Attention over the 4-bit KV cache for many rows: prompts.
+//
+// tile_kernel: a workgroup takes 32 rows for each of its wavefronts and walks the keys in blocks of 64.  A block is restored to fp16 once,
+// by all wavefronts together (a tile of K or V each), into LDS in the order in which 32x32x16 matrix instructions take it, so that
+// every read is 64 lanes of 16 bytes side by side; two blocks take turns, and the next but one is already on its way from memory.
+// S^T = K q^T lies in registers as the B operand of O^T = V^T P^T wants it: a lane's keys of a 16-key tile are 4 h .. + 3 and
+// 8 + 4 h .. + 3 (h = lane / 32), and V's fragments are laid out in that order.
+#include "ams_kv_attention.h"
+
+namespace ams_kv {
+
+typedef float f16v __attribute__((ext_vector_type(16)));
+
+constexpr int kBlock = 64;                // keys
+constexpr int kBlockTiles = kBlock / kTile;
+constexpr int kBlockSteps = kBlock / kStep;
+
+// What LDS holds of a block.
+template <int D>
+struct Block {
+  h8 k[2][D / 16][64];            // [32 keys][16 channels][lane]
+  h8 v[D / 32][kBlockTiles][64];  // [32 channels][16 keys][lane]
+};
+// Of its tiles: whether the table names a page, and the keys (bits) whose V stands for NaN, by run.
+template <int RUNS>
+struct Notes {
+  uint32_t missing[kBlockTiles], bad[kBlockTiles], by_run[kBlockTiles][RUNS];
+};
+
+// A tile of K or V on its way through a wavefront.
+template <int D, int G>
+struct Job {
+  static constexpr int RUNS = D / G;
+  uint32_t w[D / 32], s[2 * RUNS];
+  bool held;
+  __device__ __forceinline__ void load(const AttentionArgs& a, int number, int head, int tile, bool is_v, uint32_t lane) {
+    held = number >= 0;
+    const uint64_t begin = (uint64_t)a.v.pages + (uint64_t)(held ? number : 0) * (uint64_t)a.v.page_bytes + (uint64_t)(uint32_t)head * (uint32_t)a.v.block;
+    const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc((void*)begin, 0, held ? a.v.block : 0, 0x00020000);  // of no page nothing is read
+    const int in_page = (int)((uint32_t)tile - a.v.page_tiles.quotient((uint32_t)tile) * a.v.page_tiles.by);
+    Lane<D> words;
+    load_words<D>(words, from, lane, (is_v ? a.v.codes : 0) + in_page * 8 * D);
+#pragma unroll
+    for (int i = 0; i < D / 32; i++) w[i] = words.w[i];
+    const int scales = 2 * a.v.codes + in_page * kTile * RUNS * 2;
+    if (is_v) {
+#pragma unroll
+      for (int i = 0; i < 2 * RUNS; i += 2) {
+        const u2 x = __builtin_bit_cast(u2, __builtin_amdgcn_raw_buffer_load_b64(from, (lane >> 4) * (RUNS * 8u) + 4 * i, scales + a.v.scales, 0));
+        s[i] = x[0], s[i + 1] = x[1];
+      }
+    } else {
+      Scales<RUNS> x;
+      x.load(from, (lane & 15) * (RUNS * 2u), scales);
+#pragma unroll
+      for (int i = 0; i < Scales<RUNS>::WORDS; i++) s[i] = x.w[i];
+    }
+  }
+  __device__ __forceinline__ void store_k(Block<D>& block, int tile, int lane) const {
+    const int g = lane >> 4, r = lane & 15;
+    Scales<RUNS> x;
+#pragma unroll
+    for (int i = 0; i < Scales<RUNS>::WORDS; i++) x.w[i] = s[i];
+    h8* const to = &block.k[tile >> 1][g >> 1][(g & 1) * 32 + (tile & 1) * 16 + r];
+#pragma unroll
+    for (int i = 0; i < D / 32; i++) to[2 * i * 64] = restore_k(w[i], x.twice(32 * i / G));
+  }
+  __device__ __forceinline__ void store_v(Block<D>& block, Notes<RUNS>& notes, int tile, int lane) {
+    const int q = lane >> 4, c = lane & 15;
+    // a scale that stands for NaN times 0 is NaN
+    h2 nan = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 2 * RUNS; i++) nan += halves(s[i]) * h2{0, 0};
+    const bool bad = nan[0] != nan[0] || nan[1] != nan[1];
+    const bool any = __ballot(bad) != 0;
+    if (any) note_bad(notes, tile, lane);
+    if (lane == 0) notes.missing[tile] = held ? 0 : 1, notes.bad[tile] = any;
+    u2* const to = (u2*)&block.v[0][tile][(q & 1) * 32 + c] + (q >> 1);
+#pragma unroll
+    for (int i = 0; i < D / 32; i++) {
+      u2 x, y;
+      restore_v(w[i], s[32 * i / G * 2], s[32 * i / G * 2 + 1], &x, &y);
+      to[i * kBlockTiles * 128] = x;
+      to[i * kBlockTiles * 128 + 32] = y;
+    }
+  }
+  // V's runs that stand for NaN take part as zeros: what masks a key cannot be told from its 0 weight.  The rows that see one get the NaN.
+  __device__ __forceinline__ void note_bad(Notes<RUNS>& notes, int tile, int lane) {
+    const int q = lane >> 4;
+#pragma unroll
+    for (int run = 0; run < RUNS; run++) {
+      uint32_t keys = 0;
+#pragma unroll
+      for (int j = 0; j < 4; j++)
+        if ((s[2 * run + j / 2] >> 16 * (j & 1) & 0x7C00) == 0x7C00) {
+          keys |= 1u << (4 * q + j);
+          s[2 * run + j / 2] &= j & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+        }
+      keys |= (uint32_t)__shfl_xor((int)keys, 16, 64);
+      keys |= (uint32_t)__shfl_xor((int)keys, 32, 64);
+      if (lane == 0) notes.by_run[tile][run] = keys;
+    }
+  }
+};
+
+template <int D, int G>
+__global__ __launch_bounds__(64 * tile_waves(D), D == 256 ? 1 : 2) void tile_kernel(AttentionArgs a) {
+  constexpr int WAVES = tile_waves(D), ROWS = 32 * WAVES, RUNS = D / G, KF = D / 16, DT = D / 32, JOBS = 2 * kBlockTiles / WAVES;
+  const int wave = uniform((int)threadIdx.x >> 6), lane = lane_id(), h = lane >> 5, col = lane & 31;
+  const int share = (int)a.v.heads.quotient(blockIdx.x), head = blockIdx.x - share * a.v.kv_heads;
+  __shared__ Block<D> blocks[2];
+  __shared__ Notes<RUNS> notes[2];
+  __shared__ bool all_there[2];
+
+  const Extent first_64 = extent_of<ROWS>(a, lane);
+  const Split split = split_of<ROWS>(a, first_64);
+  uint32_t now = share * split.per, stop = min(now + split.per, split.total);
+  if (!split.cut && now < split.total) {  // the tiles with the most keys are a sequence's last: they go first
+    now = split.total - min(now + split.per, split.total);
+    stop = min(now + split.per, split.total);
+  }
+  const __amdgpu_buffer_rsrc_t left = __builtin_amdgcn_make_buffer_rsrc((void*)(a.parts + (int64_t)uniform(head) * 2 * a.shares * a.part_rows * (D + 4)), 0,
+                                                                        a.cut ? 2 * a.shares * a.part_rows * (D + 4) * 4 : 0, 0x00020000);  // this head's parts
+  Place place;
+  Pending left_first = {}, left_last = {};
+  int pending = 0;
+  while (now < stop && place_of<ROWS>(a, first_64, split.cut, now, &place)) {
+    const Extent& e = place.e;
+    const int rows = e.n * a.group, tile_row = place.row_tile * ROWS, row0 = tile_row + 32 * wave;
+    const uint32_t then = min(place.first + place.cost, stop);
+    const int begin_step = split.cut ? max((int)(now - place.first) - kTileSteps, 0) : 0, end_step = split.cut ? (int)(then - place.first) - kTileSteps : e.steps;
+    now = then;
+    if (end_step <= 0) break;  // the tile begins in the next share
+    const bool alone = begin_step == 0 && end_step == e.steps;
+    auto position = [&](int r) { return e.len - e.n + (int)a.by_group.quotient((uint32_t)r); };
+    // the keys of the share that some row of the tile sees
+    const int key_from = uniform(max(e.lo + begin_step * kStep, key_begin(a, position(tile_row)) & ~(kStep - 1)));
+    const int key_to = uniform(min(e.lo + end_step * kStep, key_end(a, e.len, position(min(tile_row + ROWS, rows) - 1))));
+    const int n_blocks = max((key_to - key_from + kBlock - 1) / kBlock, 0);
+    // of those the ones that every row and that no row of the wavefront sees
+    const bool idle = row0 >= rows;
+    const int p_first = position(row0), p_last = position(min(row0 + 32, rows) - 1);
+    const int whole_begin = uniform(key_begin(a, p_last)), whole_end = uniform(min(key_end(a, e.len, p_first), key_to));
+    const int some_begin = uniform(key_begin(a, p_first)), some_end = uniform(idle ? 0 : min(key_end(a, e.len, p_last), key_to));
+    const int r = row0 + col;
+    const int row_begin = key_begin(a, position(r)), row_end = r < rows ? min(key_end(a, e.len, position(r)), key_to) : 0;
+
+    h8 q[KF];
+    {
+      const int token = (int)a.by_group.quotient((uint32_t)r);
+      const uint16_t* const src = a.q + (int64_t)(e.start + token) * a.q_stride + (int64_t)(head * a.group + r - token * a.group) * a.q_head + 8 * h;
+#pragma unroll
+      for (int i = 0; i < KF; i++) {
+        u4 x = {0, 0, 0, 0};
+        if (r < rows) x = load_half8(src + 16 * i, a.vec);
+        q[i] = __builtin_bit_cast(h8, x);
+      }
+    }
+    f16v o[DT];
+    float m = -INFINITY, l = 0;
+#pragma unroll
+    for (int d = 0; d < DT; d++)
+#pragma unroll
+      for (int i = 0; i < 16; i++) o[d][i] = 0;
+
+    // A wavefront's jobs: tile `wave % 4` of each block, of K, of V, or of both.
+    const int my_tile = wave % kBlockTiles;
+    int number = -1;  // the page of that tile in 64 blocks, one to a lane
+    auto look_up = [&](int block) {
+      const int tile = key_from / kTile + (block + hidden(lane)) * kBlockTiles + my_tile;
+      const uint32_t page = a.v.page_tiles.quotient((uint32_t)tile);
+      number = -1;
+      if (tile * kTile < key_to && page < (uint32_t)a.v.table_width) {
+        const int found = a.v.table[place.b * a.v.table_stride + page];
+        if ((uint32_t)found < (uint32_t)a.v.n_pages) number = found;
+      }
+    };
+    Job<D, G> jobs[JOBS];
+    auto request = [&](int block) {
+      if (block % 64 == 0) look_up(block);
+#pragma unroll
+      for (int j = 0; j < JOBS; j++)
+        jobs[j].load(a, of_lane(number, block % 64), head, key_from / kTile + block * kBlockTiles + my_tile, JOBS == 1 ? wave >= kBlockTiles : j == 1, lane);
+    };
+    auto restore = [&](int buffer) {
+#pragma unroll
+      for (int j = 0; j < JOBS; j++) {
+        if (JOBS == 1 ? wave >= kBlockTiles : j == 1)
+          jobs[j].store_v(blocks[buffer], notes[buffer], my_tile, hidden(lane));
+        else
+          jobs[j].store_k(blocks[buffer], my_tile, hidden(lane));
+      }
+    };
+    auto compute = [&](int buffer, int key0) {
+      const Block<D>& block = blocks[buffer];
+      f16v s[2];
+#pragma unroll
+      for (int kt = 0; kt < 2; kt++) {
+#pragma unroll
+        for (int i = 0; i < 16; i++) s[kt][i] = 0;
+#pragma unroll
+        for (int i = 0; i < KF; i++) s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(block.k[kt][i][lane], q[i], s[kt], 0, 0, 0);
+      }
+      const u4 missing = *(const u4*)notes[buffer].missing;
+      const bool any_missing = uniform(missing[0] | missing[1] | missing[2] | missing[3]) != 0;
+      if (key0 < whole_begin || key0 + kBlock > whole_end || any_missing) {  // some row does not see some key
+#pragma unroll
+        for (int kt = 0; kt < 2; kt++)
+#pragma unroll
+          for (int i = 0; i < 16; i++) {
+            const int key = key0 + 32 * kt + 8 * (i / 4) + 4 * h + i % 4;
+            if (key < row_begin || key >= row_end || missing[2 * kt + i / 8]) s[kt][i] = -INFINITY;
+          }
+      }
+      float top = s[0][0];
+#pragma unroll
+      for (int i = 1; i < 32; i++) top = fmaxf(top, s[i / 16][i % 16]);
+      top *= a.scale2;
+      if (__ballot(top > m + kSlack)) {  // the maximum is raised only where a score passes it by more than the slack
+        top = fmaxf(top, m);
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        const float less = top > m ? __builtin_amdgcn_exp2f(m - top) : 1.0f;
+        m = top;
+        l *= less;
+#pragma unroll
+        for (int d = 0; d < DT; d++) o[d] *= less;
+      }
+      const float sub = m == -INFINITY ? 0.0f : m - kLift;
+      h8 p[kBlockTiles];
+      float sum[2] = {0, 0};
+#pragma unroll
+      for (int i = 0; i < 32; i++) {
+        const float v = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 16][i % 16], a.scale2, -sub));
+        sum[i & 1] += v;
+        p[i / 8][i % 8] = (_Float16)v;
+      }
+      l += sum[0] + sum[1];
+#pragma unroll
+      for (int t = 0; t < kBlockTiles; t++)
+#pragma unroll
+        for (int d = 0; d < DT; d++) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(block.v[d][t][lane], p[t], o[d], 0, 0, 0);
+      const u4 bad = *(const u4*)notes[buffer].bad;
+      if (uniform(bad[0] | bad[1] | bad[2] | bad[3])) {
+#pragma unroll
+        for (int run = 0; run < RUNS; run++) {
+          bool seen = false;
+          for (int t = 0; t < kBlockTiles; t++) {
+            const int first = key0 + kTile * t, from = min(max(row_begin - first, 0), kTile), to = min(max(row_end - first, 0), kTile);
+            if (bad[t] && !missing[t]) seen |= (notes[buffer].by_run[t][run] & ((1u << to) - 1) & ~((1u << from) - 1)) != 0;
+          }
+          if (seen) {
+#pragma unroll
+            for (int d = run * G / 32; d < (run + 1) * G / 32; d++)
+#pragma unroll
+              for (int i = 0; i < 16; i++) o[d][i] = NAN;
+          }
+        }
+      }
+    };
+
+    if (n_blocks > 0) {
+      request(0);
+      restore(0);
+      if (n_blocks > 1) request(1);
+      __syncthreads();
+#pragma unroll 1
+      for (int block = 0; block < n_blocks; block++) {
+        if (block + 1 < n_blocks) restore((block + 1) & 1);
+        if (block + 2 < n_blocks) request(block + 2);
+        const int key0 = key_from + block * kBlock;
+        if (key0 < some_end && key0 + kBlock > some_begin) compute(block & 1, key0);
+        __syncthreads();
+      }
+    }
+
+    l += __shfl_xor(l, 32, 64);
+    const int part = (2 * share + (begin_step == 0)) * a.part_rows + 32 * wave + col;
+    if (r < rows) {
+      const float scale = alone ? (l > 0 || l != l ? 1.0f / l : 0.0f) : 1.0f;
+#pragma unroll
+      for (int d = 0; d < DT; d++)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+          const f4 x = f4{o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]} * scale;
+          const int channel = 32 * d + 2 * i + 4 * h;
+          if (alone)
+            store_out(a, e.start, head, r, channel, x);
+          else
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4, x), left, (part * (D + 4) + 4 + channel) * 4, 0, kDeviceScope);
+        }
+      if (h == 0) {
+        if (alone)
+          store_lse(a, e.start, head, r, m, l);
+        else
+          __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u2, f2{m, l}), left, part * (D + 4) * 4, 0, kDeviceScope);
+      }
+    }
+    if (!alone) {
+      const int first = (int)((place.first + kTileSteps) / split.per), last = (int)((place.first + kTileSteps + e.steps - 1) / split.per);
+      left_last = Pending{e.start, tile_row, min(rows - tile_row, ROWS), first, last - first + 1};
+      if (pending == 0) left_first = left_last;
+      pending++;
+    }
+  }
+  join_pending<D, 64 * WAVES>(a, pending, left_first, left_last, left, head, (float*)blocks, all_there);
+}
+
+void launch_tile(const AttentionArgs& a, int head_dim, int scale_group, unsigned grid, hipStream_t stream) {
+  dispatch(head_dim, scale_group, [&](auto d, auto g) {
+    constexpr int D = decltype(d)::value, G = decltype(g)::value;
+    hipLaunchKernelGGL((tile_kernel<D, G>), dim3(grid), dim3(64 * tile_waves(D)), 0, stream, a);
+  });
+}
+
+}  // namespace ams_kv
