@@ -13,7 +13,8 @@ typedef float f16v __attribute__((ext_vector_type(16)));
 
 constexpr int kBlock = 64;                // keys
 constexpr int kBlockTiles = kBlock / kTile;
-constexpr int kBlockSteps = kBlock / kStep;
+constexpr int kAhead = 4;                 // fragments that are read ahead
+constexpr int kReads = 0x100, kProducts = 0x008;  // of a scheduling group: LDS reads, matrix instructions
 
 // What LDS holds of a block.
 template <int D>
@@ -42,25 +43,25 @@ struct Job {
     load_words<D>(words, from, lane, (is_v ? a.v.codes : 0) + in_page * 8 * D);
 #pragma unroll
     for (int i = 0; i < D / 32; i++) w[i] = words.w[i];
-    const int scales = 2 * a.v.codes + in_page * kTile * RUNS * 2;
-    if (is_v) {
-#pragma unroll
-      for (int i = 0; i < 2 * RUNS; i += 2) {
-        const u2 x = __builtin_bit_cast(u2, __builtin_amdgcn_raw_buffer_load_b64(from, (lane >> 4) * (RUNS * 8u) + 4 * i, scales + a.v.scales, 0));
-        s[i] = x[0], s[i + 1] = x[1];
-      }
+    // both kinds by the same loads: a token's RUNS scales of K, which begin in the first word, or the 4 RUNS of four tokens of V
+    const uint32_t mine = is_v ? (lane >> 4) * (RUNS * 8u) : (lane & 15) * (RUNS * 2u) & ~3u;
+    const int scales = 2 * a.v.codes + (is_v ? a.v.scales : 0) + in_page * kTile * RUNS * 2;
+    if constexpr (RUNS == 1) {
+      const u2 x = __builtin_bit_cast(u2, __builtin_amdgcn_raw_buffer_load_b64(from, mine, scales, 0));
+      s[0] = x[0], s[1] = x[1];
     } else {
-      Scales<RUNS> x;
-      x.load(from, (lane & 15) * (RUNS * 2u), scales);
 #pragma unroll
-      for (int i = 0; i < Scales<RUNS>::WORDS; i++) s[i] = x.w[i];
+      for (int i = 0; i < 2 * RUNS; i += 4) {
+        const u4 x = __builtin_bit_cast(u4, __builtin_amdgcn_raw_buffer_load_b128(from, i == 0 || is_v ? mine + 4 * i : 0x7FFE0000u, scales, 0));
+        s[i] = x[0], s[i + 1] = x[1], s[i + 2] = x[2], s[i + 3] = x[3];
+      }
     }
   }
   __device__ __forceinline__ void store_k(Block<D>& block, int tile, int lane) const {
     const int g = lane >> 4, r = lane & 15;
     Scales<RUNS> x;
 #pragma unroll
-    for (int i = 0; i < Scales<RUNS>::WORDS; i++) x.w[i] = s[i];
+    for (int i = 0; i < Scales<RUNS>::WORDS; i++) x.w[i] = RUNS == 1 ? s[i] >> 16 * (r & 1) : s[i];
     h8* const to = &block.k[tile >> 1][g >> 1][(g & 1) * 32 + (tile & 1) * 16 + r];
 #pragma unroll
     for (int i = 0; i < D / 32; i++) to[2 * i * 64] = restore_k(w[i], x.twice(32 * i / G));
@@ -193,14 +194,28 @@ __global__ __launch_bounds__(64 * tile_waves(D), D == 256 ? 1 : 2) void tile_ker
     };
     auto compute = [&](int buffer, int key0) {
       const Block<D>& block = blocks[buffer];
+      // Fragments are read four instructions ahead of the one that takes them; left to itself the compiler reads each one where it is used
+      // and waits for it.
+      constexpr int NK = 2 * KF, NV = kBlockTiles * DT;
+      h8 f[kAhead];
       f16v s[2];
 #pragma unroll
-      for (int kt = 0; kt < 2; kt++) {
+      for (int i = 0; i < 16; i++) s[0][i] = s[1][i] = 0;
 #pragma unroll
-        for (int i = 0; i < 16; i++) s[kt][i] = 0;
+      for (int n = 0; n < kAhead; n++) f[n] = block.k[n & 1][n >> 1][lane];
 #pragma unroll
-        for (int i = 0; i < KF; i++) s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(block.k[kt][i][lane], q[i], s[kt], 0, 0, 0);
+      for (int n = 0; n < NK; n++) {
+        s[n & 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[n % kAhead], q[n >> 1], s[n & 1], 0, 0, 0);
+        if (n + kAhead < NK) f[n % kAhead] = block.k[(n + kAhead) & 1][(n + kAhead) >> 1][lane];
       }
+      __builtin_amdgcn_sched_group_barrier(kReads, kAhead, 0);
+#pragma unroll
+      for (int n = 0; n < NK; n++) {
+        __builtin_amdgcn_sched_group_barrier(kProducts, 1, 0);
+        if (n + kAhead < NK) __builtin_amdgcn_sched_group_barrier(kReads, 1, 0);
+      }
+#pragma unroll
+      for (int n = 0; n < kAhead; n++) f[n] = block.v[n % DT][n / DT][lane];
       const u4 missing = *(const u4*)notes[buffer].missing;
       const bool any_missing = uniform(missing[0] | missing[1] | missing[2] | missing[3]) != 0;
       if (key0 < whole_begin || key0 + kBlock > whole_end || any_missing) {  // some row does not see some key
@@ -236,9 +251,15 @@ __global__ __launch_bounds__(64 * tile_waves(D), D == 256 ? 1 : 2) void tile_ker
       }
       l += sum[0] + sum[1];
 #pragma unroll
-      for (int t = 0; t < kBlockTiles; t++)
+      for (int n = 0; n < NV; n++) {
+        o[n % DT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[n % kAhead], p[n / DT], o[n % DT], 0, 0, 0);
+        if (n + kAhead < NV) f[n % kAhead] = block.v[(n + kAhead) % DT][(n + kAhead) / DT][lane];
+      }
 #pragma unroll
-        for (int d = 0; d < DT; d++) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(block.v[d][t][lane], p[t], o[d], 0, 0, 0);
+      for (int n = 0; n < NV; n++) {
+        __builtin_amdgcn_sched_group_barrier(kProducts, 1, 1);
+        if (n + kAhead < NV) __builtin_amdgcn_sched_group_barrier(kReads, 1, 1);
+      }
       const u4 bad = *(const u4*)notes[buffer].bad;
       if (uniform(bad[0] | bad[1] | bad[2] | bad[3])) {
 #pragma unroll
