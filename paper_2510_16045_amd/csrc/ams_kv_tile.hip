@@ -22,10 +22,11 @@ struct Block {
   h8 k[2][D / 16][64];            // [32 keys][16 channels][lane]
   h8 v[D / 32][kBlockTiles][64];  // [32 channels][16 keys][lane]
 };
-// Of its tiles: whether the table names a page, and the keys (bits) whose V stands for NaN, by run.
+// Of its tiles: whether the table names no page, and whether V stands for NaN somewhere; if so the keys (bits), by run.
+constexpr uint32_t kMissing = 1, kBad = 2;
 template <int RUNS>
 struct Notes {
-  uint32_t missing[kBlockTiles], bad[kBlockTiles], by_run[kBlockTiles][RUNS];
+  uint32_t what[kBlockTiles], bad[kBlockTiles][RUNS];
 };
 
 // A tile of K or V on its way through a wavefront.
@@ -75,7 +76,7 @@ struct Job {
     const bool bad = nan[0] != nan[0] || nan[1] != nan[1];
     const bool any = __ballot(bad) != 0;
     if (any) note_bad(notes, tile, lane);
-    if (lane == 0) notes.missing[tile] = held ? 0 : 1, notes.bad[tile] = any;
+    if (lane == 0) notes.what[tile] = (held ? 0 : kMissing) | (any ? kBad : 0);
     u2* const to = (u2*)&block.v[0][tile][(q & 1) * 32 + c] + (q >> 1);
 #pragma unroll
     for (int i = 0; i < D / 32; i++) {
@@ -99,7 +100,7 @@ struct Job {
         }
       keys |= (uint32_t)__shfl_xor((int)keys, 16, 64);
       keys |= (uint32_t)__shfl_xor((int)keys, 32, 64);
-      if (lane == 0) notes.by_run[tile][run] = keys;
+      if (lane == 0) notes.bad[tile][run] = keys;
     }
   }
 };
@@ -197,6 +198,7 @@ __global__ __launch_bounds__(64 * tile_waves(D), D == 256 ? 1 : 2) void tile_ker
       // Fragments are read four instructions ahead of the one that takes them; left to itself the compiler reads each one where it is used
       // and waits for it.
       constexpr int NK = 2 * KF, NV = kBlockTiles * DT;
+      const u4 what = *(const u4*)notes[buffer].what;
       h8 f[kAhead];
       f16v s[2];
 #pragma unroll
@@ -216,15 +218,14 @@ __global__ __launch_bounds__(64 * tile_waves(D), D == 256 ? 1 : 2) void tile_ker
       }
 #pragma unroll
       for (int n = 0; n < kAhead; n++) f[n] = block.v[n % DT][n / DT][lane];
-      const u4 missing = *(const u4*)notes[buffer].missing;
-      const bool any_missing = uniform(missing[0] | missing[1] | missing[2] | missing[3]) != 0;
-      if (key0 < whole_begin || key0 + kBlock > whole_end || any_missing) {  // some row does not see some key
+      const uint32_t anything = (uint32_t)uniform((int)(what[0] | what[1] | what[2] | what[3]));
+      if (key0 < whole_begin || key0 + kBlock > whole_end || (anything & kMissing)) {  // some row does not see some key
 #pragma unroll
         for (int kt = 0; kt < 2; kt++)
 #pragma unroll
           for (int i = 0; i < 16; i++) {
             const int key = key0 + 32 * kt + 8 * (i / 4) + 4 * h + i % 4;
-            if (key < row_begin || key >= row_end || missing[2 * kt + i / 8]) s[kt][i] = -INFINITY;
+            if (key < row_begin || key >= row_end || (what[2 * kt + i / 8] & kMissing)) s[kt][i] = -INFINITY;
           }
       }
       float top = s[0][0];
@@ -260,14 +261,13 @@ __global__ __launch_bounds__(64 * tile_waves(D), D == 256 ? 1 : 2) void tile_ker
         __builtin_amdgcn_sched_group_barrier(kProducts, 1, 1);
         if (n + kAhead < NV) __builtin_amdgcn_sched_group_barrier(kReads, 1, 1);
       }
-      const u4 bad = *(const u4*)notes[buffer].bad;
-      if (uniform(bad[0] | bad[1] | bad[2] | bad[3])) {
+      if (anything & kBad) {
 #pragma unroll
         for (int run = 0; run < RUNS; run++) {
           bool seen = false;
           for (int t = 0; t < kBlockTiles; t++) {
             const int first = key0 + kTile * t, from = min(max(row_begin - first, 0), kTile), to = min(max(row_end - first, 0), kTile);
-            if (bad[t] && !missing[t]) seen |= (notes[buffer].by_run[t][run] & ((1u << to) - 1) & ~((1u << from) - 1)) != 0;
+            if (what[t] & kBad) seen |= (notes[buffer].bad[t][run] & ((1u << to) - 1) & ~((1u << from) - 1)) != 0;
           }
           if (seen) {
 #pragma unroll
