@@ -171,63 +171,64 @@ __device__ __forceinline__ void store_lse(const AttentionArgs& a, int start, int
   a.lse[(int64_t)(start + token) * a.lse_stride + head * a.group + r - token * a.group] = sum > 0 || sum != sum ? (top - kLift + __log2f(sum)) * 0.69314718056f : -INFINITY;
 }
 
-// Adds up the parts of a row tile.  D / 4 lanes take a row, four channels each; of the workgroup's groups of
-// lanes as many take the rows as there are (a power of two), and the others share the parts of a row; 8 parts are asked for before the
-// first is used.
-template <int D, int THREADS>
+// Adds up the parts of a row tile.  D / 4 lanes take a row, four channels each; of the workgroup's groups of lanes as many take rows
+// as there are (a power of two), U rows each at once, and the others share the parts of a row, P of them at once: U P parts of rows are
+// asked for before the first is used.
+template <int D, int THREADS, int U, int P>
 __device__ __forceinline__ void join_parts(const AttentionArgs& a, const Pending& tile, __amdgpu_buffer_rsrc_t left, int head, float* lds) {
-  constexpr int LANES = D / 4, GROUPS = THREADS / LANES, AHEAD = 8;
-  f4* const xs = (f4*)lds;             // [group][lane]
+  constexpr int LANES = D / 4, GROUPS = THREADS / LANES;
+  f4* const xs = (f4*)lds;                // [group][lane]
   f2* const stats = (f2*)(xs + THREADS);  // [group]
   const int group = threadIdx.x / LANES, c = threadIdx.x % LANES;
   const int rows = tile.rows, first = tile.first, count = tile.count;
   int takers = 1;  // groups that take rows
   while (takers < rows && takers < GROUPS) takers *= 2;
   const int sharers = GROUPS / takers, mine = group / takers;
-  for (int i0 = 0; i0 < rows; i0 += takers) {
-    const int i = i0 + group % takers;
-    float top = -INFINITY, sum = 0;
-    f4 x = {0, 0, 0, 0};
-    for (int s0 = mine; s0 < count; s0 += sharers * AHEAD) {
-      f4 from[AHEAD];
-      f2 stat[AHEAD];
+  auto add = [](float& top, float& sum, f4& x, float part_top, float part_sum, f4 part) {
+    const float most = fmaxf(top, part_top);
+    const float less = top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top - most), by = part_top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(part_top - most);
+    top = most;
+    sum = sum * less + part_sum * by;
+    x = x * less + part * by;
+  };
+#pragma unroll 1
+  for (int i0 = 0; i0 < rows; i0 += takers * U) {
+    float top[U], sum[U];
+    f4 x[U];
 #pragma unroll
-      for (int j = 0; j < AHEAD; j++) {
-        const int s = s0 + j * sharers;
-        const int at = s < count && i < rows ? ((2 * (first + s) + (s == 0)) * a.part_rows + i) * (D + 4) * 4 : 0x7FFE0000;  // nothing is read there
-        from[j] = __builtin_bit_cast(f4, __builtin_amdgcn_raw_buffer_load_b128(left, at + 16 + 16 * c, 0, kDeviceScope));
-        stat[j] = __builtin_bit_cast(f2, __builtin_amdgcn_raw_buffer_load_b64(left, at, 0, kDeviceScope));
-        if (s >= count) stat[j] = f2{-INFINITY, 0};
-      }
-      float most = top;
+    for (int u = 0; u < U; u++) top[u] = -INFINITY, sum[u] = 0, x[u] = f4{0, 0, 0, 0};
+#pragma unroll 1
+    for (int s0 = mine; s0 < count; s0 += sharers * P) {
+      f4 from[U][P];
+      f2 stat[U][P];
 #pragma unroll
-      for (int j = 0; j < AHEAD; j++) most = fmaxf(most, stat[j][0]);
-      const float less = top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top - most);
-      top = most;
-      sum *= less, x *= less;
+      for (int u = 0; u < U; u++)
 #pragma unroll
-      for (int j = 0; j < AHEAD; j++) {
-        const float by = stat[j][0] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(stat[j][0] - top);
-        sum += stat[j][1] * by;
-        x += from[j] * by;
-      }
+        for (int j = 0; j < P; j++) {
+          const int s = s0 + j * sharers, i = i0 + u * takers + group % takers;
+          const int at = s < count && i < rows ? ((2 * (first + s) + (s == 0)) * a.part_rows + i) * (D + 4) * 4 : 0x7FFE0000;  // nothing is read there
+          from[u][j] = __builtin_bit_cast(f4, __builtin_amdgcn_raw_buffer_load_b128(left, at + 16 + 16 * c, 0, kDeviceScope));
+          stat[u][j] = __builtin_bit_cast(f2, __builtin_amdgcn_raw_buffer_load_b64(left, at, 0, kDeviceScope));
+          if (s >= count) stat[u][j] = f2{-INFINITY, 0};
+        }
+#pragma unroll
+      for (int u = 0; u < U; u++)
+#pragma unroll
+        for (int j = 0; j < P; j++) add(top[u], sum[u], x[u], stat[u][j][0], stat[u][j][1], from[u][j]);
     }
-    __syncthreads();  // what was in LDS has been read
-    xs[threadIdx.x] = x;
-    if (c == 0) stats[group] = f2{top, sum};
-    __syncthreads();
-    if (mine == 0 && i < rows) {
-      top = -INFINITY, sum = 0;
-      x = f4{0, 0, 0, 0};
-      for (int j = 0; j < sharers; j++) top = fmaxf(top, stats[j * takers + group][0]);
-      for (int j = 0; j < sharers; j++) {
-        const f2 stat = stats[j * takers + group];
-        const float by = stat[0] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(stat[0] - top);
-        sum += stat[1] * by;
-        x += xs[(j * takers + group) * LANES + c] * by;
-      }
-      store_out(a, tile.start, head, tile.row0 + i, 4 * c, x * (sum > 0 || sum != sum ? 1.0f / sum : 0.0f));
-      if (c == 0) store_lse(a, tile.start, head, tile.row0 + i, top, sum);
+    if (sharers > 1) {  // then every row has a taker, in its first turn
+      xs[threadIdx.x] = x[0];
+      if (c == 0) stats[group] = f2{top[0], sum[0]};
+      __syncthreads();
+      for (int j = 1; j < sharers && mine == 0; j++) add(top[0], sum[0], x[0], stats[j * takers + group][0], stats[j * takers + group][1], xs[(j * takers + group) * LANES + c]);
+      __syncthreads();
+    }
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+      const int i = i0 + u * takers + group % takers;
+      if (mine > 0 || i >= rows) continue;
+      store_out(a, tile.start, head, tile.row0 + i, 4 * c, x[u] * (sum[u] > 0 || sum[u] != sum[u] ? 1.0f / sum[u] : 0.0f));
+      if (c == 0) store_lse(a, tile.start, head, tile.row0 + i, top[u], sum[u]);
     }
   }
 }
@@ -235,7 +236,7 @@ __device__ __forceinline__ void join_parts(const AttentionArgs& a, const Pending
 // The end of a workgroup whose share has `pending` tiles that lie in others too (only its first and its last can).  Every wavefront's
 // stores have been acknowledged before the workgroup is counted in, and the parts are asked for after the count has come back; they go
 // to the level of the memory system that all compute units share.
-template <int D, int THREADS>
+template <int D, int THREADS, int U, int P>
 __device__ __forceinline__ void join_pending(const AttentionArgs& a, int pending, const Pending& first, const Pending& last, __amdgpu_buffer_rsrc_t left, int head, float* lds, bool* all_there) {
   if (pending == 0) return;
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -251,16 +252,16 @@ __device__ __forceinline__ void join_pending(const AttentionArgs& a, int pending
   __syncthreads();
 #pragma unroll 1
   for (int i = 0; i < pending; i++)
-    if (all_there[i]) join_parts<D, THREADS>(a, i == 0 ? first : last, left, head, lds);
+    if (all_there[i]) join_parts<D, THREADS, U, P>(a, i == 0 ? first : last, left, head, lds);
 }
 
 // ---- the kernels' launches -----------------------------------------------------------------------------
-// Wavefronts of a workgroup, and of stream_kernel workgroups of a compute unit: what the registers allow.
-constexpr int tile_waves(int d) { return d == 256 ? 4 : 8; }
+// Wavefronts of a workgroup, and workgroups of a compute unit: what the registers allow.
 constexpr int stream_waves(int, int) { return 4; }
 constexpr int stream_groups(int d, int qt) { return d * qt <= 128 ? 3 : d * qt < 512 ? 2 : 1; }
+constexpr int tile_groups(int d, int waves) { return d == 256 || waves == 8 ? 1 : 2; }
 void launch_stream(const AttentionArgs& a, int head_dim, int scale_group, int qt, unsigned grid, hipStream_t stream);
-void launch_tile(const AttentionArgs& a, int head_dim, int scale_group, unsigned grid, hipStream_t stream);
+void launch_tile(const AttentionArgs& a, int head_dim, int scale_group, int waves, unsigned grid, hipStream_t stream);  // 8 only up to D = 128
 
 }  // namespace ams_kv
 #endif

@@ -9,31 +9,36 @@ namespace ams_kv {
 
 // ---- launch ------------------------------------------------------------------------------------------
 constexpr int kComputeUnits = 256;
-constexpr int kStreamRows = 64;  // up to so many rows of a kv head stream_kernel takes
+constexpr int kStreamRows = 64;   // up to so many rows of a kv head stream_kernel takes
+constexpr int kLongKeys = 4096;   // keys from which on tiles of 256 rows are the faster ones, where they fill the chip
 constexpr size_t kCountBytes = 64 * 1024;  // of a workspace: counts of any call (kv_heads x shares of them), at its front
 static_assert(4 * kComputeUnits * sizeof(uint32_t) <= kCountBytes && AMS_KV_MAX_HEADS * sizeof(uint32_t) <= kCountBytes, "one for each share of each head");
 
 struct Plan {
   bool tile;  // tile_kernel
+  int waves;  // of its workgroups
   int qt, rows, part_rows;
   int64_t row_tiles;  // at most so many over all sequences
   int64_t shares;
   bool cut;
   size_t workspace;   // bytes that this many shares need
 };
-Plan make_plan(const ams_kv_cache* c, int64_t rows, int heads, int64_t max_q_len, size_t workspace) {
+Plan make_plan(const ams_kv_cache* c, int64_t rows, int heads, int64_t max_q_len, int64_t window, size_t workspace) {
   Plan p;
   const int R = heads / c->kv_heads;
   const int64_t most = (c->q_starts ? std::min(max_q_len > 0 ? max_q_len : rows, rows) : 1) * R;
   p.tile = most > kStreamRows;
+  const int64_t capacity = (int64_t)c->table_width * c->page_size, keys = window > 0 ? std::min(window, capacity) : capacity;
   p.qt = most <= 16 ? 1 : most <= 32 || c->head_dim == 256 ? 2 : 4;
-  p.rows = p.tile ? 32 * tile_waves(c->head_dim) : 16 * p.qt;
+  p.waves = 4;
+  if (p.tile && c->head_dim < 256 && (rows * R / 256 + c->batch) * c->kv_heads >= kComputeUnits && keys >= kLongKeys) p.waves = 8;
+  p.rows = p.tile ? 32 * p.waves : 16 * p.qt;
   p.row_tiles = c->q_starts ? rows * R / p.rows + c->batch : c->batch * (int64_t)((R + p.rows - 1) / p.rows);
-  const int64_t tile_steps = std::max<int64_t>(((int64_t)c->table_width * c->page_size + kStep - 1) / kStep, 1);
+  const int64_t tile_steps = std::max<int64_t>((capacity + kStep - 1) / kStep, 1);
   p.part_rows = (int)std::min<int64_t>(c->q_starts ? rows * R : R, p.rows);
   const size_t part = (size_t)c->kv_heads * p.part_rows * (c->head_dim + 4) * sizeof(float);
   const size_t room = std::min<size_t>(workspace, AMS_KV_WORKSPACE_BYTES);
-  const int64_t fit = std::max<int64_t>((p.tile ? 1 : stream_groups(c->head_dim, p.qt)) * kComputeUnits / c->kv_heads, 1);
+  const int64_t fit = std::max<int64_t>((p.tile ? tile_groups(c->head_dim, p.waves) : stream_groups(c->head_dim, p.qt)) * kComputeUnits / c->kv_heads, 1);
   p.shares = std::min(std::min(fit, p.row_tiles * kMaxParts), room < kCountBytes ? 0 : (int64_t)((room - kCountBytes) / part / 2));
   // tiles of many rows are cut only where there are too few of them: their parts are large
   if (p.tile && p.row_tiles * 2 > fit) p.shares = 0;
@@ -54,7 +59,7 @@ int ams_kv_attention_workspace_bytes(const ams_kv_cache* cache, int64_t rows, in
   if (!bytes) return AMS_ERR_NULL;
   if (const int rc = make_view(cache, rows, &v); rc != AMS_OK) return rc;
   if (heads < 1 || heads % cache->kv_heads || heads > AMS_KV_MAX_HEADS) return AMS_ERR_SHAPE;
-  *bytes = make_plan(cache, rows, heads, max_q_len, SIZE_MAX).workspace;
+  *bytes = make_plan(cache, rows, heads, max_q_len, 0, SIZE_MAX).workspace;
   return AMS_OK;
 }
 
@@ -75,12 +80,12 @@ int ams_kv_attention(const ams_kv_cache* cache, const uint16_t* Q, uint16_t* O, 
   a.group = heads / cache->kv_heads, a.by_group = divisor((uint32_t)a.group);
   a.causal = causal != 0, a.window = (int)std::min<int64_t>(window, 0x3FFFFFFF);
   a.vec = aligned(Q, 16) && aligned(O, 8) && (q_stride | q_head_stride) % 8 == 0 && (o_stride | o_head_stride) % 4 == 0;
-  const Plan p = make_plan(cache, rows, heads, max_q_len, workspace ? workspace_bytes : 0);
+  const Plan p = make_plan(cache, rows, heads, max_q_len, window, workspace ? workspace_bytes : 0);
   a.shares = (int)p.shares, a.cut = p.cut, a.part_rows = p.part_rows;
   const int64_t grid = p.shares * cache->kv_heads;
   if (grid > 0x7FFFFFFF) return AMS_ERR_SHAPE;
   if (p.tile)
-    launch_tile(a, cache->head_dim, cache->scale_group, (unsigned)grid, (hipStream_t)stream);
+    launch_tile(a, cache->head_dim, cache->scale_group, p.waves, (unsigned)grid, (hipStream_t)stream);
   else
     launch_stream(a, cache->head_dim, cache->scale_group, p.qt, (unsigned)grid, (hipStream_t)stream);
   return hipGetLastError() == hipSuccess ? AMS_OK : AMS_ERR_LAUNCH;

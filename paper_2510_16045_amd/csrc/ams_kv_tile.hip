@@ -105,9 +105,9 @@ struct Job {
   }
 };
 
-template <int D, int G>
-__global__ __launch_bounds__(64 * tile_waves(D), D == 256 ? 1 : 2) void tile_kernel(AttentionArgs a) {
-  constexpr int WAVES = tile_waves(D), ROWS = 32 * WAVES, RUNS = D / G, KF = D / 16, DT = D / 32, JOBS = 2 * kBlockTiles / WAVES;
+template <int D, int G, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void tile_kernel(AttentionArgs a) {
+  constexpr int ROWS = 32 * WAVES, RUNS = D / G, KF = D / 16, DT = D / 32, JOBS = 2 * kBlockTiles / WAVES;
   const int wave = uniform((int)threadIdx.x >> 6), lane = lane_id(), h = lane >> 5, col = lane & 31;
   const int share = (int)a.v.heads.quotient(blockIdx.x), head = blockIdx.x - share * a.v.kv_heads;
   __shared__ Block<D> blocks[2];
@@ -323,13 +323,19 @@ __global__ __launch_bounds__(64 * tile_waves(D), D == 256 ? 1 : 2) void tile_ker
       pending++;
     }
   }
-  join_pending<D, 64 * WAVES>(a, pending, left_first, left_last, left, head, (float*)blocks, all_there);
+  join_pending<D, 64 * WAVES, 4, 4>(a, pending, left_first, left_last, left, head, (float*)blocks, all_there);
 }
 
-void launch_tile(const AttentionArgs& a, int head_dim, int scale_group, unsigned grid, hipStream_t stream) {
+void launch_tile(const AttentionArgs& a, int head_dim, int scale_group, int waves, unsigned grid, hipStream_t stream) {
   dispatch(head_dim, scale_group, [&](auto d, auto g) {
     constexpr int D = decltype(d)::value, G = decltype(g)::value;
-    hipLaunchKernelGGL((tile_kernel<D, G>), dim3(grid), dim3(64 * tile_waves(D)), 0, stream, a);
+    if constexpr (D < 256) {
+      if (waves == 8) {
+        hipLaunchKernelGGL((tile_kernel<D, G, 8>), dim3(grid), dim3(512), 0, stream, a);
+        return;
+      }
+    }
+    hipLaunchKernelGGL((tile_kernel<D, G, 4>), dim3(grid), dim3(256), 0, stream, a);
   });
 }
 
