@@ -259,7 +259,6 @@ __device__ __forceinline__ void join_pending(const AttentionArgs& a, int pending
 // Wavefronts of a workgroup, and workgroups of a compute unit: what the registers allow.
 constexpr int stream_waves(int, int) { return 4; }
 constexpr int stream_groups(int d, int qt) { return d * qt <= 128 ? 3 : d * qt < 512 ? 2 : 1; }
-constexpr int tile_groups(int d, int waves) { return d == 256 || waves == 8 ? 1 : 2; }
 void launch_stream(const AttentionArgs& a, int head_dim, int scale_group, int qt, unsigned grid, hipStream_t stream);
 void launch_tile(const AttentionArgs& a, int head_dim, int scale_group, int waves, unsigned grid, hipStream_t stream);  // 8 only up to D = 128
 

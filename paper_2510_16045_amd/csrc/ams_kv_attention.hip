@@ -10,6 +10,7 @@ namespace ams_kv {
 // ---- launch ------------------------------------------------------------------------------------------
 constexpr int kComputeUnits = 256;
 constexpr int kStreamRows = 64;   // up to so many rows of a kv head stream_kernel takes
+constexpr int kFewTiles = 160;    // tiles of 128 rows: with fewer the chip is not full, and stream_kernel, which shares long keys out, is faster
 constexpr int kLongKeys = 4096;   // keys from which on tiles of 256 rows are the faster ones, where they fill the chip
 constexpr size_t kCountBytes = 64 * 1024;  // of a workspace: counts of any call (kv_heads x shares of them), at its front
 static_assert(4 * kComputeUnits * sizeof(uint32_t) <= kCountBytes && AMS_KV_MAX_HEADS * sizeof(uint32_t) <= kCountBytes, "one for each share of each head");
@@ -27,22 +28,21 @@ Plan make_plan(const ams_kv_cache* c, int64_t rows, int heads, int64_t max_q_len
   Plan p;
   const int R = heads / c->kv_heads;
   const int64_t most = (c->q_starts ? std::min(max_q_len > 0 ? max_q_len : rows, rows) : 1) * R;
-  p.tile = most > kStreamRows;
   const int64_t capacity = (int64_t)c->table_width * c->page_size, keys = window > 0 ? std::min(window, capacity) : capacity;
   p.qt = most <= 16 ? 1 : most <= 32 || c->head_dim == 256 ? 2 : 4;
+  const int64_t tiles = rows * R / 128 * c->kv_heads;
+  p.tile = most > kStreamRows && (tiles >= kFewTiles || keys <= kUncutSteps * kStep);
   p.waves = 4;
-  if (p.tile && c->head_dim < 256 && (rows * R / 256 + c->batch) * c->kv_heads >= kComputeUnits && keys >= kLongKeys) p.waves = 8;
+  if (p.tile && c->head_dim < 256 && tiles >= 2 * kComputeUnits && keys >= kLongKeys) p.waves = 8;
   p.rows = p.tile ? 32 * p.waves : 16 * p.qt;
   p.row_tiles = c->q_starts ? rows * R / p.rows + c->batch : c->batch * (int64_t)((R + p.rows - 1) / p.rows);
   const int64_t tile_steps = std::max<int64_t>((capacity + kStep - 1) / kStep, 1);
   p.part_rows = (int)std::min<int64_t>(c->q_starts ? rows * R : R, p.rows);
   const size_t part = (size_t)c->kv_heads * p.part_rows * (c->head_dim + 4) * sizeof(float);
   const size_t room = std::min<size_t>(workspace, AMS_KV_WORKSPACE_BYTES);
-  const int64_t fit = std::max<int64_t>((p.tile ? tile_groups(c->head_dim, p.waves) : stream_groups(c->head_dim, p.qt)) * kComputeUnits / c->kv_heads, 1);
+  const int64_t fit = std::max<int64_t>(stream_groups(c->head_dim, p.qt) * kComputeUnits / c->kv_heads, 1);
   p.shares = std::min(std::min(fit, p.row_tiles * kMaxParts), room < kCountBytes ? 0 : (int64_t)((room - kCountBytes) / part / 2));
-  // tiles of many rows are cut only where there are too few of them: their parts are large
-  if (p.tile && p.row_tiles * 2 > fit) p.shares = 0;
-  p.cut = p.shares > 1 && tile_steps > kUncutSteps && p.row_tiles * (tile_steps + kTileSteps) <= 0x7FFFFFFF;
+  p.cut = !p.tile && p.shares > 1 && tile_steps > kUncutSteps && p.row_tiles * (tile_steps + kTileSteps) <= 0x7FFFFFFF;
   p.workspace = p.cut ? kCountBytes + 2 * (size_t)p.shares * part : 0;
   if (!p.cut) p.shares = p.row_tiles;
   return p;

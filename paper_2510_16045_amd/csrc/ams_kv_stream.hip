@@ -338,7 +338,7 @@ __global__ __launch_bounds__(64 * stream_waves(D, QT), stream_groups(D, QT) * st
     }
     __syncthreads();  // what the tile left in LDS has been read
   }
-  join_pending<D, 64 * kStreamWaves, 1, 8>(a, pending, left_first, left_last, left, head, (float*)shared, all_there);
+  join_pending<D, 64 * kStreamWaves, QT == 1 ? 1 : 4, QT == 1 ? 8 : 4>(a, pending, left_first, left_last, left, head, (float*)shared, all_there);
 }
 
 void launch_stream(const AttentionArgs& a, int head_dim, int scale_group, int qt, unsigned grid, hipStream_t stream) {

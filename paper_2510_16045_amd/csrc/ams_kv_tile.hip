@@ -112,32 +112,17 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void tile_kernel(Atte
   const int share = (int)a.v.heads.quotient(blockIdx.x), head = blockIdx.x - share * a.v.kv_heads;
   __shared__ Block<D> blocks[2];
   __shared__ Notes<RUNS> notes[2];
-  __shared__ bool all_there[2];
-
   const Extent first_64 = extent_of<ROWS>(a, lane);
-  const Split split = split_of<ROWS>(a, first_64);
-  uint32_t now = share * split.per, stop = min(now + split.per, split.total);
-  if (!split.cut && now < split.total) {  // the tiles with the most keys are a sequence's last: they go first
-    now = split.total - min(now + split.per, split.total);
-    stop = min(now + split.per, split.total);
-  }
-  const __amdgpu_buffer_rsrc_t left = __builtin_amdgcn_make_buffer_rsrc((void*)(a.parts + (int64_t)uniform(head) * 2 * a.shares * a.part_rows * (D + 4)), 0,
-                                                                        a.cut ? 2 * a.shares * a.part_rows * (D + 4) * 4 : 0, 0x00020000);  // this head's parts
+  const Split split = split_of<ROWS>(a, first_64);  // a tile each
   Place place;
-  Pending left_first = {}, left_last = {};
-  int pending = 0;
-  while (now < stop && place_of<ROWS>(a, first_64, split.cut, now, &place)) {
+  // the tiles with the most keys are a sequence's last: they go first
+  if ((uint32_t)share < split.total && place_of<ROWS>(a, first_64, false, split.total - 1 - share, &place)) {
     const Extent& e = place.e;
     const int rows = e.n * a.group, tile_row = place.row_tile * ROWS, row0 = tile_row + 32 * wave;
-    const uint32_t then = min(place.first + place.cost, stop);
-    const int begin_step = split.cut ? max((int)(now - place.first) - kTileSteps, 0) : 0, end_step = split.cut ? (int)(then - place.first) - kTileSteps : e.steps;
-    now = then;
-    if (end_step <= 0) break;  // the tile begins in the next share
-    const bool alone = begin_step == 0 && end_step == e.steps;
     auto position = [&](int r) { return e.len - e.n + (int)a.by_group.quotient((uint32_t)r); };
-    // the keys of the share that some row of the tile sees
-    const int key_from = uniform(max(e.lo + begin_step * kStep, key_begin(a, position(tile_row)) & ~(kStep - 1)));
-    const int key_to = uniform(min(e.lo + end_step * kStep, key_end(a, e.len, position(min(tile_row + ROWS, rows) - 1))));
+    // the keys that some row of the tile sees, from a cache tile on
+    const int key_from = uniform(key_begin(a, position(tile_row)) & ~(kTile - 1));
+    const int key_to = uniform(key_end(a, e.len, position(min(tile_row + ROWS, rows) - 1)));
     const int n_blocks = max((key_to - key_from + kBlock - 1) / kBlock, 0);
     // of those the ones that every row and that no row of the wavefront sees
     const bool idle = row0 >= rows;
@@ -295,35 +280,15 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void tile_kernel(Atte
     }
 
     l += __shfl_xor(l, 32, 64);
-    const int part = (2 * share + (begin_step == 0)) * a.part_rows + 32 * wave + col;
     if (r < rows) {
-      const float scale = alone ? (l > 0 || l != l ? 1.0f / l : 0.0f) : 1.0f;
+      const float scale = l > 0 || l != l ? 1.0f / l : 0.0f;
 #pragma unroll
       for (int d = 0; d < DT; d++)
 #pragma unroll
-        for (int i = 0; i < 16; i += 4) {
-          const f4 x = f4{o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]} * scale;
-          const int channel = 32 * d + 2 * i + 4 * h;
-          if (alone)
-            store_out(a, e.start, head, r, channel, x);
-          else
-            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4, x), left, (part * (D + 4) + 4 + channel) * 4, 0, kDeviceScope);
-        }
-      if (h == 0) {
-        if (alone)
-          store_lse(a, e.start, head, r, m, l);
-        else
-          __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u2, f2{m, l}), left, part * (D + 4) * 4, 0, kDeviceScope);
-      }
-    }
-    if (!alone) {
-      const int first = (int)((place.first + kTileSteps) / split.per), last = (int)((place.first + kTileSteps + e.steps - 1) / split.per);
-      left_last = Pending{e.start, tile_row, min(rows - tile_row, ROWS), first, last - first + 1};
-      if (pending == 0) left_first = left_last;
-      pending++;
+        for (int i = 0; i < 16; i += 4) store_out(a, e.start, head, r, 32 * d + 2 * i + 4 * h, f4{o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]} * scale);
+      if (h == 0) store_lse(a, e.start, head, r, m, l);
     }
   }
-  join_pending<D, 64 * WAVES, 4, 4>(a, pending, left_first, left_last, left, head, (float*)blocks, all_there);
 }
 
 void launch_tile(const AttentionArgs& a, int head_dim, int scale_group, int waves, unsigned grid, hipStream_t stream) {
