@@ -256,10 +256,9 @@ __device__ __forceinline__ void join_pending(const AttentionArgs& a, int pending
 }
 
 // ---- the kernels' launches -----------------------------------------------------------------------------
-// Wavefronts of a workgroup, and workgroups of a compute unit: what the registers allow.
-constexpr int stream_waves(int, int) { return 4; }
-constexpr int stream_groups(int d, int qt) { return d * qt <= 128 ? 3 : d * qt < 512 ? 2 : 1; }
-void launch_stream(const AttentionArgs& a, int head_dim, int scale_group, int qt, unsigned grid, hipStream_t stream);
+// Workgroups of a compute unit: what the registers allow.
+constexpr int stream_groups(int d, int qt, int waves) { return waves == 8 ? 1 : d * qt <= 128 ? 3 : d * qt < 512 ? 2 : 1; }
+void launch_stream(const AttentionArgs& a, int head_dim, int scale_group, int qt, int waves, unsigned grid, hipStream_t stream);  // 8 only for qt = 1, up to D = 128
 void launch_tile(const AttentionArgs& a, int head_dim, int scale_group, int waves, unsigned grid, hipStream_t stream);  // 8 only up to D = 128
 
 }  // namespace ams_kv

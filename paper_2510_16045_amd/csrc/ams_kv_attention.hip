@@ -11,6 +11,8 @@ namespace ams_kv {
 constexpr int kComputeUnits = 256;
 constexpr int kStreamRows = 64;   // up to so many rows of a kv head stream_kernel takes
 constexpr int kFewTiles = 160;    // tiles of 128 rows: with fewer the chip is not full, and stream_kernel, which shares long keys out, is faster
+constexpr int kLoneTiles = 64;    // of stream_kernel: so many or fewer have eight wavefronts (one sequence of 131071, 8 heads: 42 -> 38 us)
+constexpr int kShortKeys = 4096;  // so have up to 256 tiles with so many keys at most (64 x 1000, 4 heads: 14.4 -> 12.1 us; 32 ragged x 8192, 8 heads: 42 -> 46)
 constexpr int kLongKeys = 4096;   // keys from which on tiles of 256 rows are the faster ones, where they fill the chip
 constexpr size_t kCountBytes = 64 * 1024;  // of a workspace: counts of any call (kv_heads x shares of them), at its front
 static_assert(4 * kComputeUnits * sizeof(uint32_t) <= kCountBytes && AMS_KV_MAX_HEADS * sizeof(uint32_t) <= kCountBytes, "one for each share of each head");
@@ -36,11 +38,13 @@ Plan make_plan(const ams_kv_cache* c, int64_t rows, int heads, int64_t max_q_len
   if (p.tile && c->head_dim < 256 && tiles >= 2 * kComputeUnits && keys >= kLongKeys) p.waves = 8;
   p.rows = p.tile ? 32 * p.waves : 16 * p.qt;
   p.row_tiles = c->q_starts ? rows * R / p.rows + c->batch : c->batch * (int64_t)((R + p.rows - 1) / p.rows);
+  // few tiles, or short ones of which no compute unit has two: eight wavefronts to a tile
+  if (!p.tile && p.qt == 1 && c->head_dim < 256 && (p.row_tiles * c->kv_heads <= kLoneTiles || (p.row_tiles * c->kv_heads <= kComputeUnits && capacity <= kShortKeys))) p.waves = 8;
   const int64_t tile_steps = std::max<int64_t>((capacity + kStep - 1) / kStep, 1);
   p.part_rows = (int)std::min<int64_t>(c->q_starts ? rows * R : R, p.rows);
   const size_t part = (size_t)c->kv_heads * p.part_rows * (c->head_dim + 4) * sizeof(float);
   const size_t room = std::min<size_t>(workspace, AMS_KV_WORKSPACE_BYTES);
-  const int64_t fit = std::max<int64_t>(stream_groups(c->head_dim, p.qt) * kComputeUnits / c->kv_heads, 1);
+  const int64_t fit = std::max<int64_t>(stream_groups(c->head_dim, p.qt, p.waves) * kComputeUnits / c->kv_heads, 1);
   p.shares = std::min(std::min(fit, p.row_tiles * kMaxParts), room < kCountBytes ? 0 : (int64_t)((room - kCountBytes) / part / 2));
   p.cut = !p.tile && p.shares > 1 && tile_steps > kUncutSteps && p.row_tiles * (tile_steps + kTileSteps) <= 0x7FFFFFFF;
   p.workspace = p.cut ? kCountBytes + 2 * (size_t)p.shares * part : 0;
@@ -87,7 +91,7 @@ int ams_kv_attention(const ams_kv_cache* cache, const uint16_t* Q, uint16_t* O, 
   if (p.tile)
     launch_tile(a, cache->head_dim, cache->scale_group, p.waves, (unsigned)grid, (hipStream_t)stream);
   else
-    launch_stream(a, cache->head_dim, cache->scale_group, p.qt, (unsigned)grid, (hipStream_t)stream);
+    launch_stream(a, cache->head_dim, cache->scale_group, p.qt, p.waves, (unsigned)grid, (hipStream_t)stream);
   return hipGetLastError() == hipSuccess ? AMS_OK : AMS_ERR_LAUNCH;
 }
 

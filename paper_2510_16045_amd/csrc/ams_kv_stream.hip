@@ -99,16 +99,16 @@ __device__ __forceinline__ void nan_of_seen_keys(uint8_t* stage, int lane, int f
   wave_sync();
 }
 
-template <int D, int G, int QT>
-__global__ __launch_bounds__(64 * stream_waves(D, QT), stream_groups(D, QT) * stream_waves(D, QT) / 4) void stream_kernel(AttentionArgs a) {
-  constexpr int kStreamWaves = stream_waves(D, QT), ROWS = 16 * QT, RUNS = D / G, DT = D / 16, KB = D / 32, AT_ONCE = DT < 8 ? DT : 8;
+template <int D, int G, int QT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, stream_groups(D, QT, WAVES) * WAVES / 4) void stream_kernel(AttentionArgs a) {
+  constexpr int ROWS = 16 * QT, RUNS = D / G, DT = D / 16, KB = D / 32, AT_ONCE = DT < 8 ? DT : 8;
   const int wave = uniform((int)threadIdx.x >> 6), lane = lane_id();
   const int share = (int)a.v.heads.quotient(blockIdx.x), head = blockIdx.x - share * a.v.kv_heads;
   // While keys are read: the rows of q as the matrix instructions take them, and V's scales of each wavefront's step.  Then the
   // wavefronts' results, eight d-tiles of a column tile at a time.
-  constexpr int Q_BYTES = KB * QT * 1024, STAGE = 64 * RUNS, PARTS = kStreamWaves * AT_ONCE * 1024;
-  __shared__ __align__(16) uint8_t shared[Q_BYTES + kStreamWaves * STAGE > PARTS ? Q_BYTES + kStreamWaves * STAGE : PARTS];
-  __shared__ float tops[kStreamWaves][ROWS], sums[kStreamWaves][ROWS];
+  constexpr int Q_BYTES = KB * QT * 1024, STAGE = 64 * RUNS, PARTS = WAVES * AT_ONCE * 1024;
+  __shared__ __align__(16) uint8_t shared[Q_BYTES + WAVES * STAGE > PARTS ? Q_BYTES + WAVES * STAGE : PARTS];
+  __shared__ float tops[WAVES][ROWS], sums[WAVES][ROWS];
   __shared__ bool all_there[2];
   h8* const q_rows = (h8*)shared;
   uint8_t* const stage = shared + Q_BYTES + wave * STAGE;
@@ -138,7 +138,7 @@ __global__ __launch_bounds__(64 * stream_waves(D, QT), stream_groups(D, QT) * st
     const int to = uniform(min(e.lo / kStep + end_step, (key_end(a, e.len, p_last) + kStep - 1) / kStep));
     const int whole_begin = uniform(key_begin(a, p_last)), whole_end = uniform(key_end(a, e.len, p_first));
     Pages pages;
-    pages.look_up(a, place.b, from + wave + kStreamWaves * hidden(lane), to);
+    pages.look_up(a, place.b, from + wave + WAVES * hidden(lane), to);
     // the tile's rows: a lane has one of each column tile
     const int load_lane = hidden(lane);
 #pragma unroll
@@ -146,9 +146,9 @@ __global__ __launch_bounds__(64 * stream_waves(D, QT), stream_groups(D, QT) * st
       const int r = row0 + 16 * t + (load_lane & 15), token = (int)a.by_group.quotient((uint32_t)r);
       const uint16_t* src = a.q + (int64_t)(e.start + token) * a.q_stride + (int64_t)(head * a.group + r - token * a.group) * a.q_head + 8 * (load_lane >> 4);
 #pragma unroll
-      for (int i0 = 0; i0 < KB; i0 += kStreamWaves) {
+      for (int i0 = 0; i0 < KB; i0 += WAVES) {
         const int i = i0 + wave;
-        if (KB < kStreamWaves && i >= KB) break;
+        if (KB < WAVES && i >= KB) break;
         u4 x = {0, 0, 0, 0};
         if (r < rows) x = load_half8(src + 32 * i, a.vec);
         q_rows[(i * QT + t) * 64 + lane] = __builtin_bit_cast(h8, x);
@@ -248,12 +248,12 @@ __global__ __launch_bounds__(64 * stream_waves(D, QT), stream_groups(D, QT) * st
         scores(k, s);
         const bool held[2] = {of_lane(pages.number[0], at) >= 0, of_lane(pages.number[1], at) >= 0};
         const bool whole = step * kStep >= whole_begin && (step + 1) * kStep <= whole_end && held[0] && held[1];  // every row sees every key
-        const bool more = step + kStreamWaves < to;
+        const bool more = step + WAVES < to;
         if (more && ++at == 64) {
           at = 0;
-          pages.look_up(a, place.b, step + kStreamWaves + kStreamWaves * hidden(lane), to);
+          pages.look_up(a, place.b, step + WAVES + WAVES * hidden(lane), to);
         }
-        const int next = more ? step + kStreamWaves : step;
+        const int next = more ? step + WAVES : step;
         const Tile t0(a, pages, head, next, 0, at), t1(a, pages, head, next, 1, at);
         k.load(a, t0, 0, lane), k.load(a, t1, 1, lane);
         int begin[QT], end[QT];
@@ -293,7 +293,7 @@ __global__ __launch_bounds__(64 * stream_waves(D, QT), stream_groups(D, QT) * st
 #pragma unroll
     for (int t = 0; t < QT; t++) {
       const int r = row0 + 16 * t + col;
-      float top = -INFINITY, sum = 0, by[kStreamWaves], scale = 0;
+      float top = -INFINITY, sum = 0, by[WAVES], scale = 0;
 #pragma unroll
       for (int d0 = 0; d0 < DT; d0 += AT_ONCE) {
         __syncthreads();
@@ -302,19 +302,19 @@ __global__ __launch_bounds__(64 * stream_waves(D, QT), stream_groups(D, QT) * st
         __syncthreads();
         if (d0 == 0) {
 #pragma unroll
-          for (int w = 0; w < kStreamWaves; w++) top = fmaxf(top, tops[w][16 * t + col]);
+          for (int w = 0; w < WAVES; w++) top = fmaxf(top, tops[w][16 * t + col]);
 #pragma unroll
-          for (int w = 0; w < kStreamWaves; w++) {
+          for (int w = 0; w < WAVES; w++) {
             const float mine = tops[w][16 * t + col];
             by[w] = mine == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mine - top);
             sum += sums[w][16 * t + col] * by[w];
           }
           scale = alone ? (sum > 0 || sum != sum ? 1.0f / sum : 0.0f) : 1.0f;
         }
-        for (int d = wave; d < AT_ONCE; d += kStreamWaves) {
+        for (int d = wave; d < AT_ONCE; d += WAVES) {
           f4 x = {0, 0, 0, 0};
 #pragma unroll
-          for (int w = 0; w < kStreamWaves; w++) x += parts[(w * AT_ONCE + d) * 64 + done] * by[w];
+          for (int w = 0; w < WAVES; w++) x += parts[(w * AT_ONCE + d) * 64 + done] * by[w];
           if (r >= rows) continue;
           const int channel = 16 * (d0 + d) + 4 * g;
           if (alone)
@@ -338,19 +338,19 @@ __global__ __launch_bounds__(64 * stream_waves(D, QT), stream_groups(D, QT) * st
     }
     __syncthreads();  // what the tile left in LDS has been read
   }
-  join_pending<D, 64 * kStreamWaves, QT == 1 ? 1 : 4, QT == 1 ? 8 : 4>(a, pending, left_first, left_last, left, head, (float*)shared, all_there);
+  join_pending<D, 64 * WAVES, QT == 1 ? 1 : 4, QT == 1 ? 8 : 4>(a, pending, left_first, left_last, left, head, (float*)shared, all_there);
 }
 
-void launch_stream(const AttentionArgs& a, int head_dim, int scale_group, int qt, unsigned grid, hipStream_t stream) {
+void launch_stream(const AttentionArgs& a, int head_dim, int scale_group, int qt, int waves, unsigned grid, hipStream_t stream) {
   dispatch(head_dim, scale_group, [&](auto d, auto g) {
     constexpr int D = decltype(d)::value, G = decltype(g)::value;
-    auto launch = [&](auto kernel, int qt) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * stream_waves(D, qt)), 0, stream, a); };
-    switch (qt) {
-      case 1: launch(stream_kernel<D, G, 1>, 1); break;
-      case 2: launch(stream_kernel<D, G, 2>, 2); break;
-      default:
-        if constexpr (D < 256) launch(stream_kernel<D, G, 4>, 4);  // 256 accumulators do not fit beside the rows
+    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * waves), 0, stream, a); };
+    if constexpr (D < 256) {
+      if (waves == 8) return launch(stream_kernel<D, G, 1, 8>);
+      if (qt == 4) return launch(stream_kernel<D, G, 4, 4>);  // 256 accumulators do not fit beside the rows
     }
+    if (qt == 1) return launch(stream_kernel<D, G, 1, 4>);
+    launch(stream_kernel<D, G, 2, 4>);
   });
 }
 
