@@ -66,8 +66,8 @@ const char* ams_strerror(int code);
 
 /*
  * Optional one-time set-up for the current device: checks that it is a gfx950 (else
- * AMS_ERR_DEVICE) and raises the dynamic-LDS limit of every Linear kernel (they use up to
- * 160 KiB).  Every device entry point does the same for itself on its first call, so this
+ * AMS_ERR_DEVICE), raises the dynamic-LDS limit of every Linear kernel (they use up to
+ * 160 KiB) and loads those of the KV cache.  Every device entry point does the same for itself on its first call, so this
  * is only REQUIRED before the first call of an entry point happens inside a HIP stream
  * capture (function attributes should not be changed while capturing).  Allocates nothing,
  * enqueues nothing; may be called any number of times, once per device that is used (the first call

@@ -38,17 +38,16 @@ def attention(q, k, v, scale, causal=True, window=0):
         seen &= key > position - window
     out, size = np.zeros(q.shape), np.zeros(q.shape)
     lse = np.full((n, heads), -np.inf)
+    some = seen.any(1)
+    if not some.any():
+        return out, lse, size
     for h in range(heads):
         kh, vh = k[:, h * kv_heads // heads], v[:, h * kv_heads // heads]
-        for i in range(n):
-            at = seen[i]
-            if not at.any():
-                continue
-            s = kh[at] @ q[i, h].astype(np.float64) * scale
-            top = s.max()
-            p = np.exp(s - top)
-            total = p.sum()
-            out[i, h] = p @ vh[at] / total
-            size[i, h] = p @ np.abs(vh[at]) / total
-            lse[i, h] = top + np.log(total)
+        s = np.where(seen, q[:, h].astype(np.float64) @ kh.T * scale, -np.inf)[some]
+        top = s.max(-1, keepdims=True)
+        p = np.exp(s - top)
+        total = p.sum(-1, keepdims=True)
+        out[some, h] = p @ vh / total
+        size[some, h] = p @ np.abs(vh) / total
+        lse[some, h] = (top + np.log(total))[:, 0]
     return out, lse, size

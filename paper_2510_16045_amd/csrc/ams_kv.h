@@ -224,6 +224,14 @@ int make_view(const ams_kv_cache* c, int64_t rows, View* v);
 bool aligned(const void* p, int bytes);
 // AMS_OK on a gfx950 (ams_kernels.hip).
 int device_status();
+// Each file's kernels on the current device, so that a first call may be captured: one of a file brings in all of them.
+inline bool loaded(const void* kernel) {
+  hipFuncAttributes attributes;
+  return hipFuncGetAttributes(&attributes, kernel) == hipSuccess;
+}
+bool load_cache();
+bool load_stream();
+bool load_tile();
 
 }  // namespace ams_kv
 #endif

@@ -269,6 +269,8 @@ int run_rows(const ams_kv_cache* cache, int64_t rows, uint16_t* k, uint16_t* v, 
   return hipGetLastError() == hipSuccess ? AMS_OK : AMS_ERR_LAUNCH;
 }
 
+bool load_cache() { return loaded((const void*)write_kernel<64, 32>); }
+
 bool aligned(const void* p, int bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
 
 static bool sizes_ok(int kv_heads, int head_dim, int page_size, int scale_group) {

@@ -129,8 +129,8 @@ __global__ __launch_bounds__(64 * WAVES, stream_groups(D, QT, WAVES) * WAVES / 4
     // the share's steps of the tile that some row sees, and the keys that every row sees
     const uint32_t then = min(place.first + place.cost, stop);
     const int begin_step = split.cut ? max((int)(now - place.first) - kTileSteps, 0) : 0, end_step = split.cut ? (int)(then - place.first) - kTileSteps : e.steps;
+    if (end_step <= 0 || then <= now) break;  // the tile begins in the next share (and starts that are not ascending end somewhere)
     now = then;
-    if (end_step <= 0) break;  // the tile begins in the next share
     const bool alone = begin_step == 0 && end_step == e.steps;
     const int last_row = min(row0 + ROWS, rows) - 1;
     const int p_first = e.len - e.n + (int)a.by_group.quotient((uint32_t)row0), p_last = e.len - e.n + (int)a.by_group.quotient((uint32_t)last_row);
@@ -331,7 +331,7 @@ __global__ __launch_bounds__(64 * WAVES, stream_groups(D, QT, WAVES) * WAVES / 4
       }
     }
     if (!alone) {
-      const int first = (int)((place.first + kTileSteps) / split.per), last = (int)((place.first + kTileSteps + e.steps - 1) / split.per);
+      const int first = min((int)((place.first + kTileSteps) / split.per), a.shares - 1), last = (int)((place.first + kTileSteps + e.steps - 1) / split.per);
       left_first = pending == 0 ? Pending{e.start, row0, min(rows - row0, ROWS), first, last - first + 1} : left_first;
       left_last = Pending{e.start, row0, min(rows - row0, ROWS), first, last - first + 1};
       pending++;
@@ -340,6 +340,8 @@ __global__ __launch_bounds__(64 * WAVES, stream_groups(D, QT, WAVES) * WAVES / 4
   }
   join_pending<D, 64 * WAVES, QT == 1 ? 1 : 4, QT == 1 ? 8 : 4>(a, pending, left_first, left_last, left, head, (float*)shared, all_there);
 }
+
+bool load_stream() { return loaded((const void*)stream_kernel<64, 32, 1, 4>); }
 
 void launch_stream(const AttentionArgs& a, int head_dim, int scale_group, int qt, int waves, unsigned grid, hipStream_t stream) {
   dispatch(head_dim, scale_group, [&](auto d, auto g) {

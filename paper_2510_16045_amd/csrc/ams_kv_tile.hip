@@ -291,6 +291,8 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void tile_kernel(Atte
   }
 }
 
+bool load_tile() { return loaded((const void*)tile_kernel<64, 32, 4>); }
+
 void launch_tile(const AttentionArgs& a, int head_dim, int scale_group, int waves, unsigned grid, hipStream_t stream) {
   dispatch(head_dim, scale_group, [&](auto d, auto g) {
     constexpr int D = decltype(d)::value, G = decltype(g)::value;

@@ -298,3 +298,53 @@ def test_a_captured_step_follows_the_lengths():
         torch.cuda.synchronize()
         assert torch.equal(out, want) and torch.equal(cache, eager_cache), i
         assert bool(out.any())
+
+
+def test_a_prompt_that_fills_the_chip():
+    # 64 heads of 1024 rows, and a table for more than 4096 keys: tiles of 256 rows
+    c = Case([1100], [1024], heads=64, kv_heads=64, D=64, G=64, page=64, spare=60)
+    assert c.table.shape[1] * 64 >= 4096
+    c.check()
+
+
+@pytest.mark.parametrize("D,G", [(64, 32), (128, 64)])
+def test_many_tiles_that_are_shared_out(D, G):
+    # 80 tiles and a table for more than 4096 keys: four wavefronts to a tile, shares that begin and end inside of tiles
+    lens = [3000, 1, 0, 40, 2500, 999, 17, 1200, 33, 1600]
+    Case(lens, [1] * 10, heads=16, kv_heads=8, D=D, G=G, page=64, spare=30).check()
+    Case(lens, [1] * 10, heads=16, kv_heads=8, D=D, G=G, page=64, spare=30, window=1500).check()
+
+
+def test_prompts_of_more_sequences_than_a_wavefront_has_lanes():
+    rng = np.random.default_rng(10)
+    lens = [int(n) for n in rng.integers(0, 50, 90)]
+    lens[75] = 400
+    counts = [min(n, int(k)) for n, k in zip(lens, rng.integers(0, 40, 90))]
+    counts[75] = 390
+    Case(lens, counts, heads=2, kv_heads=1, D=64, G=32, page=16).check(max_q_len=390)
+
+
+def test_pages_that_a_prompt_does_not_find():
+    c = Case([300], [200], heads=2, kv_heads=1, page=16)
+    c.table[0, 3] = -1
+    c.table[0, 16] = 1 << 20
+    out = host(c.run())
+    k, v = (O.held(x, 32) for x in c.seqs[0])
+    there = np.ones(300, dtype=bool)
+    there[48:64] = there[256:272] = False
+    for i in range(200):
+        at = there & (np.arange(300) <= 100 + i)
+        want, _, size = O.attention(c.q[i : i + 1], k[at], v[at], c.D**-0.5, causal=False)
+        ok, worst = near(out[i : i + 1], want, size, 300)
+        assert ok, (i, worst)
+
+
+def test_row_starts_that_make_no_sense_touch_nothing_else():
+    c = Case([60, 40, 20], [3, 2, 4], heads=2, kv_heads=1)
+    q = dev(c.q)
+    for starts in ([0, 100, 50, 9], [5, 2, 8, -4], [1 << 30, 0, 0, 0], [-5, -5, 3, 1 << 30]):
+        for hint in (None, 100):
+            store = torch.full((c.q.shape[0] + 2, 2, 128), 7.0, dtype=torch.float16, device="cuda")
+            ams.ams_kv_attention(q, c.cache, c.table, c.kv_lens, c.G, q_starts=dev(np.array(starts, dtype=np.int32)), max_q_len=hint, workspace=WORKSPACE, out=store[1:-1])
+            assert bool((store[0] == 7).all()) and bool((store[-1] == 7).all())
+            assert not bool(torch.isnan(store).any())
