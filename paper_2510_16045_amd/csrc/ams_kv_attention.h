@@ -18,7 +18,6 @@
 
 namespace ams_kv {
 
-
 constexpr int kDeviceScope = 16;  // cache policy (sc1) of a buffer load or store that the whole device sees
 constexpr int kStep = 32;         // keys of a wavefront's step
 constexpr int kMinShare = 16;     // steps of a share: four for each wavefront
@@ -63,19 +62,32 @@ __device__ __forceinline__ Extent extent_of(const AttentionArgs& a, int b) {
   return e;
 }
 
-__device__ __forceinline__ uint32_t wave_sum(uint32_t x) {
-#pragma unroll
-  for (int i = 1; i < 64; i *= 2) x += (uint32_t)__shfl_xor((int)x, i, 64);
-  return (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
-}
-__device__ __forceinline__ int wave_prefix(int x) {  // inclusive
-#pragma unroll
-  for (int i = 1; i < 64; i *= 2) {
-    const int y = __shfl_up(x, i, 64);
-    if (lane_id() >= i) x += y;
-  }
+// Sums over the lanes up to a lane's own: within rows of 16, then the rows'.  Every lane of the wavefront takes part.  Lane patterns of
+// the adds themselves; trips through LDS, six at a time and two times on every workgroup's way to its first load, cost half a
+// microsecond to a microsecond a call.
+__device__ __forceinline__ uint32_t wave_prefix(uint32_t x) {
+  constexpr int kUp = 0x110, kRowEnd = 0x142, kHalfEnd = 0x143;  // n lanes up in a row; the end of the row before; of the first half
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kUp + 1, 0xF, 0xF, false);
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kUp + 2, 0xF, 0xF, false);
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kUp + 4, 0xF, 0xF, false);
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kUp + 8, 0xF, 0xF, false);
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kRowEnd, 0xA, 0xF, false);
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kHalfEnd, 0xC, 0xF, false);
   return x;
 }
+__device__ __forceinline__ uint32_t wave_sum(uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)wave_prefix(x), 63); }
+// A lane's value and that of the lane 32 (16) further, in either order.
+__device__ __forceinline__ f2 with_32(float x) {
+  const auto y = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
+  return f2{__builtin_bit_cast(float, (unsigned)y[0]), __builtin_bit_cast(float, (unsigned)y[1])};
+}
+__device__ __forceinline__ f2 with_16(float x) {
+  const auto y = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
+  return f2{__builtin_bit_cast(float, (unsigned)y[0]), __builtin_bit_cast(float, (unsigned)y[1])};
+}
+__device__ __forceinline__ float larger(f2 x) { return fmaxf(x[0], x[1]); }
+__device__ __forceinline__ float sum_of(f2 x) { return x[0] + x[1]; }
+
 // x, of which the compiler knows nothing: what follows from it is not worked out before it is needed and kept in registers.
 __device__ __forceinline__ int hidden(int x) {
   asm volatile("" : "+v"(x));

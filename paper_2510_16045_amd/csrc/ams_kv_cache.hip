@@ -13,7 +13,7 @@ struct TileRows {
 };
 __device__ __forceinline__ bool tile_rows(const View& v, int item, TileRows* t) {
   auto first_item = [&](int b) { return v.starts ? row_start(v, b) / kTile + 2 * b : b; };
-  const int b = sequence_of(v.batch, item, first_item);
+  const int b = v.starts ? sequence_of(v.batch, item, first_item) : min(item, v.batch - 1);
   const int start = row_start(v, b), n = max(row_start(v, b + 1) - start, 0), len = kv_len(v, b);
   const int p0 = len - n;  // position of the first row
   const int tile = (p0 >> 4) + item - first_item(b);

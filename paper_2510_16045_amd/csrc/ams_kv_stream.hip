@@ -188,8 +188,7 @@ __global__ __launch_bounds__(64 * WAVES, stream_groups(D, QT, WAVES) * WAVES / 4
         top *= a.scale2;
         if (__ballot(top > m[t] + kSlack)) {
           top = fmaxf(top, m[t]);
-          top = fmaxf(top, __shfl_xor(top, 16, 64));
-          top = fmaxf(top, __shfl_xor(top, 32, 64));
+          top = larger(with_32(larger(with_16(top))));
           const float less = top > m[t] ? __builtin_amdgcn_exp2f(m[t] - top) : 1.0f;
           m[t] = top;
           l[t] *= less;
@@ -285,8 +284,7 @@ __global__ __launch_bounds__(64 * WAVES, stream_groups(D, QT, WAVES) * WAVES / 4
     const int done = hidden(lane), g = done >> 4, col = done & 15;
 #pragma unroll
     for (int t = 0; t < QT; t++) {
-      l[t] += __shfl_xor(l[t], 16, 64);
-      l[t] += __shfl_xor(l[t], 32, 64);
+      l[t] = sum_of(with_32(sum_of(with_16(l[t]))));
       if (g == 0) tops[wave][16 * t + col] = m[t], sums[wave][16 * t + col] = l[t];
     }
     const int part = (2 * share + (begin_step == 0)) * a.part_rows;

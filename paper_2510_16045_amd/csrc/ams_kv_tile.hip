@@ -219,7 +219,7 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void tile_kernel(Atte
       top *= a.scale2;
       if (__ballot(top > m + kSlack)) {  // the maximum is raised only where a score passes it by more than the slack
         top = fmaxf(top, m);
-        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        top = larger(with_32(top));
         const float less = top > m ? __builtin_amdgcn_exp2f(m - top) : 1.0f;
         m = top;
         l *= less;
@@ -279,7 +279,7 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void tile_kernel(Atte
       }
     }
 
-    l += __shfl_xor(l, 32, 64);
+    l = sum_of(with_32(l));
     if (r < rows) {
       const float scale = l > 0 || l != l ? 1.0f / l : 0.0f;
 #pragma unroll
