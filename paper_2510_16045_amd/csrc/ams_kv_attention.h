@@ -24,6 +24,8 @@ constexpr int kMinShare = 16;     // steps of a share: four for each wavefront
 constexpr int kTileSteps = 14;    // what it takes to begin a tile and to leave its result, in steps
 constexpr int kUncutSteps = 32;   // a tile of so many is not cut: joining its parts takes longer than its steps
 constexpr int kMaxParts = 64;     // a tile in more parts costs its last workgroup more than the others gain
+constexpr int kNear = 8;          // parts of a tile that are added up first where there are many
+constexpr int kTrips = 2;         // one workgroup adds up all parts of a tile if it waits for them no more than so often
 constexpr float kLift = 8.0f;     // exponents of P are raised by this: below it P keeps fp16's full precision over 2^-22 of the largest
 constexpr float kSlack = 7.0f;    // how far (log2) a score may pass the running maximum before that is raised: 2^(8 + 7) is in fp16
 
@@ -32,7 +34,7 @@ struct AttentionArgs {
   const uint16_t* q;
   uint16_t* out;
   float* lse;
-  uint32_t* counts;  // [kv head][share in which the tile begins]
+  uint32_t* counts;  // [of tiles, of kNear shares of a tile][kv head][share in which they begin]
   float* parts;      // [kv head][2 share + (the tile begins in it)][row of the tile][max, sum, -, -, D values]
   int64_t q_stride, q_head, out_stride, out_head, lse_stride;
   float scale2;  // softmax_scale * log2(e)
@@ -185,23 +187,25 @@ __device__ __forceinline__ void store_lse(const AttentionArgs& a, int start, int
 
 // Adds up the parts of a row tile.  D / 4 lanes take a row, four channels each; of the workgroup's groups of lanes as many take rows
 // as there are (a power of two), U rows each at once, and the others share the parts of a row, P of them at once: U P parts of rows are
-// asked for before the first is used.
-template <int D, int THREADS, int U, int P>
-__device__ __forceinline__ void join_parts(const AttentionArgs& a, const Pending& tile, __amdgpu_buffer_rsrc_t left, int head, float* lds) {
+// asked for before the first is used.  The parts are those of every APARTth share from `from` on; the sum becomes the tile's result, or
+// takes the place of the first of them.
+template <int D, int THREADS, int U, int P, int APART = 1, bool RESULT = true>
+__device__ __forceinline__ void join_parts(const AttentionArgs& a, const Pending& tile, __amdgpu_buffer_rsrc_t left, int head, float* lds, int from, int count) {
   constexpr int LANES = D / 4, GROUPS = THREADS / LANES;
   f4* const xs = (f4*)lds;                // [group][lane]
   f2* const stats = (f2*)(xs + THREADS);  // [group]
   const int group = threadIdx.x / LANES, c = threadIdx.x % LANES;
-  const int rows = tile.rows, first = tile.first, count = tile.count;
+  const int rows = tile.rows;
   int takers = 1;  // groups that take rows
   while (takers < rows && takers < GROUPS) takers *= 2;
   const int sharers = GROUPS / takers, mine = group / takers;
-  auto add = [](float& top, float& sum, f4& x, float part_top, float part_sum, f4 part) {
+  auto place = [&](int s, int i) { return ((2 * (from + s * APART) + (s == 0 && from == tile.first)) * a.part_rows + i) * (D + 4) * 4; };
+  auto add = [](float& top, float& sum, f4& x, float part_top, float part_sum, f4 more) {
     const float most = fmaxf(top, part_top);
     const float less = top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top - most), by = part_top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(part_top - most);
     top = most;
     sum = sum * less + part_sum * by;
-    x = x * less + part * by;
+    x = x * less + more * by;
   };
 #pragma unroll 1
   for (int i0 = 0; i0 < rows; i0 += takers * U) {
@@ -211,22 +215,22 @@ __device__ __forceinline__ void join_parts(const AttentionArgs& a, const Pending
     for (int u = 0; u < U; u++) top[u] = -INFINITY, sum[u] = 0, x[u] = f4{0, 0, 0, 0};
 #pragma unroll 1
     for (int s0 = mine; s0 < count; s0 += sharers * P) {
-      f4 from[U][P];
+      f4 part[U][P];
       f2 stat[U][P];
 #pragma unroll
       for (int u = 0; u < U; u++)
 #pragma unroll
         for (int j = 0; j < P; j++) {
           const int s = s0 + j * sharers, i = i0 + u * takers + group % takers;
-          const int at = s < count && i < rows ? ((2 * (first + s) + (s == 0)) * a.part_rows + i) * (D + 4) * 4 : 0x7FFE0000;  // nothing is read there
-          from[u][j] = __builtin_bit_cast(f4, __builtin_amdgcn_raw_buffer_load_b128(left, at + 16 + 16 * c, 0, kDeviceScope));
+          const int at = s < count && i < rows ? place(s, i) : 0x7FFE0000;  // nothing is read there
+          part[u][j] = __builtin_bit_cast(f4, __builtin_amdgcn_raw_buffer_load_b128(left, at + 16 + 16 * c, 0, kDeviceScope));
           stat[u][j] = __builtin_bit_cast(f2, __builtin_amdgcn_raw_buffer_load_b64(left, at, 0, kDeviceScope));
           if (s >= count) stat[u][j] = f2{-INFINITY, 0};
         }
 #pragma unroll
       for (int u = 0; u < U; u++)
 #pragma unroll
-        for (int j = 0; j < P; j++) add(top[u], sum[u], x[u], stat[u][j][0], stat[u][j][1], from[u][j]);
+        for (int j = 0; j < P; j++) add(top[u], sum[u], x[u], stat[u][j][0], stat[u][j][1], part[u][j]);
     }
     if (sharers > 1) {  // then every row has a taker, in its first turn
       xs[threadIdx.x] = x[0];
@@ -239,37 +243,69 @@ __device__ __forceinline__ void join_parts(const AttentionArgs& a, const Pending
     for (int u = 0; u < U; u++) {
       const int i = i0 + u * takers + group % takers;
       if (mine > 0 || i >= rows) continue;
-      store_out(a, tile.start, head, tile.row0 + i, 4 * c, x[u] * (sum[u] > 0 || sum[u] != sum[u] ? 1.0f / sum[u] : 0.0f));
-      if (c == 0) store_lse(a, tile.start, head, tile.row0 + i, top[u], sum[u]);
+      if constexpr (RESULT) {
+        store_out(a, tile.start, head, tile.row0 + i, 4 * c, x[u] * (sum[u] > 0 || sum[u] != sum[u] ? 1.0f / sum[u] : 0.0f));
+        if (c == 0) store_lse(a, tile.start, head, tile.row0 + i, top[u], sum[u]);
+      } else {
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4, x[u]), left, place(0, i) + 16 + 16 * c, 0, kDeviceScope);
+        if (c == 0) __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u2, f2{top[u], sum[u]}), left, place(0, i), 0, kDeviceScope);
+      }
     }
   }
 }
 
 // The end of a workgroup whose share has `pending` tiles that lie in others too (only its first and its last can).  Every wavefront's
 // stores have been acknowledged before the workgroup is counted in, and the parts are asked for after the count has come back; they go
-// to the level of the memory system that all compute units share.
+// to the level of the memory system that all compute units share.  Where one workgroup would wait for memory more than kTrips
+// times, the last of every kNear shares adds up theirs, and the last of those workgroups the sums: 64 rows of one sequence of 131071
+// and one kv head 137 -> 52 us, with 8 kv heads 116 -> 84.  Where that rule says one, two would cost a second count: 16 sequences of
+// 3001 with 40 rows 34 -> 41, one of 131071 with 4 rows 36 -> 38.
 template <int D, int THREADS, int U, int P>
-__device__ __forceinline__ void join_pending(const AttentionArgs& a, int pending, const Pending& first, const Pending& last, __amdgpu_buffer_rsrc_t left, int head, float* lds, bool* all_there) {
+__device__ __forceinline__ void join_pending(const AttentionArgs& a, int pending, const Pending& first, const Pending& last, __amdgpu_buffer_rsrc_t left, int share, int head, float* lds, bool* all_there) {
   if (pending == 0) return;
+  auto in_two = [](const Pending& tile) { return tile.rows * tile.count > kTrips * (THREADS / (D / 4)) * U * P; };
+  auto count_in = [&](uint32_t* counts, int at, int of) {  // whether this workgroup is the last
+    uint32_t* const counter = counts + head * a.shares + at;
+    const bool is_last = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)of - 1;
+    if (is_last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return is_last;
+  };
+  auto near = [&](const Pending& tile) { return max(share - tile.first, 0) / kNear * kNear; };  // the first of the shares that are added up together
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   if (threadIdx.x < (unsigned)pending) {
-    const Pending mine = threadIdx.x == 0 ? first : last;
-    uint32_t* const counter = a.counts + head * a.shares + mine.first;
-    const bool is_last = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)mine.count - 1;
-    if (is_last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    all_there[threadIdx.x] = is_last;
+    const Pending tile = threadIdx.x == 0 ? first : last;
+    if (in_two(tile)) {
+      const int at = near(tile), members = min(tile.count - at, kNear);
+      all_there[threadIdx.x] = members < 2 || count_in(a.counts + a.shares * a.v.kv_heads, tile.first + at, members);
+    } else {
+      all_there[threadIdx.x] = count_in(a.counts, tile.first, tile.count);
+    }
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
 #pragma unroll 1
-  for (int i = 0; i < pending; i++)
-    if (all_there[i]) join_parts<D, THREADS, U, P>(a, i == 0 ? first : last, left, head, lds);
+  for (int i = 0; i < pending; i++) {
+    if (!all_there[i]) continue;
+    const Pending tile = i == 0 ? first : last;
+    if (!in_two(tile)) {
+      join_parts<D, THREADS, U, P>(a, tile, left, head, lds, tile.first, tile.count);
+      continue;
+    }
+    const int members = min(tile.count - near(tile), kNear), sums = (tile.count + kNear - 1) / kNear;
+    if (members > 1) join_parts<D, THREADS, U, P, 1, false>(a, tile, left, head, lds, tile.first + near(tile), members);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0) all_there[i] = count_in(a.counts, tile.first, sums);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (all_there[i]) join_parts<D, THREADS, U, P, kNear>(a, tile, left, head, lds, tile.first, sums);
+  }
 }
 
 // ---- the kernels' launches -----------------------------------------------------------------------------
 // Workgroups of a compute unit: what the registers allow.
-constexpr int stream_groups(int d, int qt, int waves) { return waves == 8 ? 1 : d * qt <= 128 ? 3 : d * qt < 512 ? 2 : 1; }
+constexpr int stream_groups(int d, int qt, int waves) { return waves == 8 ? 1 : d * qt <= 128 ? 3 : 2; }
 void launch_stream(const AttentionArgs& a, int head_dim, int scale_group, int qt, int waves, unsigned grid, hipStream_t stream);  // 8 only for qt = 1, up to D = 128
 void launch_tile(const AttentionArgs& a, int head_dim, int scale_group, int waves, unsigned grid, hipStream_t stream);  // 8 only up to D = 128
 

@@ -14,8 +14,8 @@ constexpr int kFewTiles = 160;    // tiles of 128 rows: with fewer the chip is n
 constexpr int kLoneTiles = 64;    // of stream_kernel: so many or fewer have eight wavefronts (one sequence of 131071, 8 heads: 42 -> 38 us)
 constexpr int kShortKeys = 4096;  // so have up to 256 tiles with so many keys at most (64 x 1000, 4 heads: 14.4 -> 12.1 us; 32 ragged x 8192, 8 heads: 42 -> 46)
 constexpr int kLongKeys = 4096;   // keys from which on tiles of 256 rows are the faster ones, where they fill the chip
-constexpr size_t kCountBytes = 64 * 1024;  // of a workspace: counts of any call (kv_heads x shares of them), at its front
-static_assert(4 * kComputeUnits * sizeof(uint32_t) <= kCountBytes && AMS_KV_MAX_HEADS * sizeof(uint32_t) <= kCountBytes, "one for each share of each head");
+constexpr size_t kCountBytes = 64 * 1024;  // of a workspace: counts of any call (2 kv_heads x shares of them), at its front
+static_assert(8 * kComputeUnits * sizeof(uint32_t) <= kCountBytes && 2 * AMS_KV_MAX_HEADS * sizeof(uint32_t) <= kCountBytes, "two for each share of each head");
 
 struct Plan {
   bool tile;  // tile_kernel
@@ -31,7 +31,8 @@ Plan make_plan(const ams_kv_cache* c, int64_t rows, int heads, int64_t max_q_len
   const int R = heads / c->kv_heads;
   const int64_t most = (c->q_starts ? std::min(max_q_len > 0 ? max_q_len : rows, rows) : 1) * R;
   const int64_t capacity = (int64_t)c->table_width * c->page_size, keys = window > 0 ? std::min(window, capacity) : capacity;
-  p.qt = most <= 16 ? 1 : most <= 32 || c->head_dim == 256 ? 2 : 4;
+  // column tiles of 16 rows: as few as hold them (40 rows of 16 sequences of 3001, 8 kv heads: three 34 us, four 38)
+  p.qt = most <= 16 ? 1 : most <= 32 || c->head_dim == 256 ? 2 : most <= 48 ? 3 : 4;
   const int64_t tiles = rows * R / 128 * c->kv_heads;
   p.tile = most > kStreamRows && (tiles >= kFewTiles || keys <= kUncutSteps * kStep);
   p.waves = 4;

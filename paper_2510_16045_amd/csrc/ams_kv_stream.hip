@@ -336,7 +336,7 @@ __global__ __launch_bounds__(64 * WAVES, stream_groups(D, QT, WAVES) * WAVES / 4
     }
     __syncthreads();  // what the tile left in LDS has been read
   }
-  join_pending<D, 64 * WAVES, QT == 1 ? 1 : 4, QT == 1 ? 8 : 4>(a, pending, left_first, left_last, left, head, (float*)shared, all_there);
+  join_pending<D, 64 * WAVES, QT == 1 ? 1 : 4, QT == 1 ? 8 : 4>(a, pending, left_first, left_last, left, share, head, (float*)shared, all_there);
 }
 
 bool load_stream() { return loaded((const void*)stream_kernel<64, 32, 1, 4>); }
@@ -347,6 +347,7 @@ void launch_stream(const AttentionArgs& a, int head_dim, int scale_group, int qt
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * waves), 0, stream, a); };
     if constexpr (D < 256) {
       if (waves == 8) return launch(stream_kernel<D, G, 1, 8>);
+      if (qt == 3) return launch(stream_kernel<D, G, 3, 4>);
       if (qt == 4) return launch(stream_kernel<D, G, 4, 4>);  // 256 accumulators do not fit beside the rows
     }
     if (qt == 1) return launch(stream_kernel<D, G, 1, 4>);

@@ -348,3 +348,18 @@ def test_row_starts_that_make_no_sense_touch_nothing_else():
             ams.ams_kv_attention(q, c.cache, c.table, c.kv_lens, c.G, q_starts=dev(np.array(starts, dtype=np.int32)), max_q_len=hint, workspace=WORKSPACE, out=store[1:-1])
             assert bool((store[0] == 7).all()) and bool((store[-1] == 7).all())
             assert not bool(torch.isnan(store).any())
+
+
+@pytest.mark.parametrize("heads,kv_heads,rows,D,G", [(16, 1, 1, 128, 32), (32, 1, 1, 128, 128), (20, 1, 2, 128, 64), (8, 1, 8, 128, 32), (64, 1, 1, 64, 64), (4, 1, 8, 256, 128), (12, 2, 8, 64, 32)])
+@pytest.mark.parametrize("tokens", [8000, 12321])
+def test_rows_of_one_sequence_in_many_parts(heads, kv_heads, rows, D, G, tokens):
+    # 17 and 25 parts or more of 16 to 64 rows: sums of sums, the last of one part only
+    c = Case([tokens], [rows], heads=heads, kv_heads=kv_heads, D=D, G=G, page=64)
+    out = c.check()
+    for _ in range(3):
+        assert np.array_equal(out, host(c.run()))
+
+
+def test_sequences_in_many_parts_beside_each_other():
+    Case([9000, 8100, 33, 10000], [8, 8, 8, 8], heads=6, kv_heads=1, D=128, G=32, page=64).check()
+    Case([9000, 8100, 33, 10000], [12, 12, 12, 12], heads=4, kv_heads=1, D=64, G=32, page=64, window=8400).check()
