@@ -6,11 +6,11 @@
 // kv head are rows of one problem: row r of a sequence is token r / R of its query rows and head r % R of the kv head's R.
 //
 // Split of the work: the host knows neither lengths nor (with row starts) how many rows a sequence has, so every workgroup works it
-// out from them: the steps of all row tiles of a kv head, one tile after the other, are cut into equal shares, as many as there are
-// workgroups that fit on the chip at once.  A share may begin and end inside a tile; that a workgroup begins a tile counts as much as
-// kTileSteps steps.  Where no tile has more than kUncutSteps, shares are made of whole tiles.  Of a tile that lies in several shares every
-// workgroup leaves its part (max, sum, O) in the workspace and counts itself in; the one that comes last adds all of them up, always in
-// the same order, and clears the count.  Nobody waits for anybody.
+// out from them.  tile_kernel's workgroups take a tile of rows each.  For stream_kernel the steps of all row tiles of a kv head, one tile
+// after the other, are cut into equal shares, as many as there are workgroups that fit on the chip at once.  A share may begin and end
+// inside a tile; that a workgroup begins a tile counts as much as kTileSteps steps.  Where no tile has more than kUncutSteps, shares are
+// made of whole tiles.  Of a tile that lies in several shares every workgroup leaves its part (max, sum, O) in the workspace and counts
+// itself in; the one that comes last adds all of them up, always in the same order, and clears the count.  Nobody waits for anybody.
 #ifndef AMS_KV_ATTENTION_H_
 #define AMS_KV_ATTENTION_H_
 
@@ -20,11 +20,11 @@ namespace ams_kv {
 
 constexpr int kDeviceScope = 16;  // cache policy (sc1) of a buffer load or store that the whole device sees
 constexpr int kStep = 32;         // keys of a wavefront's step
-constexpr int kMinShare = 16;     // steps of a share: four for each wavefront
-constexpr int kTileSteps = 14;    // what it takes to begin a tile and to leave its result, in steps
-constexpr int kUncutSteps = 32;   // a tile of so many is not cut: joining its parts takes longer than its steps
-constexpr int kMaxParts = 64;     // a tile in more parts costs its last workgroup more than the others gain
-constexpr int kNear = 8;          // parts of a tile that are added up first where there are many
+constexpr int kMinShare = 16;     // steps of a share (4 sequences of 3000, 8 kv heads: 8 or 16 11.5 us, 32 17.6)
+constexpr int kTileSteps = 14;    // what it takes to begin a tile and to leave its result, in steps (32 ragged sequences of up to 8192, 8 kv heads: 8 42.8 us, 14 41.5, 24 42.3)
+constexpr int kUncutSteps = 32;   // a tile of so many is not cut: joining its parts takes longer than its steps (64 of up to 1000, 4 kv heads: 32 or 64 11.2 us, 16 18.4)
+constexpr int kMaxParts = 64;     // of a tile (one of 131071: at most 32 parts 54 us, 64 41, 128 42; 64 rows of it, one kv head: 64 52, 128 59)
+constexpr int kNear = 8;          // parts of a tile that are added up first where there are many (64 rows of 131071, one kv head: 4 62 us, 8 52; 8 kv heads: 8 85, 16 90)
 constexpr int kTrips = 2;         // one workgroup adds up all parts of a tile if it waits for them no more than so often
 constexpr float kLift = 8.0f;     // exponents of P are raised by this: below it P keeps fp16's full precision over 2^-22 of the largest
 constexpr float kSlack = 7.0f;    // how far (log2) a score may pass the running maximum before that is raised: 2^(8 + 7) is in fp16
@@ -259,7 +259,7 @@ __device__ __forceinline__ void join_parts(const AttentionArgs& a, const Pending
 // to the level of the memory system that all compute units share.  Where one workgroup would wait for memory more than kTrips
 // times, the last of every kNear shares adds up theirs, and the last of those workgroups the sums: 64 rows of one sequence of 131071
 // and one kv head 137 -> 52 us, with 8 kv heads 116 -> 84.  Where that rule says one, two would cost a second count: 16 sequences of
-// 3001 with 40 rows 34 -> 41, one of 131071 with 4 rows 36 -> 38.
+// 3001 with 40 rows 33 -> 40, one of 131071 with 4 rows 36 -> 38.
 template <int D, int THREADS, int U, int P>
 __device__ __forceinline__ void join_pending(const AttentionArgs& a, int pending, const Pending& first, const Pending& last, __amdgpu_buffer_rsrc_t left, int share, int head, float* lds, bool* all_there) {
   if (pending == 0) return;
@@ -304,7 +304,8 @@ __device__ __forceinline__ void join_pending(const AttentionArgs& a, int pending
 }
 
 // ---- the kernels' launches -----------------------------------------------------------------------------
-// Workgroups of a compute unit: what the registers allow.
+// Workgroups of a compute unit: what the registers allow (a fourth one where 16 rows of 128 channels leave room gains nothing; four column
+// tiles of 128 channels: two 40 us, one 42, at 16 sequences of 3001, 8 kv heads and 64 rows).
 constexpr int stream_groups(int d, int qt, int waves) { return waves == 8 ? 1 : d * qt <= 128 ? 3 : 2; }
 void launch_stream(const AttentionArgs& a, int head_dim, int scale_group, int qt, int waves, unsigned grid, hipStream_t stream);  // 8 only for qt = 1, up to D = 128
 void launch_tile(const AttentionArgs& a, int head_dim, int scale_group, int waves, unsigned grid, hipStream_t stream);  // 8 only up to D = 128

@@ -9,11 +9,21 @@ namespace ams_kv {
 
 // ---- launch ------------------------------------------------------------------------------------------
 constexpr int kComputeUnits = 256;
-constexpr int kStreamRows = 64;   // up to so many rows of a kv head stream_kernel takes
-constexpr int kFewTiles = 160;    // tiles of 128 rows: with fewer the chip is not full, and stream_kernel, which shares long keys out, is faster
-constexpr int kLoneTiles = 64;    // of stream_kernel: so many or fewer have eight wavefronts (one sequence of 131071, 8 heads: 42 -> 38 us)
-constexpr int kShortKeys = 4096;  // so have up to 256 tiles with so many keys at most (64 x 1000, 4 heads: 14.4 -> 12.1 us; 32 ragged x 8192, 8 heads: 42 -> 46)
-constexpr int kLongKeys = 4096;   // keys from which on tiles of 256 rows are the faster ones, where they fill the chip
+// Rows of a kv head that stream_kernel takes in one tile.  Beyond them it reads the cache once for every 64, where tile_kernel restores
+// it once for 128 or 256 rows.
+constexpr int kStreamRows = 64;
+// Tiles of 128 rows: with fewer the chip is not full, and stream_kernel, which shares long keys out, is faster (512 rows over 8192 keys, 32
+// query and 8 kv heads, 128 tiles: 114 us, tile_kernel 124; 8 times 64 rows over 4096: 64 and 82).  Keys of kUncutSteps steps are never
+// shared out.
+constexpr int kFewTiles = 160;
+// Tiles of stream_kernel: so many or fewer have eight wavefronts (one sequence of 131071, 8 kv heads: 42 -> 38 us).
+constexpr int kLoneTiles = 64;
+// So have up to 256 tiles with so many keys at most (64 x 1000, 4 kv heads: 14.4 -> 12.1 us; 32 ragged x 8192, 8 heads: 42 -> 46).
+constexpr int kShortKeys = 4096;
+// Keys from which on tiles of 256 rows, which restore a key once for twice the rows, are the faster ones where they fill the chip (2048 rows
+// over 8192 keys: 267 us, tiles of 128 285); with fewer the shorter tiles end more evenly (4 times 1024 over 1024: 76 and 69; a window of
+// 512: 64 and 54).
+constexpr int kLongKeys = 4096;
 constexpr size_t kCountBytes = 64 * 1024;  // of a workspace: counts of any call (2 kv_heads x shares of them), at its front
 static_assert(8 * kComputeUnits * sizeof(uint32_t) <= kCountBytes && 2 * AMS_KV_MAX_HEADS * sizeof(uint32_t) <= kCountBytes, "two for each share of each head");
 
@@ -31,7 +41,7 @@ Plan make_plan(const ams_kv_cache* c, int64_t rows, int heads, int64_t max_q_len
   const int R = heads / c->kv_heads;
   const int64_t most = (c->q_starts ? std::min(max_q_len > 0 ? max_q_len : rows, rows) : 1) * R;
   const int64_t capacity = (int64_t)c->table_width * c->page_size, keys = window > 0 ? std::min(window, capacity) : capacity;
-  // column tiles of 16 rows: as few as hold them (40 rows of 16 sequences of 3001, 8 kv heads: three 34 us, four 38)
+  // column tiles of 16 rows: as few as hold them (40 rows of 16 sequences of 3001, 8 kv heads: three 33 us, four 38)
   p.qt = most <= 16 ? 1 : most <= 32 || c->head_dim == 256 ? 2 : most <= 48 ? 3 : 4;
   const int64_t tiles = rows * R / 128 * c->kv_heads;
   p.tile = most > kStreamRows && (tiles >= kFewTiles || keys <= kUncutSteps * kStep);

@@ -3,6 +3,10 @@
 // Both are one pass over the rows: 4 D bytes of K and V per token and head on one side, D + 4 D / scale_group on the other.
 // A wavefront takes a tile of 16 tokens of one head; the rows of a sequence are its last ones, so a tile is found from the row
 // starts alone: sequence b has at most floor(rows / 16) + 2 tiles, and those of b begin at floor(start / 16) + 2 b.
+//
+// Memory bounds them, and the launch where there are few rows.  16384 rows of 8 heads of 128 channels, runs of 32: written in 19.8 us (86 MB,
+// 4.3 TB/s), read back in 14.2 (6.1 TB/s; a copy of 1 GiB goes at 5.1, a bare read at 7.1); 131072 rows read back in 114 to 123 (5.6 to 6.0); one row for
+// each of 32 sequences 4.5 and 3.3 us, where an empty launch takes 2.
 #include "ams_kv.h"
 
 namespace ams_kv {
