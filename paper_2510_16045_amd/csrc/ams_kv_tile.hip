@@ -18,7 +18,11 @@ typedef float f16v __attribute__((ext_vector_type(16)));
 
 constexpr int kBlock = 64;                // keys
 constexpr int kBlockTiles = kBlock / kTile;
-constexpr int kAhead = 4;                 // fragments that are read ahead (2: 269 us where 4 take 267, 8: 271)
+// Fragments that are read ahead (2048 rows over 8192 keys of 128 channels: 2 269 us, 4 267, 8 271), and wavefronts of a SIMD: with 64 channels
+// and workgroups of four there are registers for four, and two fragments (seven prompts of up to 1999, a window of 512, 16 heads:
+// 49.9 -> 45.1 us; 16 of 2000 149 -> 142; 4 of 1024 over all keys 34.5 -> 35.5).
+constexpr int ahead(int d, int waves) { return d == 64 && waves == 4 ? 2 : 4; }
+constexpr int tile_waves(int d, int waves) { return d == 256 ? 1 : d == 64 && waves == 4 ? 4 : 2; }
 constexpr int kReads = 0x100, kProducts = 0x008;  // of a scheduling group: LDS reads, matrix instructions
 
 // What LDS holds of a block.
@@ -111,8 +115,8 @@ struct Job {
 };
 
 template <int D, int G, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void tile_kernel(AttentionArgs a) {
-  constexpr int ROWS = 32 * WAVES, RUNS = D / G, KF = D / 16, DT = D / 32, JOBS = 2 * kBlockTiles / WAVES;
+__global__ __launch_bounds__(64 * WAVES, tile_waves(D, WAVES)) void tile_kernel(AttentionArgs a) {
+  constexpr int ROWS = 32 * WAVES, RUNS = D / G, KF = D / 16, DT = D / 32, JOBS = 2 * kBlockTiles / WAVES, AHEAD = ahead(D, WAVES);
   const int wave = uniform((int)threadIdx.x >> 6), lane = lane_id(), h = lane >> 5, col = lane & 31;
   const int share = (int)a.v.heads.quotient(blockIdx.x), head = blockIdx.x - share * a.v.kv_heads;
   __shared__ Block<D> blocks[2];
@@ -185,29 +189,29 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void tile_kernel(Atte
     };
     auto compute = [&](int buffer, int key0) {
       const Block<D>& block = blocks[buffer];
-      // Fragments are read four instructions ahead of the one that takes them; left to itself the compiler reads each one where it is used
+      // Fragments are read AHEAD instructions ahead of the one that takes them; left to itself the compiler reads each one where it is used
       // and waits for it.
       constexpr int NK = 2 * KF, NV = kBlockTiles * DT;
       const u4 what = *(const u4*)notes[buffer].what;
-      h8 f[kAhead];
+      h8 f[AHEAD];
       f16v s[2];
 #pragma unroll
       for (int i = 0; i < 16; i++) s[0][i] = s[1][i] = 0;
 #pragma unroll
-      for (int n = 0; n < kAhead; n++) f[n] = block.k[n & 1][n >> 1][lane];
+      for (int n = 0; n < AHEAD; n++) f[n] = block.k[n & 1][n >> 1][lane];
 #pragma unroll
       for (int n = 0; n < NK; n++) {
-        s[n & 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[n % kAhead], q[n >> 1], s[n & 1], 0, 0, 0);
-        if (n + kAhead < NK) f[n % kAhead] = block.k[(n + kAhead) & 1][(n + kAhead) >> 1][lane];
+        s[n & 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[n % AHEAD], q[n >> 1], s[n & 1], 0, 0, 0);
+        if (n + AHEAD < NK) f[n % AHEAD] = block.k[(n + AHEAD) & 1][(n + AHEAD) >> 1][lane];
       }
-      __builtin_amdgcn_sched_group_barrier(kReads, kAhead, 0);
+      __builtin_amdgcn_sched_group_barrier(kReads, AHEAD, 0);
 #pragma unroll
       for (int n = 0; n < NK; n++) {
         __builtin_amdgcn_sched_group_barrier(kProducts, 1, 0);
-        if (n + kAhead < NK) __builtin_amdgcn_sched_group_barrier(kReads, 1, 0);
+        if (n + AHEAD < NK) __builtin_amdgcn_sched_group_barrier(kReads, 1, 0);
       }
 #pragma unroll
-      for (int n = 0; n < kAhead; n++) f[n] = block.v[n % DT][n / DT][lane];
+      for (int n = 0; n < AHEAD; n++) f[n] = block.v[n % DT][n / DT][lane];
       const uint32_t anything = (uint32_t)uniform((int)(what[0] | what[1] | what[2] | what[3]));
       if (key0 < whole_begin || key0 + kBlock > whole_end || (anything & kMissing)) {  // some row does not see some key
 #pragma unroll
@@ -243,13 +247,13 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void tile_kernel(Atte
       l += sum[0] + sum[1];
 #pragma unroll
       for (int n = 0; n < NV; n++) {
-        o[n % DT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[n % kAhead], p[n / DT], o[n % DT], 0, 0, 0);
-        if (n + kAhead < NV) f[n % kAhead] = block.v[(n + kAhead) % DT][(n + kAhead) / DT][lane];
+        o[n % DT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[n % AHEAD], p[n / DT], o[n % DT], 0, 0, 0);
+        if (n + AHEAD < NV) f[n % AHEAD] = block.v[(n + AHEAD) % DT][(n + AHEAD) / DT][lane];
       }
 #pragma unroll
       for (int n = 0; n < NV; n++) {
         __builtin_amdgcn_sched_group_barrier(kProducts, 1, 1);
-        if (n + kAhead < NV) __builtin_amdgcn_sched_group_barrier(kReads, 1, 1);
+        if (n + AHEAD < NV) __builtin_amdgcn_sched_group_barrier(kReads, 1, 1);
       }
       if (anything & kBad) {
 #pragma unroll
