@@ -307,7 +307,7 @@ __device__ __forceinline__ void join_pending(const AttentionArgs& a, int pending
 // Workgroups of a compute unit: what the registers allow (a fourth one where 16 rows of 128 channels leave room gains nothing; four column
 // tiles of 128 channels: two 40 us, one 42, at 16 sequences of 3001, 8 kv heads and 64 rows).
 constexpr int stream_groups(int d, int qt, int waves) { return waves == 8 ? 1 : d * qt <= 128 ? 3 : 2; }
-void launch_stream(const AttentionArgs& a, int head_dim, int scale_group, int qt, int waves, unsigned grid, hipStream_t stream);  // 8 only for qt = 1, up to D = 128
+void launch_stream(const AttentionArgs& a, int head_dim, int scale_group, int qt, int waves, unsigned grid, hipStream_t stream);  // 8 only up to D = 128, there for any qt, below for qt = 1
 void launch_tile(const AttentionArgs& a, int head_dim, int scale_group, int waves, unsigned grid, hipStream_t stream);  // 8 only up to D = 128
 
 }  // namespace ams_kv

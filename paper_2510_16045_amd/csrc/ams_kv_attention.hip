@@ -12,11 +12,12 @@ constexpr int kComputeUnits = 256;
 // Rows of a kv head that stream_kernel takes in one tile.  Beyond them it reads the cache once for every 64, where tile_kernel restores
 // it once for 128 or 256 rows.
 constexpr int kStreamRows = 64;
-// Tiles of 128 rows: with fewer the chip is not full, and stream_kernel, which shares long keys out, is faster (512 rows over 8192 keys, 32
-// query and 8 kv heads, 128 tiles: 114 us, tile_kernel 124; 8 times 64 rows over 4096: 64 and 82).  Keys of kUncutSteps steps are never
-// shared out.
-constexpr int kFewTiles = 160;
-// Tiles of stream_kernel: so many or fewer have eight wavefronts (one sequence of 131071, 8 kv heads: 42 -> 38 us).
+// Tiles of 128 rows: with fewer the chip is not full, and stream_kernel, which shares keys out, is faster (32 query and 8 kv heads of 128, 8192
+// keys: 512 rows, 128 tiles, 100 us, tile_kernel 193; 256 tiles 170 and 198; 384 252 and 257; of 256 channels 192 tiles 272 and 297, 256 335
+// and 313).  With fewer keys the shares fit less well (16 heads, 2048 keys: 128 tiles 34 and 56, 160 58 and 55, 192 64 and 57, 256 54 and
+// 59).  Keys of kUncutSteps steps are never shared out.
+constexpr int kFewTiles = 320, kFewWideTiles = 224, kFewShortTiles = 160;  // of up to 128 channels, of 256, and with fewer than kLongKeys keys
+// Tiles of 16 rows of stream_kernel: so many or fewer have eight wavefronts (one sequence of 131071, 8 kv heads: 42 -> 38 us).
 constexpr int kLoneTiles = 64;
 // So have up to 256 tiles with so many keys at most (64 x 1000, 4 kv heads: 14.4 -> 12.1 us; 32 ragged x 8192, 8 heads: 42 -> 46).
 constexpr int kShortKeys = 4096;
@@ -44,13 +45,18 @@ Plan make_plan(const ams_kv_cache* c, int64_t rows, int heads, int64_t max_q_len
   // column tiles of 16 rows: as few as hold them (40 rows of 16 sequences of 3001, 8 kv heads: three 33 us, four 38)
   p.qt = most <= 16 ? 1 : most <= 32 || c->head_dim == 256 ? 2 : most <= 48 ? 3 : 4;
   const int64_t tiles = rows * R / 128 * c->kv_heads;
-  p.tile = most > kStreamRows && (tiles >= kFewTiles || keys <= kUncutSteps * kStep);
+  p.tile = most > kStreamRows && (tiles >= (keys < kLongKeys ? kFewShortTiles : c->head_dim == 256 ? kFewWideTiles : kFewTiles) || keys <= kUncutSteps * kStep);
   p.waves = 4;
   if (p.tile && c->head_dim < 256 && tiles >= 2 * kComputeUnits && keys >= kLongKeys) p.waves = 8;
   p.rows = p.tile ? 32 * p.waves : 16 * p.qt;
   p.row_tiles = c->q_starts ? rows * R / p.rows + c->batch : c->batch * (int64_t)((R + p.rows - 1) / p.rows);
-  // few tiles, or short ones of which no compute unit has two: eight wavefronts to a tile
-  if (!p.tile && p.qt == 1 && c->head_dim < 256 && (p.row_tiles * c->kv_heads <= kLoneTiles || (p.row_tiles * c->kv_heads <= kComputeUnits && capacity <= kShortKeys))) p.waves = 8;
+  // Tiles of stream_kernel, if no sequence has more rows than the caller says: eight wavefronts where they are few, or short and no compute
+  // unit has two; with several column tiles of 128 channels wherever no compute unit has two (16 rows of 32 sequences of 1500, 32 query and
+  // 8 kv heads: 48 -> 30 us; 64 of one of 131071: 85 -> 70; with two, 64 sequences of 500 and 8 rows: 17 -> 25; 64 channels: 64 rows of one of
+  // 131071 51 -> 49, 32 rows 41 -> 46).
+  const int64_t about = std::min<int64_t>(p.row_tiles, c->batch * ((most + p.rows - 1) / p.rows)) * c->kv_heads;
+  if (!p.tile && p.qt == 1 && c->head_dim < 256 && (about <= kLoneTiles || (about <= kComputeUnits && capacity <= kShortKeys))) p.waves = 8;
+  if (!p.tile && p.qt > 1 && c->head_dim == 128 && about <= kComputeUnits) p.waves = 8;
   const int64_t tile_steps = std::max<int64_t>((capacity + kStep - 1) / kStep, 1);
   p.part_rows = (int)std::min<int64_t>(c->q_starts ? rows * R : R, p.rows);
   const size_t part = (size_t)c->kv_heads * p.part_rows * (c->head_dim + 4) * sizeof(float);

@@ -353,8 +353,13 @@ void launch_stream(const AttentionArgs& a, int head_dim, int scale_group, int qt
   dispatch(head_dim, scale_group, [&](auto d, auto g) {
     constexpr int D = decltype(d)::value, G = decltype(g)::value;
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * waves), 0, stream, a); };
+    if constexpr (D == 128) {
+      if (waves == 8 && qt == 2) return launch(stream_kernel<D, G, 2, 8>);
+      if (waves == 8 && qt == 3) return launch(stream_kernel<D, G, 3, 8>);
+      if (waves == 8 && qt == 4) return launch(stream_kernel<D, G, 4, 8>);
+    }
     if constexpr (D < 256) {
-      if (waves == 8) return launch(stream_kernel<D, G, 1, 8>);
+      if (waves == 8 && qt == 1) return launch(stream_kernel<D, G, 1, 8>);
       if (qt == 3) return launch(stream_kernel<D, G, 3, 4>);
       if (qt == 4) return launch(stream_kernel<D, G, 4, 4>);  // 256 accumulators do not fit beside the rows
     }

@@ -363,3 +363,13 @@ def test_rows_of_one_sequence_in_many_parts(heads, kv_heads, rows, D, G, tokens)
 def test_sequences_in_many_parts_beside_each_other():
     Case([9000, 8100, 33, 10000], [8, 8, 8, 8], heads=6, kv_heads=1, D=128, G=32, page=64).check()
     Case([9000, 8100, 33, 10000], [12, 12, 12, 12], heads=4, kv_heads=1, D=64, G=32, page=64, window=8400).check()
+
+
+@pytest.mark.parametrize("rows", [10, 20, 31])
+@pytest.mark.parametrize("D,G", [(64, 64), (128, 32)])
+def test_drafts_of_many_sequences(D, G, rows):
+    # 272 tiles of two to four column tiles, more than there are compute units: four wavefronts to a tile, uncut (lengths up to 500) and cut
+    lens = [40 + (97 * b) % 460 for b in range(34)]
+    Case(lens, [rows] * 34, heads=16, kv_heads=8, D=D, G=G, page=64).check()
+    lens[5] = 2600
+    Case(lens, [rows] * 34, heads=16, kv_heads=8, D=D, G=G, page=64).check()
