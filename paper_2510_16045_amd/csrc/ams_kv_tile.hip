@@ -7,9 +7,9 @@
 // 8 + 4 h .. + 3 (h = lane / 32), and V's fragments are laid out in that order.
 //
 // What bounds it is the issue of instructions, which two wavefronts of a SIMD share: 2048 rows over 8192 keys, 32 query and 8 kv heads of 128
-// channels: 240 Gflop in 263 us, 0.91 Pflop/s, where a library product of 8192 x 8192 x 8192 reaches 1.16.  In copies with parts taken out:
+// channels: 241 Gflop in 254 to 263 us, 0.92 to 0.95 Pflop/s, where a library product of 8192 x 8192 x 8192 reaches 1.16.  In copies with parts taken out:
 // without restoring 235 us, without S too 165, without O too 136, without the softmax as well 101.  Tiles are never cut: keys of cut
-// tiles were joined through the workspace at 340 us.  With a window of 512, seven sequences of up to 1999 tokens, 16 heads of 64: 46 us.
+// tiles were joined through the workspace at 340 us.  With a window of 512, seven sequences of up to 1999 tokens, 16 heads of 64: 40 us.
 #include "ams_kv_attention.h"
 
 namespace ams_kv {
