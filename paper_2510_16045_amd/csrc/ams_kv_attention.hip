@@ -12,11 +12,12 @@ constexpr int kComputeUnits = 256;
 // Rows of a kv head that stream_kernel takes in one tile.  Beyond them it reads the cache once for every 64, where tile_kernel restores
 // it once for 128 or 256 rows.
 constexpr int kStreamRows = 64;
-// Tiles of 128 rows: with fewer the chip is not full, and stream_kernel, which shares keys out, is faster (32 query and 8 kv heads of 128, 8192
-// keys: 512 rows, 128 tiles, 100 us, tile_kernel 193; 256 tiles 170 and 198; 384 252 and 257; of 256 channels 192 tiles 272 and 297, 256 335
-// and 313).  With fewer keys the shares fit less well (16 heads, 2048 keys: 128 tiles 34 and 56, 160 58 and 55, 192 64 and 57, 256 54 and
-// 59).  Keys of kUncutSteps steps are never shared out.
-constexpr int kFewTiles = 320, kFewWideTiles = 224, kFewShortTiles = 160;  // of up to 128 channels, of 256, and with fewer than kLongKeys keys
+// Tiles of 128 rows: with fewer stream_kernel, which shares keys out evenly, is faster than tiles that do not fill the chip, or of different
+// lengths: 32 query and 8 kv heads of 128, one sequence of 8192: 128 tiles 100 us, tile_kernel 193; 256 tiles 170 and 198; 384 252 and
+// 257; lengths of 819 to 8192, 432 tiles 219 and 264; 8 of 4096, 400 tiles 235 and 241, 512 193 and 156; 256 channels, 8 of up to 4096, 280
+// tiles 165 and 222, 440 235 and 270, but one of 8192, 256 tiles, 335 and 313.  With fewer keys the shares fit less well (16 heads, 2048
+// keys: 128 tiles 34 and 56, 160 58 and 55, 192 64 and 57, 256 54 and 59).  Keys of kUncutSteps steps are never shared out.
+constexpr int kFewTiles = 448, kFewShortTiles = 160;  // with kLongKeys keys or more, and with fewer
 // Tiles of 16 rows of stream_kernel: so many or fewer have eight wavefronts (one sequence of 131071, 8 kv heads: 42 -> 38 us).
 constexpr int kLoneTiles = 64;
 // So have up to 256 tiles with so many keys at most (64 x 1000, 4 kv heads: 14.4 -> 12.1 us; 32 ragged x 8192, 8 heads: 42 -> 46).
@@ -45,7 +46,7 @@ Plan make_plan(const ams_kv_cache* c, int64_t rows, int heads, int64_t max_q_len
   // column tiles of 16 rows: as few as hold them (40 rows of 16 sequences of 3001, 8 kv heads: three 33 us, four 38)
   p.qt = most <= 16 ? 1 : most <= 32 || c->head_dim == 256 ? 2 : most <= 48 ? 3 : 4;
   const int64_t tiles = rows * R / 128 * c->kv_heads;
-  p.tile = most > kStreamRows && (tiles >= (keys < kLongKeys ? kFewShortTiles : c->head_dim == 256 ? kFewWideTiles : kFewTiles) || keys <= kUncutSteps * kStep);
+  p.tile = most > kStreamRows && (tiles >= (keys < kLongKeys ? kFewShortTiles : kFewTiles) || keys <= kUncutSteps * kStep);
   p.waves = 4;
   if (p.tile && c->head_dim < 256 && tiles >= 2 * kComputeUnits && keys >= kLongKeys) p.waves = 8;
   p.rows = p.tile ? 32 * p.waves : 16 * p.qt;
