@@ -6,11 +6,16 @@
 // kv head are rows of one problem: row r of a sequence is token r / R of its query rows and head r % R of the kv head's R.
 //
 // Split of the work: the host knows neither lengths nor (with row starts) how many rows a sequence has, so every workgroup works it
-// out from them.  tile_kernel's workgroups take a tile of rows each.  For stream_kernel the steps of all row tiles of a kv head, one tile
-// after the other, are cut into equal shares, as many as there are workgroups that fit on the chip at once.  A share may begin and end
-// inside a tile; that a workgroup begins a tile counts as much as kTileSteps steps.  Where no tile has more than kUncutSteps, shares are
-// made of whole tiles.  Of a tile that lies in several shares every workgroup leaves its part (max, sum, O) in the workspace and counts
-// itself in; the one that comes last adds all of them up, always in the same order, and clears the count.  Nobody waits for anybody.
+// out from them.  tile_kernel's workgroups take a tile of rows each.  For stream_kernel the steps of all row tiles of a kv head are shared
+// out among as many workgroups as fit on the chip at once:
+//   where no tile has more than kUncutSteps, whole tiles;
+//   where there are two shares or more for a tile, parts of one tile each, of up to so many steps that there are enough shares (8 sequences
+//   of 2400 with 16 rows, 32 query and 8 kv heads: 37 us if shares cross tiles, 24 so; 16 of 3001 with 40 rows 30 and 28.5; 8 of 2000 with
+//   4 rows 17 and 13; but 4 of 3000 11.7 and 12.4: the split takes longer to work out);
+//   else, and for a tile alone, which has no other to cross into, equal shares of all steps, one tile after the other, which may begin and
+//   end inside a tile; that a workgroup begins a tile counts as much as kTileSteps steps.
+// Of a tile that lies in several shares every workgroup leaves its part (max, sum, O) in the workspace and counts itself in; the one that
+// comes last adds all of them up, always in the same order, and clears the count.  Nobody waits for anybody.
 #ifndef AMS_KV_ATTENTION_H_
 #define AMS_KV_ATTENTION_H_
 
@@ -98,24 +103,43 @@ __device__ __forceinline__ int hidden(int x) {
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ int of_lane(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
 
-// How much a share is, and all row tiles together: in steps with kTileSteps more for each tile, or in tiles that are not cut.
+// How much a share is, and all row tiles together: in tiles that are not cut; in parts of one tile each, of which a step is `pieces`; or in
+// steps with kTileSteps more for each tile.
 struct Split {
   uint32_t per, total;
+  float pieces;
   bool cut;
 };
-__device__ __forceinline__ uint32_t tile_cost(const Extent& e, bool cut) { return cut ? e.steps + kTileSteps : 1; }
+__device__ __forceinline__ uint32_t tile_cost(const Extent& e, const Split& split) {
+  if (!split.cut) return 1;
+  return split.pieces > 0 ? (uint32_t)((float)e.steps * split.pieces) + 1 : e.steps + kTileSteps;
+}
 template <int ROWS>
 __device__ __forceinline__ Split split_of(const AttentionArgs& a, const Extent& first) {  // first: of the first 64 sequences
-  uint32_t tiles = first.row_tiles, cost = first.row_tiles * tile_cost(first, true), most = first.row_tiles > 0 ? first.steps : 0;
+  uint32_t tiles = first.row_tiles, steps = first.row_tiles * first.steps, most = first.row_tiles > 0 ? first.steps : 0;
   for (int b0 = 64; b0 < a.v.batch; b0 += 64) {
     const Extent x = extent_of<ROWS>(a, b0 + lane_id());
-    tiles += x.row_tiles, cost += x.row_tiles * tile_cost(x, true), most = max(most, x.row_tiles > 0 ? (uint32_t)x.steps : 0);
+    tiles += x.row_tiles, steps += x.row_tiles * x.steps, most = max(most, x.row_tiles > 0 ? (uint32_t)x.steps : 0);
   }
-  Split split;
-  split.cut = a.cut && __ballot(most > (uint32_t)kUncutSteps) != 0;
-  split.total = wave_sum(split.cut ? cost : tiles);
-  split.per = (split.total + a.shares - 1) / (uint32_t)a.shares;
-  if (split.cut) split.per = max(split.per, (uint32_t)kMinShare);
+  Split split = {1, 0, 0.0f, a.cut && __ballot(most > (uint32_t)kUncutSteps) != 0};
+  const uint32_t shares = (uint32_t)a.shares;
+  tiles = wave_sum(tiles), steps = wave_sum(steps);
+  split.total = split.cut ? steps + tiles * kTileSteps : tiles;
+  if (split.cut && tiles > 1 && 2 * tiles <= shares) {
+    const float each = __builtin_amdgcn_rcpf((float)steps) * 0.9999f;  // rounds down: no more parts than shares
+#pragma unroll 1
+    for (uint32_t spare = tiles / 2;; spare = tiles) {  // shares that rounding up takes: half a part of a tile as a rule, one at most
+      split.pieces = fminf((float)(shares - spare) * each, 1.0f / kMinShare);
+      uint32_t parts = first.row_tiles * tile_cost(first, split);
+      for (int b0 = 64; b0 < a.v.batch; b0 += 64) {
+        const Extent x = extent_of<ROWS>(a, b0 + lane_id());
+        parts += x.row_tiles * tile_cost(x, split);
+      }
+      split.total = wave_sum(parts);
+      if (split.total <= shares || spare == tiles) return split;
+    }
+  }
+  split.per = max((split.total + shares - 1) / shares, split.cut ? (uint32_t)kMinShare : 1u);
   return split;
 }
 
@@ -126,11 +150,11 @@ struct Place {
   uint32_t first, cost;
 };
 template <int ROWS>
-__device__ __forceinline__ bool place_of(const AttentionArgs& a, Extent e, bool cut, uint32_t at, Place* out) {  // e: of the first 64 sequences
+__device__ __forceinline__ bool place_of(const AttentionArgs& a, Extent e, const Split& split, uint32_t at, Place* out) {  // e: of the first 64 sequences
   uint32_t before = 0;
   for (int b0 = 0; b0 < a.v.batch; b0 += 64) {
     if (b0 > 0) e = extent_of<ROWS>(a, b0 + lane_id());
-    const uint32_t each = tile_cost(e, cut), mine = e.row_tiles * each;
+    const uint32_t each = tile_cost(e, split), mine = e.row_tiles * each;
     const uint32_t end = wave_prefix(mine) + before;
     const unsigned long long past = __ballot(end > at);
     if (past) {

@@ -8,11 +8,11 @@
 // wavefronts' sums.  The running maximum is the wavefront's own until then.
 //
 // What bounds it is memory and the way to it.  32 sequences of 819 to 8192 tokens, 32 query and 8 kv heads of 128 channels, runs of 32:
-// 165 MB in 40 us, 4.1 TB/s; one sequence of 131071, runs of 64: 143 MB in 34.5 us.  A bare read of these bytes takes 23 and 20 us, and
+// 165 MB in 41 us, 4.0 TB/s; one sequence of 131071, runs of 64: 143 MB in 36.5 us.  A bare read of these bytes takes 23 and 20 us, and
 // the loop comes near that (21 to 26); 5 us pass before the first keys are there (lengths, table, cache: three trips, each from the
 // last one's answer), 5 to 8 at the end (parts out, count, parts in).  The vector units are busy for 16 of the 40 us (280
 // instructions a step of 32 keys and 16 rows, 112 of them the conversion of codes and their scaling), the matrix units for 4.  Five rows of
-// 16 sequences of 3001 tokens, 64 and 8 heads, tiles of 40 rows: 57 MB in 28.5 us; 550 instructions a step, 11 us of them.
+// 16 sequences of 3001 tokens, 64 and 8 heads, tiles of 40 rows: 57 MB in 27 us; 550 instructions a step, 11 us of them.
 #include "ams_kv_attention.h"
 
 namespace ams_kv {
@@ -132,12 +132,20 @@ __global__ __launch_bounds__(64 * WAVES, stream_groups(D, QT, WAVES) * WAVES / 4
   Place place;
   Pending left_first = {}, left_last = {};
   int pending = 0;
-  while (now < stop && place_of<ROWS>(a, first_64, split.cut, now, &place)) {
+  while (now < stop && place_of<ROWS>(a, first_64, split, now, &place)) {
     const Extent& e = place.e;
     const int rows = e.n * a.group, row0 = place.row_tile * ROWS;
     // the share's steps of the tile that some row sees, and the keys that every row sees
     const uint32_t then = min(place.first + place.cost, stop);
-    const int begin_step = split.cut ? max((int)(now - place.first) - kTileSteps, 0) : 0, end_step = split.cut ? (int)(then - place.first) - kTileSteps : e.steps;
+    int begin_step = 0, end_step = e.steps;
+    if (split.cut && split.pieces > 0) {
+      const uint32_t part = now - place.first;
+      const float each = (float)e.steps * __builtin_amdgcn_rcpf((float)place.cost);
+      begin_step = uniform((int)((float)part * each));
+      end_step = part + 1 == place.cost ? e.steps : uniform((int)((float)(part + 1) * each));
+    } else if (split.cut) {
+      begin_step = max((int)(now - place.first) - kTileSteps, 0), end_step = (int)(then - place.first) - kTileSteps;
+    }
     if (end_step <= 0 || then <= now) break;  // the tile begins in the next share (and starts that are not ascending end somewhere)
     now = then;
     const bool alone = begin_step == 0 && end_step == e.steps;
@@ -338,7 +346,8 @@ __global__ __launch_bounds__(64 * WAVES, stream_groups(D, QT, WAVES) * WAVES / 4
       }
     }
     if (!alone) {
-      const int first = min((int)((place.first + kTileSteps) / split.per), a.shares - 1), last = (int)((place.first + kTileSteps + e.steps - 1) / split.per);
+      const int first = split.pieces > 0 ? (int)place.first : min((int)((place.first + kTileSteps) / split.per), a.shares - 1);
+      const int last = split.pieces > 0 ? (int)(place.first + place.cost) - 1 : (int)((place.first + kTileSteps + e.steps - 1) / split.per);
       left_first = pending == 0 ? Pending{e.start, row0, min(rows - row0, ROWS), first, last - first + 1} : left_first;
       left_last = Pending{e.start, row0, min(rows - row0, ROWS), first, last - first + 1};
       pending++;

@@ -125,7 +125,7 @@ __global__ __launch_bounds__(64 * WAVES, tile_waves(D, WAVES)) void tile_kernel(
   const Split split = split_of<ROWS>(a, first_64);  // a tile each
   Place place;
   // the tiles with the most keys are a sequence's last: they go first
-  if ((uint32_t)share < split.total && place_of<ROWS>(a, first_64, false, split.total - 1 - share, &place)) {
+  if ((uint32_t)share < split.total && place_of<ROWS>(a, first_64, split, split.total - 1 - share, &place)) {
     const Extent& e = place.e;
     const int rows = e.n * a.group, tile_row = place.row_tile * ROWS, row0 = tile_row + 32 * wave;
     auto position = [&](int r) { return e.len - e.n + (int)a.by_group.quotient((uint32_t)r); };
