@@ -282,7 +282,8 @@ int ams_read_probe(const void* buf, size_t bytes, uint32_t* sink, void* stream);
  * one kv head (D / 2 bytes of codes and 2 D / scale_group bytes of scales for each of K and V and token).  Inside a
  * block the layout is the library's own.  Position p of sequence b lies in page
  * block_table[b * table_stride + p / page_size].  Entries outside [0, n_pages) name no page: rows there are not written,
- * read back as zeros and are left out of attention.  Sequences may share pages that they only read.
+ * read back as zeros and are left out of attention.  Sequences may share pages that they only read.  A pool needs no
+ * initial value: attention does not depend on what it holds where no row has been written.
  *
  * Rows.  Sequence b has kv_lens[b] tokens, those of the present call among them (a length is taken as at most
  * table_width * page_size, a negative one as 0).  Rows q_starts[b] .. q_starts[b + 1] - 1 of the call's tensors are

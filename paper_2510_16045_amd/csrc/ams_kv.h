@@ -30,6 +30,9 @@ typedef uint32_t u2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 
 constexpr int kTile = 16;  // tokens of a tile
+// Bits of the largest scale that ams_kv_write stores, 10912; it stores positive ones, so larger bits are a NaN or none of its own.  The
+// codes' largest value, 6, times any finite scale above it is no fp16 value.
+constexpr uint32_t kTopScale = 0x7154;
 
 // Bytes of a block's planes.
 struct Planes {
@@ -93,6 +96,12 @@ __device__ __forceinline__ int sequence_of(int batch, int item, First first) {
     if (n < 64) break;
   }
   return found;
+}
+
+// The larger of two halves each, as unsigned numbers: of fp16 values that are not negative the larger one.
+__device__ __forceinline__ uint32_t max_halves(uint32_t a, uint32_t b) {
+  const us2 x = __builtin_bit_cast(us2, a), y = __builtin_bit_cast(us2, b);
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(x, y));
 }
 
 __device__ __forceinline__ uint32_t bits(h2 x) { return __builtin_bit_cast(uint32_t, x); }

@@ -44,11 +44,6 @@ __device__ __forceinline__ void store8(uint16_t* p, u4 x, bool vec) {
   for (int i = 0; i < 4; i++) p[2 * i] = (uint16_t)x[i], p[2 * i + 1] = (uint16_t)(x[i] >> 16);
 }
 
-__device__ __forceinline__ uint32_t max_halves(uint32_t a, uint32_t b) {
-  const us2 x = __builtin_bit_cast(us2, a), y = __builtin_bit_cast(us2, b);
-  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(x, y));
-}
-
 // A lane's value from another lane of its 16, by a data-parallel pattern.
 template <int PATTERN>
 __device__ __forceinline__ uint32_t moved(uint32_t x) {

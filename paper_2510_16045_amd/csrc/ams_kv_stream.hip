@@ -70,7 +70,9 @@ struct StepV {
 };
 
 // Runs of V that stand for NaN take part in a step's products as zeros where not every row sees every key of the step, and the rows
-// that do see one get the NaN here.  stage: the scales of the step's two tiles; begin, end: the keys that a lane's row sees.
+// that do see one get the NaN here.  So do runs whose scale is none that ams_kv_write stores (bits above kTopScale): they lie where no row has been
+// written, where a pool may hold anything, and a value that is no fp16 value any more would turn the 0 of a key that is not seen into a
+// NaN as well.  stage: the scales of the step's two tiles; begin, end: the keys that a lane's row sees.
 template <int RUNS, int G, int QT, int DT>
 __device__ __forceinline__ void nan_of_seen_keys(uint8_t* stage, int lane, int first_key, const int (&begin)[QT], const int (&end)[QT], f4 (&o)[DT][QT]) {
   const int g = lane >> 4;
@@ -82,7 +84,7 @@ __device__ __forceinline__ void nan_of_seen_keys(uint8_t* stage, int lane, int f
     for (int u = 0; u < 2; u++)
 #pragma unroll
       for (int j = 0; j < 4; j++)
-        if ((*(const uint16_t*)(stage + ((u * 4 + g) * RUNS + run) * 8 + 2 * j) & 0x7C00) == 0x7C00) bad[run] |= 1u << (16 * u + 4 * g + j);
+        if (*(const uint16_t*)(stage + ((u * 4 + g) * RUNS + run) * 8 + 2 * j) > kTopScale) bad[run] |= 1u << (16 * u + 4 * g + j);
     any |= bad[run];
   }
   if (!__ballot(any != 0)) return;

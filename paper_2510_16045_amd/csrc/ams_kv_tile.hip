@@ -31,7 +31,8 @@ struct Block {
   h8 k[2][D / 16][64];            // [32 keys][16 channels][lane]
   h8 v[D / 32][kBlockTiles][64];  // [32 channels][16 keys][lane]
 };
-// Of its tiles: whether the table names no page, and whether V stands for NaN somewhere; if so the keys (bits), by run.
+// Of its tiles: whether the table names no page, and whether V stands for NaN somewhere or has a scale that ams_kv_write does not
+// store (bits above kTopScale), as there may be where no row has been written; if so the keys (bits), by run.
 constexpr uint32_t kMissing = 1, kBad = 2;
 template <int RUNS>
 struct Notes {
@@ -78,11 +79,10 @@ struct Job {
   }
   __device__ __forceinline__ void store_v(Block<D>& block, Notes<RUNS>& notes, int tile, int lane) {
     const int q = lane >> 4, c = lane & 15;
-    // a scale that stands for NaN times 0 is NaN
-    h2 nan = {0, 0};
+    uint32_t most = 0;
 #pragma unroll
-    for (int i = 0; i < 2 * RUNS; i++) nan += halves(s[i]) * h2{0, 0};
-    const bool bad = nan[0] != nan[0] || nan[1] != nan[1];
+    for (int i = 0; i < 2 * RUNS; i++) most = max_halves(most, s[i]);
+    const bool bad = (most & 0xFFFFu) > kTopScale || most >> 16 > kTopScale;
     const bool any = __ballot(bad) != 0;
     if (any) note_bad(notes, tile, lane);
     if (lane == 0) notes.what[tile] = (held ? 0 : kMissing) | (any ? kBad : 0);
@@ -95,7 +95,7 @@ struct Job {
       to[i * kBlockTiles * 128 + 32] = y;
     }
   }
-  // V's runs that stand for NaN take part as zeros: what masks a key cannot be told from its 0 weight.  The rows that see one get the NaN.
+  // Such runs of V take part as zeros: what masks a key cannot be told from its 0 weight.  The rows that see one get the NaN.
   __device__ __forceinline__ void note_bad(Notes<RUNS>& notes, int tile, int lane) {
     const int q = lane >> 4;
 #pragma unroll
@@ -103,7 +103,7 @@ struct Job {
       uint32_t keys = 0;
 #pragma unroll
       for (int j = 0; j < 4; j++)
-        if ((s[2 * run + j / 2] >> 16 * (j & 1) & 0x7C00) == 0x7C00) {
+        if ((s[2 * run + j / 2] >> 16 * (j & 1) & 0xFFFF) > kTopScale) {
           keys |= 1u << (4 * q + j);
           s[2 * run + j / 2] &= j & 1 ? 0x0000FFFFu : 0xFFFF0000u;
         }
