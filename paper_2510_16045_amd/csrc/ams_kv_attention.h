@@ -33,6 +33,8 @@ constexpr int kNear = 8;          // parts of a tile that are added up first whe
 constexpr int kTrips = 2;         // one workgroup adds up all parts of a tile if it waits for them no more than so often
 constexpr float kLift = 8.0f;     // exponents of P are raised by this: below it P keeps fp16's full precision over 2^-22 of the largest
 constexpr float kSlack = 7.0f;    // how far (log2) a score may pass the running maximum before that is raised: 2^(8 + 7) is in fp16
+constexpr float kFar = 1048576;   // maxima (log2) from which on exponents are differences of rounded products: below it a product that is not
+                                  // rounded lies within 2^-5 of one that is, far above it further than fp16 reaches
 
 struct AttentionArgs {
   View v;
@@ -94,6 +96,15 @@ __device__ __forceinline__ f2 with_16(float x) {
 }
 __device__ __forceinline__ float larger(f2 x) { return fmaxf(x[0], x[1]); }
 __device__ __forceinline__ float sum_of(f2 x) { return x[0] + x[1]; }
+
+// Whether some lane's maximum is that large (rows that have seen no key yet have none).
+__device__ __forceinline__ bool any_far(float top) { return __ballot(fabsf(top) >= kFar && top != -INFINITY) != 0; }
+// x - top in log2, 0 for the score that the maximum `top` comes from: its product has been rounded as this one is.
+__device__ __forceinline__ float below_top(float x, float scale2, float top) {
+#pragma clang fp contract(off)
+  const float y = x * scale2;
+  return top == -INFINITY ? y : y - top;
+}
 
 // x, of which the compiler knows nothing: what follows from it is not worked out before it is needed and kept in registers.
 __device__ __forceinline__ int hidden(int x) {

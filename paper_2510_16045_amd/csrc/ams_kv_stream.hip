@@ -177,6 +177,7 @@ __global__ __launch_bounds__(64 * WAVES, stream_groups(D, QT, WAVES) * WAVES / 4
 
     f4 o[DT][QT];
     float m[QT], l[QT];
+    bool far = false;  // some row's maximum is beyond kFar
 #pragma unroll
     for (int t = 0; t < QT; t++) {
       m[t] = -INFINITY, l[t] = 0;
@@ -205,21 +206,27 @@ __global__ __launch_bounds__(64 * WAVES, stream_groups(D, QT, WAVES) * WAVES / 4
 #pragma unroll
         for (int i = 1; i < 8; i++) top = fmaxf(top, s[i / 4][t][i % 4]);
         top *= a.scale2;
-        if (__ballot(top > m[t] + kSlack)) {
+        if (__ballot(top - m[t] > kSlack)) {
           top = fmaxf(top, m[t]);
           top = larger(with_32(larger(with_16(top))));
           const float less = top > m[t] ? __builtin_amdgcn_exp2f(m[t] - top) : 1.0f;
           m[t] = top;
+          far |= any_far(top);
           l[t] *= less;
 #pragma unroll
           for (int d = 0; d < DT; d++) o[d][t] *= less;
         }
-        const float sub = m[t] == -INFINITY ? 0.0f : m[t] - kLift;
+        float scale2 = a.scale2, sub = m[t] == -INFINITY ? 0.0f : m[t] - kLift;
+        if (far) {
+#pragma unroll
+          for (int i = 0; i < 8; i++) s[i / 4][t][i % 4] = below_top(s[i / 4][t][i % 4], a.scale2, m[t]);
+          scale2 = 1.0f, sub = -kLift;
+        }
 #pragma unroll
         for (int u = 0; u < 2; u++)
 #pragma unroll
           for (int i = 0; i < 4; i++) {
-            const float v = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][t][i], a.scale2, -sub));
+            const float v = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][t][i], scale2, -sub));
             l[t] += v;
             p[t][4 * u + i] = (_Float16)v;
           }

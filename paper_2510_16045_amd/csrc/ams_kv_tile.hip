@@ -154,6 +154,7 @@ __global__ __launch_bounds__(64 * WAVES, tile_waves(D, WAVES)) void tile_kernel(
     }
     f16v o[DT];
     float m = -INFINITY, l = 0;
+    bool far = false;  // some row's maximum is beyond kFar
 #pragma unroll
     for (int d = 0; d < DT; d++)
 #pragma unroll
@@ -226,21 +227,28 @@ __global__ __launch_bounds__(64 * WAVES, tile_waves(D, WAVES)) void tile_kernel(
 #pragma unroll
       for (int i = 1; i < 32; i++) top = fmaxf(top, s[i / 16][i % 16]);
       top *= a.scale2;
-      if (__ballot(top > m + kSlack)) {  // the maximum is raised only where a score passes it by more than the slack
+      float scale2 = a.scale2;
+      if (far || __ballot(top - m > kSlack)) {  // the maximum is raised only where a score passes it by more than the slack
         top = fmaxf(top, m);
         top = larger(with_32(top));
         const float less = top > m ? __builtin_amdgcn_exp2f(m - top) : 1.0f;
         m = top;
+        far |= any_far(top);
         l *= less;
 #pragma unroll
         for (int d = 0; d < DT; d++) o[d] *= less;
+        if (far) {
+#pragma unroll
+          for (int i = 0; i < 32; i++) s[i / 16][i % 16] = below_top(s[i / 16][i % 16], a.scale2, top);
+          scale2 = 1.0f;
+        }
       }
-      const float sub = m == -INFINITY ? 0.0f : m - kLift;
+      const float sub = far ? -kLift : m == -INFINITY ? 0.0f : m - kLift;
       h8 p[kBlockTiles];
       float sum[2] = {0, 0};
 #pragma unroll
       for (int i = 0; i < 32; i++) {
-        const float v = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 16][i % 16], a.scale2, -sub));
+        const float v = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 16][i % 16], scale2, -sub));
         sum[i & 1] += v;
         p[i / 8][i % 8] = (_Float16)v;
       }
