@@ -3,7 +3,7 @@
     qkv = ams_linear(x);  ams_kv_write(k, v);  ams_kv_attention(q);  ams_linear(o)
 
 Projections of up to MAX_M rows run on the packed weights; those of prompts restore a matrix to fp16 once and multiply with the
-library GEMM.  A decode step of fixed batch is captured as a HIP graph: the sequences' lengths lie on the GPU and grow from replay to
+library GEMM; captured ones of more rows run MAX_M rows at a time.  A decode step of fixed batch is captured as a HIP graph: the sequences' lengths lie on the GPU and grow from replay to
 replay.  ``python -m paper_2510_16045_amd.attention_layer`` runs a prompt and decode steps of a Llama-3-8B-shaped block on
 random weights and prints what a step takes.
 """
@@ -27,8 +27,18 @@ class PackedLinear:
         self.scales = torch.from_numpy(scales.view(np.int16)).cuda().view(torch.float16)
 
     def __call__(self, x, out=None):
-        if x.shape[0] <= MAX_M:
+        import torch
+
+        rows = x.shape[0]
+        if rows <= MAX_M:
             return ams_linear(self.packed, self.scales, x, self.N, self.fmt, out=out)
+        if torch.cuda.is_current_stream_capturing():
+            # a graph holds kernels of this library alone: the library GEMM sets itself up at its first call, which ends the process where
+            # that is captured
+            y = torch.empty((rows, self.N), dtype=x.dtype, device=x.device) if out is None else out
+            for i in range(0, rows, MAX_M):
+                ams_linear(self.packed, self.scales, x[i : i + MAX_M], self.N, self.fmt, out=y[i : i + MAX_M])
+            return y
         y = x @ ams_dequant(self.fmt, self.packed, self.scales, self.N, self.K).t()
         return y if out is None else out.copy_(y)
 
