@@ -50,7 +50,7 @@ class AttentionLayer:
         import torch
 
         self.head_dim = qkv.shape[0] // (heads + 2 * kv_heads)
-        self.heads, self.kv_heads, self.scale_group = heads, kv_heads, scale_group
+        self.heads, self.kv_heads, self.page_size, self.scale_group = heads, kv_heads, page_size, scale_group
         self.qkv, self.o = PackedLinear(qkv, fmt), PackedLinear(o, fmt)
         self.cache = ams_kv_cache(n_pages, kv_heads, self.head_dim, page_size, scale_group)
         self.block_table = block_table
@@ -67,7 +67,11 @@ class AttentionLayer:
 
 
 class DecodeStep:
-    """A decode step of a batch as a HIP graph: x in, y out; every replay adds a token to each sequence."""
+    """A decode step of a batch as a HIP graph: x in, y out; every replay adds a token to each sequence.
+
+    A step for which a sequence has no place left in its pages is refused.  The host counts the steps from the lengths that it has seen,
+    and looks at kv_lens again, which waits for the GPU, only where the count says that there is no place; whoever makes a sequence longer by hand calls
+    recount()."""
 
     def __init__(self, layer: AttentionLayer, kv_lens):
         import torch
@@ -75,6 +79,8 @@ class DecodeStep:
         ams_init()
         batch, hidden = kv_lens.shape[0], layer.qkv.K
         self.layer, self.kv_lens = layer, kv_lens
+        self.capacity = layer.block_table.shape[1] * layer.page_size
+        self.recount()
         self.x = torch.zeros((batch, hidden), dtype=torch.float16, device="cuda")
         self.y = torch.zeros_like(self.x)
         self.graph = torch.cuda.CUDAGraph()
@@ -82,7 +88,15 @@ class DecodeStep:
             self.kv_lens += 1
             layer(self.x, self.kv_lens, out=self.y)
 
+    def recount(self):
+        self.places = self.capacity - int(self.kv_lens.max())  # that the longest sequence has left
+
     def __call__(self, x):
+        if self.places <= 0:
+            self.recount()
+        if self.places <= 0:
+            raise ValueError(f"a sequence has no place for another token: the block table has room for {self.capacity}")
+        self.places -= 1
         self.x.copy_(x)
         self.graph.replay()
         return self.y

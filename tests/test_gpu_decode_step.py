@@ -1,4 +1,4 @@
-"""The captured decode step of attention_layer.py: batches of more rows than a Linear takes at once."""
+"""The captured decode step of attention_layer.py: batches of more rows than a Linear takes at once, and sequences whose pages are full."""
 
 import os
 import subprocess
@@ -45,3 +45,47 @@ def test_a_large_batch_may_be_the_first_call_of_a_process(batch):
     assert run.returncode == 0, run.stderr[-2000:]
     errors = [float(x) for x in run.stdout.split()]
     assert len(errors) == 5 and max(errors) < 1e-2  # the bound of test_gpu_attention_layer.py: a value in some hundreds on the other side of a tie
+
+
+def test_a_step_that_finds_no_place_is_refused():
+    from paper_2510_16045_amd.attention_layer import DecodeStep
+
+    _, layer = layer_of(3, 2)
+    lens = torch.tensor([2 * PAGE - 2, 5, 0], dtype=torch.int32, device="cuda")
+    step = DecodeStep(layer, lens)
+    x = torch.ones((3, HIDDEN), dtype=torch.float16, device="cuda")
+    for _ in range(2):
+        step(x)
+    before = layer.cache.clone(), lens.tolist()
+    assert before[1] == [2 * PAGE, 7, 2]
+    for _ in range(2):
+        with pytest.raises(ValueError, match="no place"):
+            step(x)
+    torch.cuda.synchronize()
+    assert torch.equal(layer.cache, before[0]) and lens.tolist() == before[1]
+    lens[0] = 0  # the sequence has ended: its slot begins anew
+    for _ in range(2 * PAGE - 7):
+        step(x)
+    assert lens.tolist() == [2 * PAGE - 7, 2 * PAGE, 2 * PAGE - 5]
+    with pytest.raises(ValueError, match="no place"):
+        step(x)
+    lens.copy_(torch.tensor([1, 1, 2 * PAGE - 1], dtype=torch.int32))
+    step(x)
+    lens[1] = 2 * PAGE - 1  # a longer one in its place: the host is told
+    step.recount()
+    with pytest.raises(ValueError, match="no place"):
+        step(x)
+    lens[2] = 3
+    step(x)
+    assert lens.tolist() == [3, 2 * PAGE, 4]
+
+
+def test_sequences_that_are_full_from_the_beginning():
+    from paper_2510_16045_amd.attention_layer import DecodeStep
+
+    _, layer = layer_of(2, 1)
+    lens = torch.tensor([PAGE, 1], dtype=torch.int32, device="cuda")
+    step = DecodeStep(layer, lens)
+    with pytest.raises(ValueError, match="no place"):
+        step(torch.ones((2, HIDDEN), dtype=torch.float16, device="cuda"))
+    assert lens.tolist() == [PAGE, 1]
