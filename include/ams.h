@@ -289,7 +289,8 @@ int ams_read_probe(const void* buf, size_t bytes, uint32_t* sink, void* stream);
  * table_width * page_size, a negative one as 0).  Rows q_starts[b] .. q_starts[b + 1] - 1 of the call's tensors are
  * its LAST rows: with n of them row i has position kv_lens[b] - n + i.  q_starts is ascending, [batch + 1]; NULL: one
  * row per sequence (rows = batch).  Rows that no sequence has are left alone.  Rows with a negative position are
- * not written, read back as zeros, and see no key.
+ * not written, read back as zeros, and see no key where attention is causal; without `causal` a row's position is of
+ * no account.
  *
  * block_table, kv_lens and q_starts are device memory and are read by the kernels only: a captured call follows
  * them from replay to replay, and no entry point waits for the device.  Whatever they hold, nothing outside of the
