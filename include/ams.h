@@ -341,12 +341,19 @@ int ams_kv_read(const ams_kv_cache* cache, uint16_t* K, uint16_t* V, int64_t row
  *   workspace    device, 16-byte aligned, zero-filled once before its first use (the calls leave it ready for the next one,
  *                of any shape), or NULL.  With it the keys of a row may be shared out to several workgroups, which exchange
  *                their parts through it.  ams_kv_attention_workspace_bytes says how much is used at most for such a call
- *                (never more than AMS_KV_WORKSPACE_BYTES); with less, fewer workgroups.  Calls that overlap in time must
- *                not share it.
+ *                (never more than AMS_KV_WORKSPACE_BYTES); with less, fewer workgroups, but not much fewer than without one: where it is
+ *                too small for that it is not used.  Calls that overlap in time must not share it.
  * Deterministic.  Errors: NULL, SHAPE (softmax_scale not above 0 or not finite among them), ALIGN, DEVICE, LAUNCH.
  */
 #define AMS_KV_WORKSPACE_BYTES (64 << 20)
 int ams_kv_attention_workspace_bytes(const ams_kv_cache* cache, int64_t rows, int heads, int64_t max_q_len, size_t* bytes);
+/*
+ * Which kernel and launch shape a call gets, as a short text for logs and tests: "tile ..." (prompts that fill the chip) or "stream ..."
+ * followed by key=value pairs: rows of a workgroup's tile, wavefronts, workgroups, and whether keys may be shared out to several workgroups
+ * (they are where the lengths, which only the device knows, ask for it).  Host only, launches nothing, reads nothing of the device's.
+ */
+int ams_kv_attention_plan(const ams_kv_cache* cache, int64_t rows, int heads, int64_t window, int64_t max_q_len, size_t workspace_bytes,
+                          char* text, size_t text_len);
 int ams_kv_attention(const ams_kv_cache* cache, const uint16_t* Q, uint16_t* O, float* lse, int64_t rows, int heads,
                      int64_t q_stride, int64_t q_head_stride, int64_t o_stride, int64_t o_head_stride, int64_t lse_stride,
                      float softmax_scale, int causal, int64_t window, int64_t max_q_len, void* workspace,

@@ -84,6 +84,7 @@ def load_library():
     lib.ams_kv_block_bytes.argtypes = [_int, _int, _int, ctypes.POINTER(ctypes.c_size_t)]
     lib.ams_kv_write.argtypes = lib.ams_kv_read.argtypes = [ctypes.POINTER(_KvCache), _vp, _vp, *[_i64] * 5, _vp]
     lib.ams_kv_attention_workspace_bytes.argtypes = [ctypes.POINTER(_KvCache), _i64, _int, _i64, ctypes.POINTER(ctypes.c_size_t)]
+    lib.ams_kv_attention_plan.argtypes = [ctypes.POINTER(_KvCache), _i64, _int, _i64, _i64, ctypes.c_size_t, ctypes.c_char_p, ctypes.c_size_t]
     lib.ams_kv_attention.argtypes = [ctypes.POINTER(_KvCache), _vp, _vp, _vp, _i64, _int, *[_i64] * 5, ctypes.c_float, _int, _i64, _i64, _vp, ctypes.c_size_t, _vp]
     lib.ams_read_probe.argtypes = [_vp, ctypes.c_size_t, _vp, _vp]
     _lib = lib
@@ -596,6 +597,14 @@ def ams_kv_attention_workspace_bytes(q, cache, block_table, kv_lens, scale_group
     view = _kv_view(cache, block_table, kv_lens, q_starts, q.shape[-1], scale_group)
     _check(load_library().ams_kv_attention_workspace_bytes(ctypes.byref(view), q.shape[0], q.shape[1], max_q_len or 0, ctypes.byref(out)), "ams_kv_attention_workspace_bytes")
     return out.value
+
+
+def ams_kv_attention_plan(q, cache, block_table, kv_lens, scale_group: int = 32, q_starts=None, max_q_len: int = None, window: int = 0, workspace_bytes: int = KV_WORKSPACE_BYTES) -> str:
+    """Which kernel and launch shape ams_kv_attention would use for such a call with so much workspace."""
+    buf = ctypes.create_string_buffer(256)
+    view = _kv_view(cache, block_table, kv_lens, q_starts, q.shape[-1], scale_group)
+    _check(load_library().ams_kv_attention_plan(ctypes.byref(view), q.shape[0], q.shape[1], window, max_q_len or 0, workspace_bytes, buf, len(buf)), "ams_kv_attention_plan")
+    return buf.value.decode()
 
 
 def ams_kv_attention(q, cache, block_table, kv_lens, scale_group: int = 32, q_starts=None, max_q_len: int = None, softmax_scale: float = None, causal: bool = True, window: int = 0,
