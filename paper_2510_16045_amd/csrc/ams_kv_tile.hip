@@ -36,8 +36,10 @@ struct Block {
 constexpr uint32_t kMissing = 1, kBad = 2;
 template <int RUNS>
 struct Notes {
-  uint32_t what[kBlockTiles], bad[kBlockTiles][RUNS];
+  alignas(16) uint32_t what[kBlockTiles];  // read as one
+  uint32_t bad[kBlockTiles][RUNS];
 };
+static_assert(alignof(Notes<1>) >= alignof(u4) && kBlockTiles == 4, "one read of 16 bytes");
 
 // A tile of K or V on its way through a wavefront.
 template <int D, int G>
