@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 
 from oracle import kv_oracle as O
-from tests.test_gpu_kv_attention import Case, near
+from tests.test_gpu_kv_attention import Case, counts_are_zero, near, workspace  # noqa: F401  (the fixtures of that file)
 from tests.test_gpu_kv_cache import host
 
 torch = pytest.importorskip("torch")
