@@ -129,3 +129,19 @@ def test_the_plan_of_a_call_is_that_of_the_entry_point():
         ams.ams_kv_attention_plan(q[:, :3], *args, q_starts=starts_of([3]))
     with pytest.raises(ams.AmsError):
         ams.ams_kv_attention_plan(q, *args, q_starts=starts_of([3]), window=-1)
+
+
+@pytest.mark.parametrize("count", [1, 80])
+def test_a_pool_beyond_32_bits(count):
+    D, G, page, kv_heads, n = 128, 32, 1024, 8, 1100
+    rng = np.random.default_rng(count)
+    n_pages = (5 << 30) // (kv_heads * ams.ams_kv_block_bytes(D, page, G)) + 1
+    cache = torch.empty((n_pages, kv_heads, ams.ams_kv_block_bytes(D, page, G)), dtype=torch.uint8, device="cuda")
+    assert cache.numel() > 1 << 32
+    k, v, q = (rng.standard_normal((m, h, D)).astype(np.float16) for m, h in ((n, kv_heads), (n, kv_heads), (count, 32)))
+    where = dev(np.array([[n_pages - 1, n_pages // 2 + 1]], dtype=np.int32)), dev(np.array([n], dtype=np.int32))
+    ams.ams_kv_write(cache, dev(k), dev(v), *where, G, q_starts=starts_of([n]))
+    out = host(ams.ams_kv_attention(dev(q), cache, *where, G, q_starts=starts_of([count]), max_q_len=count, workspace=torch.zeros(1 << 20, dtype=torch.uint8, device="cuda")))
+    want, _, size = O.attention(q, O.held(k, G), O.held(v, G), D**-0.5)
+    ok, worst = near(out, want, size, n)
+    assert ok, worst
