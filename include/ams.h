@@ -336,8 +336,8 @@ int ams_kv_read(const ams_kv_cache* cache, uint16_t* K, uint16_t* V, int64_t row
  * the last `window` of these.  fp32 sums and statistics; the weights are rounded to fp16 for the matrix cores, their sum is
  * not.  A row that sees no key gives O = 0, lse = -inf.  A masked key has no effect, whatever it holds.
  *   lse          device [rows][heads] fp32 with rows lse_stride apart, or NULL
- *   max_q_len    the most rows that any sequence has, as far as the caller knows (0: unknown): it chooses between
- *                kernels, results hold whatever it says
+ *   max_q_len    the most rows that any sequence has, as far as the caller knows (0: unknown, reckoned as all rows of the call):
+ *                it chooses between kernels, as table_width does, which stands for the lengths; results hold whatever they say
  *   workspace    device, 16-byte aligned, zero-filled once before its first use (the calls leave it ready for the next one,
  *                of any shape), or NULL.  With it the keys of a row may be shared out to several workgroups, which exchange
  *                their parts through it.  ams_kv_attention_workspace_bytes says how much is used at most for such a call

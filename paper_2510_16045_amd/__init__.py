@@ -612,7 +612,8 @@ def ams_kv_attention(q, cache, block_table, kv_lens, scale_group: int = 32, q_st
     """softmax(softmax_scale * q k^T) v over the cache, fp16 [rows, heads, head_dim] like q (a view too); heads / kv_heads of them share a kv head.
 
     q's rows are the last rows of their sequences, as in ams_kv_write: a row sees the keys up to its own (causal), of these the last
-    `window` if that is not 0.  softmax_scale: head_dim ** -0.5 by default.  max_q_len: the most rows of a sequence, if known.
+    `window` if that is not 0.  softmax_scale: head_dim ** -0.5 by default.  max_q_len: the most rows of a sequence, if
+    known (drafts are faster with it; the table's width stands for the lengths where a kernel is chosen).
     workspace: a uint8 CUDA tensor, zero-filled once, that calls may share one after the other; without one a row's keys are not shared out
     to several workgroups.
     lse: fp32 [rows, heads], receives log(sum(exp(scores)))."""

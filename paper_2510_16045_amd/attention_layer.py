@@ -2,6 +2,7 @@
 
     qkv = ams_linear(x);  ams_kv_write(k, v);  ams_kv_attention(q);  ams_linear(o)
 
+q and k are used as the projection gives them: a model with rotary embeddings rotates them between the projection and ams_kv_write.
 Projections of up to MAX_M rows run on the packed weights; those of prompts restore a matrix to fp16 once and multiply with the
 library GEMM; captured ones of more rows run MAX_M rows at a time.  A decode step of fixed batch is captured as a HIP graph: the sequences' lengths lie on the GPU and grow from replay to
 replay.  ``python -m paper_2510_16045_amd.attention_layer`` runs a prompt and decode steps of a Llama-3-8B-shaped block on
@@ -58,7 +59,9 @@ class AttentionLayer:
         self.workspace = torch.zeros(KV_WORKSPACE_BYTES, dtype=torch.uint8, device="cuda") if workspace is None else workspace
 
     def __call__(self, x, kv_lens, q_starts=None, max_q_len: int = None, out=None):
-        """x fp16 [rows, hidden]: the last rows of sequences of kv_lens[b] tokens, these among them."""
+        """x fp16 [rows, hidden]: the last rows of sequences of kv_lens[b] tokens, these among them.
+
+        max_q_len: the most rows of any of them, where the caller knows (drafts are faster with it)."""
         rows = self.qkv(x).view(-1, self.heads + 2 * self.kv_heads, self.head_dim)
         q, k, v = rows[:, : self.heads], rows[:, self.heads : self.heads + self.kv_heads], rows[:, self.heads + self.kv_heads :]
         ams_kv_write(self.cache, k, v, self.block_table, kv_lens, self.scale_group, q_starts=q_starts)
@@ -69,9 +72,9 @@ class AttentionLayer:
 class DecodeStep:
     """A decode step of a batch as a HIP graph: x in, y out; every replay adds a token to each sequence.
 
-    A step for which a sequence has no place left in its pages is refused.  The host counts the steps from the lengths that it has seen,
-    and looks at kv_lens again, which waits for the GPU, only where the count says that there is no place; whoever makes a sequence longer by hand calls
-    recount()."""
+    A step for which a sequence has no place left in the block table is refused.  The host counts the steps from the lengths that it has
+    seen, and looks at kv_lens again, which waits for the GPU, only where by that count there is no place; whoever makes a sequence
+    longer by hand calls recount()."""
 
     def __init__(self, layer: AttentionLayer, kv_lens):
         import torch

@@ -7,9 +7,9 @@
 // 8 + 4 h .. + 3 (h = lane / 32), and V's fragments are laid out in that order.
 //
 // What bounds it is the issue of instructions, which two wavefronts of a SIMD share: 2048 rows over 8192 keys, 32 query and 8 kv heads of 128
-// channels: 241 Gflop in 254 to 263 us, 0.92 to 0.95 Pflop/s, where a library product of 8192 x 8192 x 8192 reaches 1.16.  In copies with parts taken out:
+// channels: 241 Gflop in 261 to 270 us, 0.89 to 0.92 Pflop/s, where a library product of 8192 x 8192 x 8192 reaches 1.16.  In copies with parts taken out:
 // without restoring 235 us, without S too 165, without O too 136, without the softmax as well 101.  Tiles are never cut: keys of cut
-// tiles were joined through the workspace at 340 us.  With a window of 512, seven sequences of up to 1999 tokens, 16 heads of 64: 40 us.
+// tiles were joined through the workspace at 340 us.  With a window of 512, seven sequences of up to 1999 tokens, 16 heads of 64: 41 us.
 #include "ams_kv_attention.h"
 
 namespace ams_kv {
@@ -252,7 +252,7 @@ __global__ __launch_bounds__(64 * WAVES, tile_waves(D, WAVES)) void tile_kernel(
       for (int i = 0; i < 32; i++) {
         const float v = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 16][i % 16], scale2, -sub));
         sum[i & 1] += v;
-        p[i / 8][i % 8] = (_Float16)v;
+        p[i / 8][i % 8] = (_Float16)v;  // as in stream_kernel
       }
       l += sum[0] + sum[1];
 #pragma unroll
