@@ -287,8 +287,8 @@ int ams_read_probe(const void* buf, size_t bytes, uint32_t* sink, void* stream);
  *
  * Rows.  Sequence b has kv_lens[b] tokens, those of the present call among them (a length is taken as at most
  * table_width * page_size, a negative one as 0).  Rows q_starts[b] .. q_starts[b + 1] - 1 of the call's tensors are
- * its LAST rows: with n of them row i has position kv_lens[b] - n + i.  q_starts is ascending, [batch + 1]; NULL: one
- * row per sequence (rows = batch).  Rows that no sequence has are left alone.  Rows with a negative position are
+ * its LAST rows: with n of them row i has position kv_lens[b] - n + i.  q_starts is ascending, [batch + 1] (of others
+ * rows may be left alone); NULL: one row per sequence (rows = batch).  Rows that no sequence has are left alone.  Rows with a negative position are
  * not written, read back as zeros, and see no key where attention is causal; without `causal` a row's position is of
  * no account.
  *

@@ -49,6 +49,7 @@ struct AttentionArgs {
   Divisor by_group;
   int shares;        // workgroups of one kv head
   int cut;           // whether a tile may lie in several
+  int row_tiles;     // at most so many over all sequences, if row starts ascend
   int part_rows;     // rows of a tile in `parts`
   int causal, window, vec;
 };
@@ -130,11 +131,12 @@ __device__ __forceinline__ Split split_of(const AttentionArgs& a, const Extent& 
   uint32_t tiles = first.row_tiles, steps = first.row_tiles * first.steps, most = first.row_tiles > 0 ? first.steps : 0;
   for (int b0 = 64; b0 < a.v.batch; b0 += 64) {
     const Extent x = extent_of<ROWS>(a, b0 + lane_id());
-    tiles += x.row_tiles, steps += x.row_tiles * x.steps, most = max(most, x.row_tiles > 0 ? (uint32_t)x.steps : 0);
+    tiles = min(tiles + x.row_tiles, 1u << 25), steps += x.row_tiles * x.steps, most = max(most, x.row_tiles > 0 ? (uint32_t)x.steps : 0);
   }
   Split split = {1, 0, 0.0f, a.cut && __ballot(most > (uint32_t)kUncutSteps) != 0};
   const uint32_t shares = (uint32_t)a.shares;
   tiles = wave_sum(tiles), steps = wave_sum(steps);
+  if (tiles > (uint32_t)a.row_tiles) return split;  // starts that do not ascend: there is no bound to the work, and the sums may wrap
   split.total = split.cut ? steps + tiles * kTileSteps : tiles;
   if (split.cut && tiles > 1 && 2 * tiles <= shares) {
     const float each = __builtin_amdgcn_rcpf((float)steps) * 0.9999f;  // rounds down: no more parts than shares

@@ -120,7 +120,7 @@ int ams_kv_attention(const ams_kv_cache* cache, const uint16_t* Q, uint16_t* O, 
   a.causal = causal != 0, a.window = (int)std::min<int64_t>(window, 0x3FFFFFFF);
   a.vec = aligned(Q, 16) && aligned(O, 8) && (q_stride | q_head_stride) % 8 == 0 && (o_stride | o_head_stride) % 4 == 0;
   const Plan p = make_plan(cache, rows, heads, max_q_len, window, workspace ? workspace_bytes : 0);
-  a.shares = (int)p.shares, a.cut = p.cut, a.part_rows = p.part_rows;
+  a.shares = (int)p.shares, a.cut = p.cut, a.row_tiles = (int)p.row_tiles, a.part_rows = p.part_rows;
   const int64_t grid = p.shares * cache->kv_heads;
   if (grid > 0x7FFFFFFF) return AMS_ERR_SHAPE;
   if (p.tile)
