@@ -34,8 +34,8 @@ def test_more_rows_than_there_are(shared, hint):
     assert torch.equal(c.run(workspace=ws), c.run(workspace=None if ws is None else torch.zeros_like(ws)))
 
 
-def test_starts_that_ascend_between_others():
-    # what is out of [0, rows] is taken as its end, and sequences in no order that have no more rows than there are keep theirs
+def test_starts_outside_of_the_rows():
+    # what lies outside of [0, rows] is taken as the nearer of the two
     c = Case([60, 40, 20], [3, 2, 4], heads=2, kv_heads=1)
     want = c.run(workspace=None)
     for starts in ([-3, 3, 5, 9], [0, 3, 5, 1 << 30], [-(1 << 31), 3, 5, 9]):
