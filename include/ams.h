@@ -359,6 +359,51 @@ int ams_kv_attention(const ams_kv_cache* cache, const uint16_t* Q, uint16_t* O, 
                      float softmax_scale, int causal, int64_t window, int64_t max_q_len, void* workspace,
                      size_t workspace_bytes, void* stream);
 
+/*
+ * Rotary positions: rows of Q and K are rotated by their positions, between the projection and ams_kv_write.  Pair i of a head's first
+ * rotary_dim channels, a = x[i], b = x[i + rotary_dim / 2] (interleaved: x[2 i], x[2 i + 1]), at position p becomes
+ *   magnitude * (a cos(p w_i) - b sin(p w_i)),  magnitude * (b cos(p w_i) + a sin(p w_i));
+ * the channels behind them stay as they are.  transposed: the angles are -p w_i, which takes the gradient of the rotated rows to that
+ * of the rows (and rotates back where magnitude is 1).  Products in fp32, one rounding to fp16; any position of 32 bits, negative ones too.
+ *
+ * ams_rope_frequencies  fills turns[rotary_dim / 2] (host): w_i / 2 pi as fractions of 2^64, and what the rows are multiplied with.
+ *   w_i = base^(-2 i / rotary_dim), for contexts `factor` (from 1 on) times the length that a model was trained for:
+ *   AMS_ROPE_LINEAR  w_i / factor
+ *   AMS_ROPE_NTK     of base * factor^(rotary_dim / (rotary_dim - 2))
+ *   AMS_ROPE_BANDS   w_i / factor where the pair makes less than one turn within trained_len, w_i where it makes more than four, between
+ *                    them a mixture that is linear in the turns
+ *   AMS_ROPE_YARN    the same mixture, linear in i, between the pairs that make 32 turns and one; magnitude = 1 + 0.1 ln(factor)
+ *   (magnitude is 1 otherwise; base is at least 1, above it for YARN.)  Errors: NULL, SHAPE.
+ */
+enum { AMS_ROPE_PLAIN = 0, AMS_ROPE_LINEAR = 1, AMS_ROPE_NTK = 2, AMS_ROPE_BANDS = 3, AMS_ROPE_YARN = 4 };
+#define AMS_ROPE_MAX_DIM 1024 /* of a head */
+int ams_rope_frequencies(int rotary_dim, double base, int scaling, double factor, int64_t trained_len, uint64_t* turns, float* magnitude);
+
+typedef struct ams_rotation {
+  const uint64_t* turns;    /* device, [rotary_dim / 2] */
+  const int32_t* positions; /* device, [rows], or NULL: the rows are the last ones of their sequences, as those of the KV cache's calls are */
+  const int32_t* kv_lens;   /* device, [batch] (a negative length is taken as 0) */
+  const int32_t* q_starts;  /* device, [batch + 1], or NULL: one row per sequence (rows = batch).  Rows that no sequence has are left alone */
+  int32_t batch;
+  int32_t rotary_dim;  /* even, up to head_dim */
+  int32_t interleaved, transposed;
+  float magnitude;
+} ams_rotation;
+
+typedef struct ams_rope_rows {
+  const uint16_t* in; /* device, [rows][heads][head_dim] fp16 with the given strides (in values); the channels of a head lie together */
+  uint16_t* out;      /* the same; may be `in` with its strides, but not overlap it otherwise */
+  int64_t in_stride, in_head_stride, out_stride, out_head_stride;
+  int32_t heads;
+} ams_rope_rows;
+
+/*
+ * ams_rope  rotates rows of Q and, if it is not NULL, of K (heads of the same size) in one launch.  Any strides and any 2-byte alignment;
+ * 16-byte aligned rows and multiples of 16 rotated channels (interleaved: 8) are faster.  Positions, lengths and starts are read by the
+ * kernel only: a captured call follows them.  Errors: NULL, SHAPE, ALIGN, DEVICE, LAUNCH.
+ */
+int ams_rope(const ams_rotation* rotation, const ams_rope_rows* Q, const ams_rope_rows* K, int64_t rows, int head_dim, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -29,6 +29,8 @@ SEARCH_REROUND = 1  # AMS_SEARCH_REROUND
 MAX_M = 32
 KV_WORKSPACE_BYTES = 64 << 20  # AMS_KV_WORKSPACE_BYTES
 
+ROPE_SCALINGS = ("none", "linear", "ntk", "bands", "yarn")  # AMS_ROPE_*, in their order
+
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libams.so")
 _lib = None
 
@@ -46,6 +48,18 @@ class _KvCache(ctypes.Structure):
         ("pages", _vp), ("block_table", _vp), ("kv_lens", _vp), ("q_starts", _vp), ("n_pages", _i64), ("table_stride", _i64),
         *((name, ctypes.c_int32) for name in ("table_width", "batch", "kv_heads", "head_dim", "page_size", "scale_group")),
     ]
+
+
+class _Rotation(ctypes.Structure):
+    """ams_rotation of include/ams.h."""
+
+    _fields_ = [(name, _vp) for name in ("turns", "positions", "kv_lens", "q_starts")] + [(name, ctypes.c_int32) for name in ("batch", "rotary_dim", "interleaved", "transposed")] + [("magnitude", ctypes.c_float)]
+
+
+class _RopeRows(ctypes.Structure):
+    """ams_rope_rows of include/ams.h."""
+
+    _fields_ = [("x", _vp), ("out", _vp), *((name, _i64) for name in ("in_stride", "in_head_stride", "out_stride", "out_head_stride")), ("heads", ctypes.c_int32)]
 
 
 def load_library():
@@ -86,6 +100,8 @@ def load_library():
     lib.ams_kv_attention_workspace_bytes.argtypes = [ctypes.POINTER(_KvCache), _i64, _int, _i64, ctypes.POINTER(ctypes.c_size_t)]
     lib.ams_kv_attention_plan.argtypes = [ctypes.POINTER(_KvCache), _i64, _int, _i64, _i64, ctypes.c_size_t, ctypes.c_char_p, ctypes.c_size_t]
     lib.ams_kv_attention.argtypes = [ctypes.POINTER(_KvCache), _vp, _vp, _vp, _i64, _int, *[_i64] * 5, ctypes.c_float, _int, _i64, _i64, _vp, ctypes.c_size_t, _vp]
+    lib.ams_rope_frequencies.argtypes = [_int, ctypes.c_double, _int, ctypes.c_double, _i64, _vp, ctypes.POINTER(ctypes.c_float)]
+    lib.ams_rope.argtypes = [ctypes.POINTER(_Rotation), ctypes.POINTER(_RopeRows), ctypes.POINTER(_RopeRows), _i64, _int, _vp]
     lib.ams_read_probe.argtypes = [_vp, ctypes.c_size_t, _vp, _vp]
     _lib = lib
     return lib
@@ -642,3 +658,50 @@ def ams_kv_attention(q, cache, block_table, kv_lens, scale_group: int = 32, q_st
     )
     _check(rc, "ams_kv_attention")
     return out
+
+
+def ams_rope_frequencies(rotary_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, trained_len: int = 0):
+    """What ams_rope takes of a model's rotary embedding: (turns, magnitude), int64 [rotary_dim / 2] on the host and a float.
+
+    scaling: one of ROPE_SCALINGS, for contexts `factor` times as long as the trained ones; "bands" and "yarn" take that length too."""
+    if scaling not in ROPE_SCALINGS:
+        raise ValueError(f"scaling must be one of {ROPE_SCALINGS}, it is {scaling!r}")
+    turns, magnitude = np.empty(max(rotary_dim // 2, 1), dtype=np.int64), ctypes.c_float(1.0)
+    rc = load_library().ams_rope_frequencies(rotary_dim, base, ROPE_SCALINGS.index(scaling), factor, trained_len, _np_ptr(turns), ctypes.byref(magnitude))
+    _check(rc, "ams_rope_frequencies")
+    return turns, magnitude.value
+
+
+def _rope_rows(x, out, name):
+    if tuple(out.shape) != tuple(x.shape):
+        raise ValueError(f"{name} is {list(x.shape)}, its output {list(out.shape)}")
+    return _RopeRows(_kv_rows(x, name, x.shape[1], x.shape[2]), _kv_rows(out, "out", x.shape[1], x.shape[2]), x.stride(0), x.stride(1), out.stride(0), out.stride(1), x.shape[1])
+
+
+def ams_rope(q, k, turns, positions=None, kv_lens=None, q_starts=None, magnitude: float = 1.0, interleaved: bool = False, transposed: bool = False, out=None):
+    """Rows of q and k (or None), fp16 [rows, heads, head_dim] (views too), rotated by their positions: (q, k) anew, or in out=(q, k), which
+    may be the tensors themselves.
+
+    turns: of ams_rope_frequencies, on the GPU; the first 2 * len(turns) channels of a head are rotated, halves of them paired or
+    (interleaved) neighbours.  positions: int32 [rows]; else the rows are the last ones of sequences of kv_lens tokens, as in
+    ams_kv_write, and rows that none has are left alone.  transposed: by the angles' negatives: takes a gradient back."""
+    import torch
+
+    if q.dim() != 3 or (k is not None and (k.dim() != 3 or k.shape[0] != q.shape[0] or k.shape[2] != q.shape[2])):
+        raise ValueError("q must be [rows, heads, head_dim], and k of as many rows and as wide heads")
+    if (positions is None) == (kv_lens is None) or (q_starts is not None and kv_lens is None):
+        raise ValueError("expected positions, or kv_lens and where sequences have other than one row q_starts")
+    if turns.dim() != 1 or (positions is not None and tuple(positions.shape) != (q.shape[0],)) or (kv_lens is not None and kv_lens.dim() != 1):
+        raise ValueError(f"expected turns [pairs], positions [{q.shape[0]}] or kv_lens [batch]")
+    batch = 0 if kv_lens is None else kv_lens.shape[0]
+    if q_starts is not None and tuple(q_starts.shape) != (batch + 1,):
+        raise ValueError(f"q_starts must have {batch + 1} entries")
+    if out is None:
+        out = torch.empty(q.shape, dtype=torch.float16, device=q.device), None if k is None else torch.empty(k.shape, dtype=torch.float16, device=q.device)
+    if (k is None) != (out[1] is None):
+        raise ValueError("out must hold a tensor for each of q and k")
+    index = lambda t: None if t is None else _dev_ptr(t, torch.int32)  # noqa: E731
+    rotation = _Rotation(_dev_ptr(turns, torch.int64), index(positions), index(kv_lens), index(q_starts), batch, 2 * turns.shape[0], int(interleaved), int(transposed), magnitude)
+    rows = [None if x is None else ctypes.byref(_rope_rows(x, y, name)) for x, y, name in ((q, out[0], "q"), (k, out[1], "k"))]
+    _check(load_library().ams_rope(ctypes.byref(rotation), *rows, q.shape[0], q.shape[2], _stream()), "ams_rope")
+    return tuple(out)

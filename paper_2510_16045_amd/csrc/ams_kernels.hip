@@ -2058,6 +2058,7 @@ int device_status() { return device_state(); }
 bool load_cache();
 bool load_stream();
 bool load_tile();
+bool load_rope();
 }  // namespace ams_kv
 
 extern "C" {
@@ -2072,7 +2073,7 @@ int ams_init(void) {
   if (rc == AMS_OK) rc = prepare_format<FMT_FP5>();
   if (rc == AMS_OK) rc = prepare_format<FMT_FP4>();
   if (rc == AMS_OK) rc = prepare_format<FMT_FP16>();
-  if (rc == AMS_OK && !(ams_kv::load_cache() && ams_kv::load_stream() && ams_kv::load_tile())) rc = AMS_ERR_LAUNCH;
+  if (rc == AMS_OK && !(ams_kv::load_cache() && ams_kv::load_stream() && ams_kv::load_tile() && ams_kv::load_rope())) rc = AMS_ERR_LAUNCH;
   return rc;
 }
 

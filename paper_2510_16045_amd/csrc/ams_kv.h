@@ -241,6 +241,7 @@ inline bool loaded(const void* kernel) {
 bool load_cache();
 bool load_stream();
 bool load_tile();
+bool load_rope();
 
 }  // namespace ams_kv
 #endif

@@ -1,0 +1,227 @@
+// Rotary positions: rows of Q and K rotated by their positions, pair by pair.
+//
+//   y_a = m (x_a cos t - x_b sin t),  y_b = m (x_b cos t + x_a sin t),  t = p w_i
+//
+// for pair i of a head's first `rotary_dim` channels: a, b = i, i + rotary_dim / 2, or 2 i, 2 i + 1 where they are interleaved.
+//
+// The angle.  w_i is given as a fraction of a turn in 64-bit fixed point; p times that modulo 2^64 is the angle modulo a turn, off by
+// p 2^-65 turns at most, where a product of 32-bit floats is off by 0.008 radians at p = 131072.  The upper 32 bits (1.5e-9 radians)
+// are reduced to an eighth of a turn on either side of a quarter, where sin and cos are polynomials: the Taylor series up to x^9 and
+// x^8, whose next terms are below 2e-9 and 3e-8.  So there is no table of cosines to read, and no longest position.
+#include "ams_kv.h"
+
+#include <float.h>
+#include <math.h>
+
+#include <algorithm>
+
+namespace ams_kv {
+
+struct RopeTensor {
+  const uint16_t* in;
+  uint16_t* out;
+  int64_t in_stride, in_head, out_stride, out_head;
+};
+struct RopeArgs {
+  RopeTensor q, k;
+  const uint64_t* turns;
+  const int32_t *positions, *lens, *starts;
+  int64_t rows;
+  float magnitude;
+  int batch, heads, all_heads;  // heads: of q; all_heads: with k's behind them
+  int pairs, rest;              // of a head: pairs, and channels behind them that are copied (0 where they are in place)
+  int chunks;                   // of a head: what one lane takes of it at a time
+  int at_once;                  // heads that a wavefront takes at a time
+  int passes;                   // of a wavefront
+  Divisor by_chunks, by_parts;  // parts: wavefronts of a row
+  int interleaved, transposed;
+};
+
+// The position of a row, the wavefront's own: false where no sequence has it.
+__device__ __forceinline__ bool row_position(const RopeArgs& a, int64_t row, int* position) {
+  if (a.positions) {
+    *position = a.positions[row];
+    return true;
+  }
+  if (!a.starts) {
+    if (row >= a.batch) return false;
+    *position = max(a.lens[row], 0) - 1;
+    return true;
+  }
+  for (int b0 = 0; b0 < a.batch; b0 += 64) {
+    const int b = min(b0 + lane_id(), a.batch - 1);
+    const int first = a.starts[b], end = a.starts[b + 1], len = max(a.lens[b], 0);
+    const unsigned long long found = __ballot(first <= row && row < end);
+    if (found) {
+      *position = (int)((uint32_t)__builtin_amdgcn_readlane(len, __builtin_ctzll(found)) - (uint32_t)__builtin_amdgcn_readlane(end, __builtin_ctzll(found)) + (uint32_t)row);
+      return true;
+    }
+  }
+  return false;
+}
+
+// cos and sin of p times `turn`.
+__device__ __forceinline__ void angle(uint64_t turn, int p, float magnitude, int transposed, float* c, float* s) {
+  const uint32_t low = (uint32_t)turn, high = (uint32_t)(turn >> 32);
+  uint32_t at = (uint32_t)p * high + __umulhi((uint32_t)p, low);  // of a turn, in 2^-32
+  if (p < 0) at -= low;
+  const uint32_t quarter = (at + (1u << 29)) >> 30;
+  const float x = (float)(int)(at - (quarter << 30)) * 1.46291807926715968e-9f;  // 2 pi 2^-32
+  const float xx = x * x;
+  const float sine = x + x * xx * (-1.0f / 6 + xx * (1.0f / 120 + xx * (-1.0f / 5040 + xx * (1.0f / 362880))));
+  const float cosine = 1.0f + xx * (-0.5f + xx * (1.0f / 24 + xx * (-1.0f / 720 + xx * (1.0f / 40320))));
+  const float y = quarter & 1 ? cosine : sine;
+  float z = quarter & 1 ? sine : cosine;
+  if ((quarter + 1) & 2) z = -z;
+  *c = magnitude * z;
+  *s = magnitude * (((quarter >> 1) ^ (uint32_t)transposed) & 1 ? -y : y);
+}
+
+__device__ __forceinline__ void turn_pair(_Float16& a, _Float16& b, float c, float s) {
+  const float x = (float)a, y = (float)b;
+  a = (_Float16)(x * c - y * s);
+  b = (_Float16)(y * c + x * s);
+}
+
+// A wavefront takes heads of one row, `at_once` of them side by side; its lanes keep their angles for all of them.  WIDE: a lane
+// has pieces of eight channels (two where they are halves of pairs); else one pair, or one channel that is copied.
+template <bool WIDE, bool INTERLEAVED>
+__global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
+  constexpr int PAIRS = !WIDE ? 1 : INTERLEAVED ? 4 : 8;
+  const int lane = lane_id();
+  const uint32_t unit = blockIdx.x * 4 + (uint32_t)__builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const uint32_t row = a.by_parts.quotient(unit), part = unit - row * a.by_parts.by;
+  if (row >= a.rows) return;
+  int position;
+  if (!row_position(a, row, &position)) return;
+  const int turned = a.pairs / PAIRS;  // of the chunks
+  const int sub = (int)a.by_chunks.quotient((uint32_t)lane), first_head = (int)part * a.passes * a.at_once + sub;
+  if (sub >= a.at_once) return;
+  for (int chunk = lane - sub * a.chunks; chunk < a.chunks; chunk += 64) {
+    float c[PAIRS], s[PAIRS];
+    if (chunk < turned) {
+#pragma unroll
+      for (int i = 0; i < PAIRS; i++) angle(a.turns[chunk * PAIRS + i], position, a.magnitude, a.transposed, &c[i], &s[i]);
+    }
+    for (int pass = 0; pass < a.passes; pass++) {
+      const int head = first_head + pass * a.at_once;
+      if (head >= a.all_heads) break;
+      const RopeTensor& t = head < a.heads ? a.q : a.k;
+      const int h = head < a.heads ? head : head - a.heads;
+      const uint16_t* const in = t.in + (int64_t)row * t.in_stride + (int64_t)h * t.in_head;
+      uint16_t* const out = t.out + (int64_t)row * t.out_stride + (int64_t)h * t.out_head;
+      if constexpr (WIDE) {
+        if (chunk >= turned) {
+          const int at = 2 * a.pairs + (chunk - turned) * 8;
+          *(u4*)(out + at) = *(const u4*)(in + at);
+        } else if constexpr (INTERLEAVED) {
+          h8 x = *(const h8*)(in + chunk * 8);
+#pragma unroll
+          for (int i = 0; i < 4; i++) {
+            _Float16 p = x[2 * i], q = x[2 * i + 1];
+            turn_pair(p, q, c[i], s[i]);
+            x[2 * i] = p, x[2 * i + 1] = q;
+          }
+          *(h8*)(out + chunk * 8) = x;
+        } else {
+          h8 x = *(const h8*)(in + chunk * 8), y = *(const h8*)(in + a.pairs + chunk * 8);
+#pragma unroll
+          for (int i = 0; i < 8; i++) {
+            _Float16 p = x[i], q = y[i];
+            turn_pair(p, q, c[i], s[i]);
+            x[i] = p, y[i] = q;
+          }
+          *(h8*)(out + chunk * 8) = x, *(h8*)(out + a.pairs + chunk * 8) = y;
+        }
+      } else {
+        if (chunk >= turned) {
+          out[a.pairs + chunk] = in[a.pairs + chunk];
+        } else {
+          const int i = INTERLEAVED ? 2 * chunk : chunk, j = INTERLEAVED ? i + 1 : i + a.pairs;
+          _Float16 x = __builtin_bit_cast(_Float16, in[i]), y = __builtin_bit_cast(_Float16, in[j]);
+          turn_pair(x, y, c[0], s[0]);
+          out[i] = __builtin_bit_cast(uint16_t, x), out[j] = __builtin_bit_cast(uint16_t, y);
+        }
+      }
+    }
+  }
+}
+
+bool load_rope() { return loaded((const void*)rope_kernel<true, false>); }
+
+}  // namespace ams_kv
+
+using namespace ams_kv;
+
+extern "C" {
+
+int ams_rope_frequencies(int rotary_dim, double base, int scaling, double factor, int64_t trained_len, uint64_t* turns, float* magnitude) {
+  if (!turns || !magnitude) return AMS_ERR_NULL;
+  if (rotary_dim < 2 || rotary_dim > AMS_ROPE_MAX_DIM || rotary_dim % 2 || !(base >= 1) || !(base <= 1e30)) return AMS_ERR_SHAPE;
+  if (scaling < AMS_ROPE_PLAIN || scaling > AMS_ROPE_YARN) return AMS_ERR_SHAPE;
+  if (scaling != AMS_ROPE_PLAIN && (!(factor >= 1) || !(factor <= 1e9))) return AMS_ERR_SHAPE;
+  if ((scaling == AMS_ROPE_BANDS || scaling == AMS_ROPE_YARN) && (trained_len < 1 || trained_len > INT32_MAX)) return AMS_ERR_SHAPE;
+  if (scaling == AMS_ROPE_YARN && !(base > 1)) return AMS_ERR_SHAPE;
+  constexpr double kTurn = 6.283185307179586476925;
+  const double r = rotary_dim, len = (double)trained_len;
+  if (scaling == AMS_ROPE_NTK && rotary_dim > 2) base *= pow(factor, r / (r - 2));
+  double lo = 0, hi = 0;
+  if (scaling == AMS_ROPE_YARN) {  // the pair that makes n turns within the trained length
+    auto pair = [&](double n) { return r * log(len / (kTurn * n)) / (2 * log(base)); };
+    lo = std::max(floor(pair(32)), 0.0), hi = std::min(ceil(pair(1)), r - 1);
+  }
+  for (int i = 0; i < rotary_dim / 2; i++) {
+    double w = pow(base, -2.0 * i / r), kept = 1;
+    if (scaling == AMS_ROPE_LINEAR) kept = 0;
+    if (scaling == AMS_ROPE_BANDS) kept = std::min(1.0, std::max(0.0, (len * w / kTurn - 1) / 3));
+    if (scaling == AMS_ROPE_YARN) kept = 1 - std::min(1.0, std::max(0.0, (i - lo) / std::max(hi - lo, 0.001)));
+    if (kept < 1) w = kept * w + (1 - kept) * w / factor;
+    turns[i] = (uint64_t)ldexp(w / kTurn, 64);  // below a sixth of a turn
+  }
+  *magnitude = scaling == AMS_ROPE_YARN ? (float)(0.1 * log(factor) + 1) : 1.0f;
+  return AMS_OK;
+}
+
+int ams_rope(const ams_rotation* rotation, const ams_rope_rows* Q, const ams_rope_rows* K, int64_t rows, int head_dim, void* stream) {
+  if (!rotation || !Q) return AMS_ERR_NULL;
+  const ams_rotation& r = *rotation;
+  if (rows < 0 || rows > AMS_KV_MAX_TOKENS || head_dim < 1 || head_dim > AMS_ROPE_MAX_DIM || r.rotary_dim < 2 || r.rotary_dim % 2 || r.rotary_dim > head_dim) return AMS_ERR_SHAPE;
+  if (Q->heads < 1 || Q->heads > AMS_KV_MAX_HEADS || (K && (K->heads < 1 || K->heads > AMS_KV_MAX_HEADS)) || r.batch < 0 || r.batch > AMS_KV_MAX_BATCH) return AMS_ERR_SHAPE;
+  if (!(fabsf(r.magnitude) <= FLT_MAX) || (!r.positions && !r.q_starts && rows != r.batch)) return AMS_ERR_SHAPE;
+  if (!r.turns || (rows > 0 && (!Q->in || !Q->out || (K && (!K->in || !K->out)))) || (!r.positions && r.batch > 0 && !r.kv_lens)) return AMS_ERR_NULL;
+  if (!aligned(r.turns, 8) || !aligned(r.positions, 4) || !aligned(r.kv_lens, 4) || !aligned(r.q_starts, 4)) return AMS_ERR_ALIGN;
+  bool wide = (r.interleaved ? r.rotary_dim : r.rotary_dim / 2) % 8 == 0, in_place = true;
+  for (const ams_rope_rows* t : {Q, K}) {
+    if (!t) continue;
+    if (!aligned(t->in, 2) || !aligned(t->out, 2)) return AMS_ERR_ALIGN;
+    wide = wide && aligned(t->in, 16) && aligned(t->out, 16) && (t->in_stride | t->in_head_stride | t->out_stride | t->out_head_stride) % 8 == 0;
+    in_place = in_place && t->in == t->out && t->in_stride == t->out_stride && t->in_head_stride == t->out_head_stride;
+  }
+  if (const int rc = device_status(); rc != AMS_OK) return rc;
+  if (rows == 0 || (!r.positions && r.batch == 0)) return AMS_OK;
+  RopeArgs a = {};
+  a.q = {Q->in, Q->out, Q->in_stride, Q->in_head_stride, Q->out_stride, Q->out_head_stride};
+  if (K) a.k = {K->in, K->out, K->in_stride, K->in_head_stride, K->out_stride, K->out_head_stride};
+  a.turns = r.turns, a.positions = r.positions, a.lens = r.kv_lens, a.starts = r.q_starts, a.rows = rows, a.magnitude = r.magnitude;
+  a.batch = r.batch, a.heads = Q->heads, a.all_heads = Q->heads + (K ? K->heads : 0);
+  a.pairs = r.rotary_dim / 2, a.rest = in_place ? 0 : head_dim - r.rotary_dim;
+  wide = wide && a.rest % 8 == 0;
+  const int pairs = !wide ? 1 : r.interleaved ? 4 : 8;
+  a.chunks = a.pairs / pairs + a.rest / (wide ? 8 : 1);
+  a.at_once = std::max(64 / a.chunks, 1);
+  const int64_t turns = (a.all_heads + a.at_once - 1) / a.at_once;
+  constexpr int64_t kWavefronts = 8192;
+  const int64_t parts = std::min(std::max<int64_t>(kWavefronts / rows, 1), turns);
+  a.passes = (int)((turns + parts - 1) / parts);
+  a.by_chunks = divisor((uint32_t)a.chunks), a.by_parts = divisor((uint32_t)((turns + a.passes - 1) / a.passes));
+  a.interleaved = r.interleaved != 0, a.transposed = r.transposed != 0;
+  const unsigned grid = (unsigned)((rows * a.by_parts.by + 3) / 4);
+  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, (hipStream_t)stream, a); };
+  if (wide)
+    r.interleaved ? launch(rope_kernel<true, true>) : launch(rope_kernel<true, false>);
+  else
+    r.interleaved ? launch(rope_kernel<false, true>) : launch(rope_kernel<false, false>);
+  return hipGetLastError() == hipSuccess ? AMS_OK : AMS_ERR_LAUNCH;
+}
+
+}  // extern "C"
