@@ -404,6 +404,29 @@ typedef struct ams_rope_rows {
  */
 int ams_rope(const ams_rotation* rotation, const ams_rope_rows* Q, const ams_rope_rows* K, int64_t rows, int head_dim, void* stream);
 
+/*
+ * Log probabilities of tokens, behind the vocabulary projection.  With x = logits / temperature, lse = log sum exp(x) over a row:
+ *   logprob[r]       x[tokens[r]] - lse; 0 where the token is not in [0, vocab) (a padded row)
+ *   rank[r]          how many logits are ahead of the token's: larger ones, and equal ones with a lower index; -1 where there is no token
+ *   entropy[r]       lse - sum p x, p = exp(x - lse)
+ *   top_tokens[r][i] the `top` most likely tokens in falling order, of equally likely ones the lower index first (-1 where the row has fewer);
+ *   top_logprobs[r][i] their log probabilities
+ * A logit of -inf has probability 0 and log probability -inf, in a row that has no other too (its entropy is 0).  In a row with a NaN or
+ * +inf log probabilities and entropy are NaN; a NaN is never among the top tokens nor ahead of one, and the rank of a token with a NaN is 0.
+ *   logits     device, [rows][vocab] of AMS_TYPE_*, rows `stride` values apart, any alignment of its type
+ *   tokens     device, [rows], or NULL (then logprob and rank are NULL too); logprob, rank and entropy may be NULL, top may be 0
+ *   workspace  as ams_kv_attention's, which may be the same: with it a row may be shared out to several workgroups
+ *              (ams_logprobs_workspace_bytes says how much that takes; with less it is not used)
+ * fp32 sums.  Deterministic.  Errors: NULL, SHAPE (temperature outside of 1e-6 to 1e6 among them), ALIGN, DEVICE, LAUNCH.
+ */
+enum { AMS_TYPE_FP16 = 0, AMS_TYPE_FP32 = 1 };
+#define AMS_LOGPROBS_MAX_TOP 64
+#define AMS_LOGPROBS_MAX_VOCAB (1 << 28)
+int ams_logprobs_workspace_bytes(int type, int64_t rows, int64_t vocab, int top, size_t* bytes);
+int ams_logprobs(const void* logits, int type, int64_t rows, int64_t vocab, int64_t stride, const int32_t* tokens, float temperature, int top,
+                 float* logprob, int32_t* rank, float* entropy, float* top_logprobs, int32_t* top_tokens, void* workspace,
+                 size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -8,6 +8,7 @@ native binding, which needs torch's headers, the same calls go through ctypes.
 
 from __future__ import annotations
 
+import collections
 import ctypes
 import functools
 import importlib.machinery
@@ -28,6 +29,7 @@ SEARCH_SET_BIT = 0  # AMS_SEARCH_SET_BIT
 SEARCH_REROUND = 1  # AMS_SEARCH_REROUND
 MAX_M = 32
 KV_WORKSPACE_BYTES = 64 << 20  # AMS_KV_WORKSPACE_BYTES
+MAX_TOP = 64  # AMS_LOGPROBS_MAX_TOP
 
 ROPE_SCALINGS = ("none", "linear", "ntk", "bands", "yarn")  # AMS_ROPE_*, in their order
 
@@ -102,6 +104,8 @@ def load_library():
     lib.ams_kv_attention.argtypes = [ctypes.POINTER(_KvCache), _vp, _vp, _vp, _i64, _int, *[_i64] * 5, ctypes.c_float, _int, _i64, _i64, _vp, ctypes.c_size_t, _vp]
     lib.ams_rope_frequencies.argtypes = [_int, ctypes.c_double, _int, ctypes.c_double, _i64, _vp, ctypes.POINTER(ctypes.c_float)]
     lib.ams_rope.argtypes = [ctypes.POINTER(_Rotation), ctypes.POINTER(_RopeRows), ctypes.POINTER(_RopeRows), _i64, _int, _vp]
+    lib.ams_logprobs_workspace_bytes.argtypes = [_int, _i64, _i64, _int, ctypes.POINTER(ctypes.c_size_t)]
+    lib.ams_logprobs.argtypes = [_vp, _int, _i64, _i64, _i64, _vp, ctypes.c_float, _int, *[_vp] * 6, ctypes.c_size_t, _vp]
     lib.ams_read_probe.argtypes = [_vp, ctypes.c_size_t, _vp, _vp]
     _lib = lib
     return lib
@@ -705,3 +709,59 @@ def ams_rope(q, k, turns, positions=None, kv_lens=None, q_starts=None, magnitude
     rows = [None if x is None else ctypes.byref(_rope_rows(x, y, name)) for x, y, name in ((q, out[0], "q"), (k, out[1], "k"))]
     _check(load_library().ams_rope(ctypes.byref(rotation), *rows, q.shape[0], q.shape[2], _stream()), "ams_rope")
     return tuple(out)
+
+
+LogProbs = collections.namedtuple("LogProbs", "logprob rank entropy top_logprobs top_tokens")
+LogProbs.__doc__ = """What ams_logprobs gives: of each row's token log probability (fp32) and rank (int32), the row's entropy, and its most
+likely tokens (int32) [rows, top] with their log probabilities."""
+
+
+def _logits_type(logits):
+    import torch
+
+    if logits.dim() != 2:
+        raise ValueError("logits must be [rows, vocab]")
+    if logits.dtype not in (torch.float16, torch.float32):
+        raise TypeError(f"expected {torch.float16} or {torch.float32}, got {logits.dtype}")
+    return int(logits.dtype == torch.float32)  # AMS_TYPE_*
+
+
+def ams_logprobs_workspace_bytes(logits, top: int = 0) -> int:
+    """Bytes of workspace that ams_logprobs uses for such a call; may be 0."""
+    out = ctypes.c_size_t(0)
+    _check(load_library().ams_logprobs_workspace_bytes(_logits_type(logits), *logits.shape, top, ctypes.byref(out)), "ams_logprobs_workspace_bytes")
+    return out.value
+
+
+def ams_logprobs(logits, tokens=None, top: int = 0, temperature: float = 1.0, workspace=None, out=None):
+    """Log probabilities behind the vocabulary projection: LogProbs of logits [rows, vocab], fp16 or fp32 (rows may be strided).
+
+    tokens: int32 [rows], whose log probability and rank are asked for (None: both are None; a token outside of the vocabulary has 0 and
+    -1).  top: how many of the most likely tokens (up to MAX_TOP).  temperature divides the logits.
+    workspace: a uint8 CUDA tensor, zero-filled once, as ams_kv_attention's (it may be the same); without one each row is
+    one workgroup's.  out: a LogProbs of tensors to write; those that are None are not worked out."""
+    import torch
+
+    kind, (rows, vocab) = _logits_type(logits), logits.shape
+    if not logits.is_cuda or (vocab > 1 and logits.stride(1) != 1):
+        raise ValueError("logits must be a CUDA tensor whose last dimension is contiguous")
+    if _devices != 1:
+        _check_device(logits)
+    if tokens is not None and tuple(tokens.shape) != (rows,):
+        raise ValueError(f"tokens must have {rows} entries")
+    if out is None:
+        reals = lambda *n: torch.empty(n, dtype=torch.float32, device=logits.device)  # noqa: E731
+        wholes = lambda *n: torch.empty(n, dtype=torch.int32, device=logits.device)  # noqa: E731
+        out = LogProbs(*((None, None) if tokens is None else (reals(rows), wholes(rows))), reals(rows), reals(rows, max(top, 0)), wholes(rows, max(top, 0)))
+    pointers = []
+    for name, t in zip(LogProbs._fields, out):
+        shape = (rows, top) if name.startswith("top") else (rows,)
+        if t is not None and tuple(t.shape) != shape:
+            raise ValueError(f"{name} must be {list(shape)}, it is {list(t.shape)}")
+        pointers.append(None if t is None else _dev_ptr(t, torch.int32 if name in ("rank", "top_tokens") else torch.float32))
+    rc = load_library().ams_logprobs(
+        logits.data_ptr(), kind, rows, vocab, logits.stride(0), None if tokens is None else _dev_ptr(tokens, torch.int32), temperature, top, *pointers,
+        _dev_ptr(workspace, torch.uint8) if workspace is not None else None, workspace.numel() if workspace is not None else 0, _stream()
+    )
+    _check(rc, "ams_logprobs")
+    return LogProbs(*out)

@@ -242,6 +242,7 @@ bool load_cache();
 bool load_stream();
 bool load_tile();
 bool load_rope();
+bool load_logprobs();
 
 }  // namespace ams_kv
 #endif
