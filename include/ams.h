@@ -360,6 +360,26 @@ int ams_kv_attention(const ams_kv_cache* cache, const uint16_t* Q, uint16_t* O, 
                      size_t workspace_bytes, void* stream);
 
 /*
+ * The same with the scores that other models are trained with.  With p the row's position and t = softmax_scale * Q[r, h] . K[j]:
+ *   softcap      > 0: t becomes softcap * tanh(t / softcap)
+ *   slopes       device, [heads] fp32, or NULL: then slopes[h] * |p - j| is taken off it
+ *   prefix_lens  device, [batch], or NULL (causal only): every row of sequence b that has a position (p >= 0) sees the keys
+ *                j < prefix_lens[b] of those that there are, also those behind it and those that its window has left behind
+ * in this order; fp32, the hyperbolic tangent to 2^-22.  `scores` NULL, or one that asks for none of them, is ams_kv_attention.  The
+ * workspace and what ams_kv_attention_plan says are the same for both.  Errors: as ams_kv_attention; SHAPE for a softcap below 0 or not
+ * finite, or for prefix_lens without causal.
+ */
+typedef struct ams_kv_scores {
+  const float* slopes;
+  const int32_t* prefix_lens;
+  float softcap; /* 0: none */
+} ams_kv_scores;
+int ams_kv_attention_scored(const ams_kv_cache* cache, const ams_kv_scores* scores, const uint16_t* Q, uint16_t* O, float* lse, int64_t rows, int heads,
+                            int64_t q_stride, int64_t q_head_stride, int64_t o_stride, int64_t o_head_stride, int64_t lse_stride,
+                            float softmax_scale, int causal, int64_t window, int64_t max_q_len, void* workspace, size_t workspace_bytes,
+                            void* stream);
+
+/*
  * Rotary positions: rows of Q and K are rotated by their positions, between the projection and ams_kv_write.  Pair i of a head's first
  * rotary_dim channels, a = x[i], b = x[i + rotary_dim / 2] (interleaved: x[2 i], x[2 i + 1]), at position p becomes
  *   magnitude * (a cos(p w_i) - b sin(p w_i)),  magnitude * (b cos(p w_i) + a sin(p w_i));

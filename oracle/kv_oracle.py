@@ -51,3 +51,36 @@ def attention(q, k, v, scale, causal=True, window=0):
         size[some, h] = p @ np.abs(vh) / total
         lse[some, h] = (top + np.log(total))[:, 0]
     return out, lse, size
+
+
+def scored_attention(q, k, v, scale, causal=True, window=0, softcap=0.0, slopes=None, prefix=0, heads=None):
+    """attention with capped scores, a bias by distance (slopes [heads]) and keys below `prefix` that every row with a position sees; of
+    q's heads only `heads`, if given.  q may have more rows than there are keys: the first ones have no position."""
+    n, all_heads, D = q.shape
+    length, kv_heads, _ = k.shape
+    position = np.arange(length - n, length)[:, None]
+    key = np.arange(length)[None, :]
+    seen = np.ones((n, length), dtype=bool)
+    if causal:
+        seen = (key <= position) & (key > position - (window or length + n))
+        seen |= (key < prefix) & (position >= 0)
+    heads = range(all_heads) if heads is None else heads
+    out, size, lse = np.zeros((n, len(heads), D)), np.zeros((n, len(heads), D)), np.full((n, len(heads)), -np.inf)
+    some = seen.any(1)
+    if not some.any():
+        return out, lse, size
+    for i, h in enumerate(heads):
+        kh, vh = k[:, h * kv_heads // all_heads], v[:, h * kv_heads // all_heads]
+        s = q[:, h].astype(np.float64) @ kh.T * scale
+        if softcap:
+            s = softcap * np.tanh(s / softcap)
+        if slopes is not None:
+            s = s - float(slopes[h]) * np.abs(position - key)
+        s = np.where(seen, s, -np.inf)[some]
+        top = s.max(-1, keepdims=True)
+        p = np.exp(s - top)
+        total = p.sum(-1, keepdims=True)
+        out[some, i] = p @ vh / total
+        size[some, i] = p @ np.abs(vh) / total
+        lse[some, i] = (top + np.log(total))[:, 0]
+    return out, lse, size

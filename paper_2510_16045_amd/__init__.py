@@ -52,6 +52,12 @@ class _KvCache(ctypes.Structure):
     ]
 
 
+class _KvScores(ctypes.Structure):
+    """ams_kv_scores of include/ams.h."""
+
+    _fields_ = [("slopes", _vp), ("prefix_lens", _vp), ("softcap", ctypes.c_float)]
+
+
 class _Rotation(ctypes.Structure):
     """ams_rotation of include/ams.h."""
 
@@ -102,6 +108,7 @@ def load_library():
     lib.ams_kv_attention_workspace_bytes.argtypes = [ctypes.POINTER(_KvCache), _i64, _int, _i64, ctypes.POINTER(ctypes.c_size_t)]
     lib.ams_kv_attention_plan.argtypes = [ctypes.POINTER(_KvCache), _i64, _int, _i64, _i64, ctypes.c_size_t, ctypes.c_char_p, ctypes.c_size_t]
     lib.ams_kv_attention.argtypes = [ctypes.POINTER(_KvCache), _vp, _vp, _vp, _i64, _int, *[_i64] * 5, ctypes.c_float, _int, _i64, _i64, _vp, ctypes.c_size_t, _vp]
+    lib.ams_kv_attention_scored.argtypes = [ctypes.POINTER(_KvCache), ctypes.POINTER(_KvScores), *lib.ams_kv_attention.argtypes[1:]]
     lib.ams_rope_frequencies.argtypes = [_int, ctypes.c_double, _int, ctypes.c_double, _i64, _vp, ctypes.POINTER(ctypes.c_float)]
     lib.ams_rope.argtypes = [ctypes.POINTER(_Rotation), ctypes.POINTER(_RopeRows), ctypes.POINTER(_RopeRows), _i64, _int, _vp]
     lib.ams_logprobs_workspace_bytes.argtypes = [_int, _i64, _i64, _int, ctypes.POINTER(ctypes.c_size_t)]
@@ -628,7 +635,7 @@ def ams_kv_attention_plan(q, cache, block_table, kv_lens, scale_group: int = 32,
 
 
 def ams_kv_attention(q, cache, block_table, kv_lens, scale_group: int = 32, q_starts=None, max_q_len: int = None, softmax_scale: float = None, causal: bool = True, window: int = 0,
-                     workspace=None, out=None, lse=None):
+                     workspace=None, out=None, lse=None, softcap: float = 0.0, slopes=None, prefix_lens=None):
     """softmax(softmax_scale * q k^T) v over the cache, fp16 [rows, heads, head_dim] like q (a view too); heads / kv_heads of them share a kv head.
 
     q's rows are the last rows of their sequences, as in ams_kv_write: a row sees the keys up to its own (causal), of these the last
@@ -636,8 +643,11 @@ def ams_kv_attention(q, cache, block_table, kv_lens, scale_group: int = 32, q_st
     known (drafts are faster with it; the table's width stands for the lengths where a kernel is chosen).
     workspace: a uint8 CUDA tensor, zero-filled once, that calls may share one after the other; without one a row's keys are not shared out
     to several workgroups.
-    lse: fp32 [rows, heads], receives log(sum(exp(scores)))."""
-    if out is not None and _kv_call(_KV_ATTENTION, cache, block_table, kv_lens, scale_group, q_starts, q, out, max_q_len, softmax_scale, causal, window, workspace, lse):
+    lse: fp32 [rows, heads], receives log(sum(exp(scores))).
+    softcap: scores become softcap * tanh(score / softcap) where it is not 0.  slopes: fp32 [heads]: slopes[h] times the distance of the key
+    from the row is taken off them, behind the cap.  prefix_lens: int32 [batch] (causal): keys from a sequence's first on that all of its rows see."""
+    scored = bool(softcap) or slopes is not None or prefix_lens is not None
+    if out is not None and not scored and _kv_call(_KV_ATTENTION, cache, block_table, kv_lens, scale_group, q_starts, q, out, max_q_len, softmax_scale, causal, window, workspace, lse):
         return out
     import torch
 
@@ -655,8 +665,12 @@ def ams_kv_attention(q, cache, block_table, kv_lens, scale_group: int = 32, q_st
         raise TypeError("lse must be a float32 CUDA tensor")
     if lse is not None and _devices != 1:
         _check_device(lse)
-    rc = load_library().ams_kv_attention(
-        ctypes.byref(view), _kv_rows(q, "q", heads, head_dim), _kv_rows(out, "out", heads, head_dim), lse.data_ptr() if lse is not None else None, rows, heads, q.stride(0), q.stride(1),
+    for name, t, n in (("slopes", slopes, heads), ("prefix_lens", prefix_lens, block_table.shape[0])):
+        if t is not None and tuple(t.shape) != (n,):
+            raise ValueError(f"{name} must have {n} entries, it is {list(t.shape)}")
+    scores = _KvScores(None if slopes is None else _dev_ptr(slopes, torch.float32), None if prefix_lens is None else _dev_ptr(prefix_lens, torch.int32), softcap)
+    rc = load_library().ams_kv_attention_scored(
+        ctypes.byref(view), ctypes.byref(scores), _kv_rows(q, "q", heads, head_dim), _kv_rows(out, "out", heads, head_dim), lse.data_ptr() if lse is not None else None, rows, heads, q.stride(0), q.stride(1),
         out.stride(0), out.stride(1), lse.stride(0) if lse is not None else 0, head_dim**-0.5 if softmax_scale is None else softmax_scale, int(causal), window, max_q_len or 0,
         _dev_ptr(workspace, torch.uint8) if workspace is not None else None, workspace.numel() if workspace is not None else 0, _stream()
     )

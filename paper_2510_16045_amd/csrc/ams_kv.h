@@ -241,6 +241,8 @@ inline bool loaded(const void* kernel) {
 bool load_cache();
 bool load_stream();
 bool load_tile();
+bool load_scored_stream();
+bool load_scored_tile();
 bool load_rope();
 bool load_logprobs();
 

@@ -19,6 +19,8 @@
 #ifndef AMS_KV_ATTENTION_H_
 #define AMS_KV_ATTENTION_H_
 
+#include <type_traits>
+
 #include "ams_kv.h"
 
 namespace ams_kv {
@@ -54,13 +56,40 @@ struct AttentionArgs {
   int causal, window, vec;
 };
 
+// Scores other than softmax_scale q . k: capped, biased by distance, or with keys at the sequence's beginning that every row sees.  Kernels
+// for them are instances of their own, so that the others keep their registers and instructions.
+struct ScoredArgs : AttentionArgs {
+  const float* slopes;       // [heads], or null
+  const int32_t* prefixes;   // [batch], or null
+  float cap2, to_cap;        // cap log2(e), 0 without one; 2 log2(e) softmax_scale / cap
+};
+template <typename Args>
+constexpr bool kScored = __is_same(Args, ScoredArgs);
+
+// Keys from the first on that every row with a position sees.
+__device__ __forceinline__ int prefix_of(const ScoredArgs& a, int b, int len) { return a.prefixes ? min(max(a.prefixes[b], 0), len) : 0; }
+
+// The score, in log2, of a row's product with a key.  cap tanh(x / cap) = cap - 2 cap / (exp(2 x / cap) + 1): off by 2^-23 of the cap, which is
+// less than the rounding of a weight to fp16 (2^-11) by far, and right at both ends, where the exponential is 0 or infinite.
+__device__ __forceinline__ float capped(const ScoredArgs& a, float x) {
+  const float e = __builtin_amdgcn_exp2f(x * a.to_cap);
+  return __builtin_fmaf(-2.0f * a.cap2, __builtin_amdgcn_rcpf(e + 1.0f), a.cap2);
+}
+
 // What one sequence contributes: rows, row tiles and steps of keys.
 struct Extent {
   int start, n, len, lo, row_tiles, steps;  // lo: first key (a multiple of kStep) that any row may see
 };
-template <int ROWS>
-__device__ __forceinline__ Extent extent_of(const AttentionArgs& a, int b) {
-  Extent e = {0, 0, 0, 0, 0, 0};
+struct ScoredExtent : Extent {
+  int prefix;  // keys that every row sees; lo is the first of the others
+  // Steps of the prefix that lie before lo: a sequence's steps are these, and those from lo on.
+  __device__ __forceinline__ int prefix_steps() const { return min((prefix + kStep - 1) / kStep, lo / kStep); }
+};
+template <typename Args>
+using ExtentOf = std::conditional_t<kScored<Args>, ScoredExtent, Extent>;
+template <int ROWS, typename Args>
+__device__ __forceinline__ ExtentOf<Args> extent_of(const Args& a, int b) {
+  ExtentOf<Args> e = {};
   if (b >= a.v.batch) return e;
   e.start = row_start(a.v, b);
   e.n = max(row_start(a.v, b + 1) - e.start, 0);
@@ -68,7 +97,9 @@ __device__ __forceinline__ Extent extent_of(const AttentionArgs& a, int b) {
   const int first = e.len - e.n;  // position of the first row
   e.lo = a.window > 0 ? max(first + 1 - a.window, 0) & ~(kStep - 1) : 0;
   e.row_tiles = (int)(((uint32_t)e.n * (uint32_t)a.group + ROWS - 1) / ROWS);
-  e.steps = max((e.len - e.lo + kStep - 1) / kStep, 1);  // one also where there is no key: somebody has to say so
+  e.steps = (e.len - e.lo + kStep - 1) / kStep;
+  if constexpr (kScored<Args>) e.prefix = prefix_of(a, b, e.len), e.steps += e.prefix_steps();
+  e.steps = max(e.steps, 1);  // one also where there is no key: somebody has to say so
   return e;
 }
 
@@ -126,11 +157,11 @@ __device__ __forceinline__ uint32_t tile_cost(const Extent& e, const Split& spli
   if (!split.cut) return 1;
   return split.pieces > 0 ? (uint32_t)((float)e.steps * split.pieces) + 1 : e.steps + kTileSteps;
 }
-template <int ROWS>
-__device__ __forceinline__ Split split_of(const AttentionArgs& a, const Extent& first) {  // first: of the first 64 sequences
+template <int ROWS, typename Args>
+__device__ __forceinline__ Split split_of(const Args& a, const ExtentOf<Args>& first) {  // first: of the first 64 sequences
   uint32_t tiles = first.row_tiles, steps = first.row_tiles * first.steps, most = first.row_tiles > 0 ? first.steps : 0;
   for (int b0 = 64; b0 < a.v.batch; b0 += 64) {
-    const Extent x = extent_of<ROWS>(a, b0 + lane_id());
+    const auto x = extent_of<ROWS>(a, b0 + lane_id());
     tiles = min(tiles + x.row_tiles, 1u << 25), steps += x.row_tiles * x.steps, most = max(most, x.row_tiles > 0 ? (uint32_t)x.steps : 0);
   }
   Split split = {1, 0, 0.0f, a.cut && __ballot(most > (uint32_t)kUncutSteps) != 0};
@@ -145,7 +176,7 @@ __device__ __forceinline__ Split split_of(const AttentionArgs& a, const Extent& 
       split.pieces = fminf((float)(shares - spare) * each, 1.0f / kMinShare);
       uint32_t parts = first.row_tiles * tile_cost(first, split);
       for (int b0 = 64; b0 < a.v.batch; b0 += 64) {
-        const Extent x = extent_of<ROWS>(a, b0 + lane_id());
+        const auto x = extent_of<ROWS>(a, b0 + lane_id());
         parts += x.row_tiles * tile_cost(x, split);
       }
       split.total = wave_sum(parts);
@@ -157,13 +188,14 @@ __device__ __forceinline__ Split split_of(const AttentionArgs& a, const Extent& 
 }
 
 // The row tile that the cost `at` of the whole falls on, where its own begins and how much it is.
+template <typename Args>
 struct Place {
-  Extent e;
+  ExtentOf<Args> e;
   int b, row_tile;
   uint32_t first, cost;
 };
-template <int ROWS>
-__device__ __forceinline__ bool place_of(const AttentionArgs& a, Extent e, const Split& split, uint32_t at, Place* out) {  // e: of the first 64 sequences
+template <int ROWS, typename Args>
+__device__ __forceinline__ bool place_of(const Args& a, ExtentOf<Args> e, const Split& split, uint32_t at, Place<Args>* out) {  // e: of the first 64 sequences
   uint32_t before = 0;
   for (int b0 = 0; b0 < a.v.batch; b0 += 64) {
     if (b0 > 0) e = extent_of<ROWS>(a, b0 + lane_id());
@@ -177,7 +209,8 @@ __device__ __forceinline__ bool place_of(const AttentionArgs& a, Extent e, const
       out->cost = of_lane(each, lane);
       out->row_tile = (at - first) / out->cost;
       out->first = first + out->row_tile * out->cost;
-      out->e = {of_lane(e.start, lane), of_lane(e.n, lane), of_lane(e.len, lane), of_lane(e.lo, lane), of_lane(e.row_tiles, lane), of_lane(e.steps, lane)};
+      (Extent&)out->e = {of_lane(e.start, lane), of_lane(e.n, lane), of_lane(e.len, lane), of_lane(e.lo, lane), of_lane(e.row_tiles, lane), of_lane(e.steps, lane)};
+      if constexpr (kScored<Args>) out->e.prefix = of_lane(e.prefix, lane);
       return true;
     }
     before = of_lane(end, 63);
@@ -344,8 +377,19 @@ __device__ __forceinline__ void join_pending(const AttentionArgs& a, int pending
 // Workgroups of a compute unit: what the registers allow (a fourth one where 16 rows of 128 channels leave room gains nothing; four column
 // tiles of 128 channels: two 40 us, one 42, at 16 sequences of 3001, 8 kv heads and 64 rows).
 constexpr int stream_groups(int d, int qt, int waves) { return waves == 8 ? 1 : d * qt <= 128 ? 3 : 2; }
-void launch_stream(const AttentionArgs& a, int head_dim, int scale_group, int qt, int waves, unsigned grid, hipStream_t stream);  // 8 only up to D = 128, there for any qt, below for qt = 1
-void launch_tile(const AttentionArgs& a, int head_dim, int scale_group, int waves, unsigned grid, hipStream_t stream);  // 8 only up to D = 128
+// 8 waves only up to D = 128, of stream_kernel there for any qt, below for qt = 1.
+template <typename Args>
+void launch_stream(const Args& a, int head_dim, int scale_group, int qt, int waves, unsigned grid, hipStream_t stream);
+template <typename Args>
+void launch_tile(const Args& a, int head_dim, int scale_group, int waves, unsigned grid, hipStream_t stream);
+template <>
+void launch_stream<AttentionArgs>(const AttentionArgs&, int, int, int, int, unsigned, hipStream_t);
+template <>
+void launch_stream<ScoredArgs>(const ScoredArgs&, int, int, int, int, unsigned, hipStream_t);
+template <>
+void launch_tile<AttentionArgs>(const AttentionArgs&, int, int, int, unsigned, hipStream_t);
+template <>
+void launch_tile<ScoredArgs>(const ScoredArgs&, int, int, int, unsigned, hipStream_t);
 
 }  // namespace ams_kv
 #endif

@@ -77,6 +77,14 @@ Plan make_plan(const ams_kv_cache* c, int64_t rows, int heads, int64_t max_q_len
   return p;
 }
 
+template <typename Args>
+static void launch(const Args& a, const Plan& p, const ams_kv_cache* cache, unsigned grid, hipStream_t stream) {
+  if (p.tile)
+    launch_tile(a, cache->head_dim, cache->scale_group, p.waves, grid, stream);
+  else
+    launch_stream(a, cache->head_dim, cache->scale_group, p.qt, p.waves, grid, stream);
+}
+
 }  // namespace ams_kv
 
 using namespace ams_kv;
@@ -105,17 +113,28 @@ int ams_kv_attention_plan(const ams_kv_cache* cache, int64_t rows, int heads, in
 int ams_kv_attention(const ams_kv_cache* cache, const uint16_t* Q, uint16_t* O, float* lse, int64_t rows, int heads, int64_t q_stride, int64_t q_head_stride,
                      int64_t o_stride, int64_t o_head_stride, int64_t lse_stride, float softmax_scale, int causal, int64_t window, int64_t max_q_len,
                      void* workspace, size_t workspace_bytes, void* stream) {
-  AttentionArgs a;
+  return ams_kv_attention_scored(cache, nullptr, Q, O, lse, rows, heads, q_stride, q_head_stride, o_stride, o_head_stride, lse_stride, softmax_scale, causal, window, max_q_len, workspace,
+                                 workspace_bytes, stream);
+}
+
+int ams_kv_attention_scored(const ams_kv_cache* cache, const ams_kv_scores* scores, const uint16_t* Q, uint16_t* O, float* lse, int64_t rows, int heads, int64_t q_stride,
+                            int64_t q_head_stride, int64_t o_stride, int64_t o_head_stride, int64_t lse_stride, float softmax_scale, int causal, int64_t window, int64_t max_q_len,
+                            void* workspace, size_t workspace_bytes, void* stream) {
+  ScoredArgs a;
   if (const int rc = make_view(cache, rows, &a.v); rc != AMS_OK) return rc;
   if (rows > 0 && (!Q || !O)) return AMS_ERR_NULL;
   if (heads < 1 || heads % cache->kv_heads || heads > AMS_KV_MAX_HEADS || window < 0 || (window > 0 && !causal) || max_q_len < 0 || !(softmax_scale > 0) || !(softmax_scale <= FLT_MAX)) return AMS_ERR_SHAPE;
   if (rows * (heads / cache->kv_heads) > AMS_KV_MAX_TOKENS) return AMS_ERR_SHAPE;
-  if (!aligned(Q, 2) || !aligned(O, 2) || !aligned(lse, 4) || !aligned(workspace, 16)) return AMS_ERR_ALIGN;
+  constexpr float kLog2e = 1.44269504089f;
+  const ams_kv_scores none = {nullptr, nullptr, 0}, &x = scores ? *scores : none;
+  a.slopes = x.slopes, a.prefixes = x.prefix_lens, a.cap2 = x.softcap * kLog2e, a.to_cap = x.softcap > 0 ? 2 * kLog2e * softmax_scale / x.softcap : 0;
+  if (!(x.softcap >= 0) || !(a.cap2 <= FLT_MAX / 4) || !(a.to_cap <= FLT_MAX) || (x.prefix_lens && !causal)) return AMS_ERR_SHAPE;
+  if (!aligned(Q, 2) || !aligned(O, 2) || !aligned(lse, 4) || !aligned(workspace, 16) || !aligned(x.slopes, 4) || !aligned(x.prefix_lens, 4)) return AMS_ERR_ALIGN;
   if (const int rc = device_status(); rc != AMS_OK) return rc;
   if (rows == 0 || cache->batch == 0) return AMS_OK;
   a.q = Q, a.out = O, a.lse = lse, a.counts = (uint32_t*)workspace, a.parts = (float*)((uint8_t*)workspace + kCountBytes);
   a.q_stride = q_stride, a.q_head = q_head_stride, a.out_stride = o_stride, a.out_head = o_head_stride, a.lse_stride = lse_stride;
-  a.scale2 = softmax_scale * 1.44269504089f;
+  a.scale2 = softmax_scale * kLog2e;
   a.group = heads / cache->kv_heads, a.by_group = divisor((uint32_t)a.group);
   a.causal = causal != 0, a.window = (int)std::min<int64_t>(window, 0x3FFFFFFF);
   a.vec = aligned(Q, 16) && aligned(O, 8) && (q_stride | q_head_stride) % 8 == 0 && (o_stride | o_head_stride) % 4 == 0;
@@ -123,10 +142,10 @@ int ams_kv_attention(const ams_kv_cache* cache, const uint16_t* Q, uint16_t* O, 
   a.shares = (int)p.shares, a.cut = p.cut, a.row_tiles = (int)p.row_tiles, a.part_rows = p.part_rows;
   const int64_t grid = p.shares * cache->kv_heads;
   if (grid > 0x7FFFFFFF) return AMS_ERR_SHAPE;
-  if (p.tile)
-    launch_tile(a, cache->head_dim, cache->scale_group, p.waves, (unsigned)grid, (hipStream_t)stream);
+  if (x.softcap > 0 || x.slopes || x.prefix_lens)
+    launch(a, p, cache, (unsigned)grid, (hipStream_t)stream);
   else
-    launch_stream(a, cache->head_dim, cache->scale_group, p.qt, p.waves, (unsigned)grid, (hipStream_t)stream);
+    launch<AttentionArgs>(a, p, cache, (unsigned)grid, (hipStream_t)stream);
   return hipGetLastError() == hipSuccess ? AMS_OK : AMS_ERR_LAUNCH;
 }
 

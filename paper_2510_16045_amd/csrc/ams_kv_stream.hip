@@ -15,17 +15,33 @@
 // 16 sequences of 3001 tokens, 64 and 8 heads, tiles of 40 rows: 57 MB in 27 us; 560 instructions a step, 11 us of them.
 #include "ams_kv_attention.h"
 
+#ifndef AMS_KV_SCORED  // 1: the kernels for capped, biased and prefix scores
+#define AMS_KV_SCORED 0
+#endif
+
 namespace ams_kv {
+
+// The steps of a share of a tile, in the order of their keys: all from the first on; or, of scores with a prefix, `before` ones from `first`
+// on and the others from `next` on.
+template <typename Args>
+struct Steps {
+  __device__ __forceinline__ int at(int i) const { return i; }
+};
+template <>
+struct Steps<ScoredArgs> {
+  int first, before, next;
+  __device__ __forceinline__ int at(int i) const { return i < before ? first + i : next + i - before; }
+};
 
 // The pages of 64 steps of a wavefront, one step to a lane: looked up together, read lane by lane.
 struct Pages {
   int number[2];  // of each tile of the step: -1 where the table names no page
-  __device__ __forceinline__ void look_up(const AttentionArgs& a, int b, int step, int to) {
+  __device__ __forceinline__ void look_up(const AttentionArgs& a, int b, int step, bool there) {
 #pragma unroll
     for (int t = 0; t < 2; t++) {
       const uint32_t page = a.v.page_tiles.quotient((uint32_t)(2 * step + t));
       int found = -1;
-      if (step < to && page < (uint32_t)a.v.table_width) found = a.v.table[b * a.v.table_stride + page];
+      if (there && page < (uint32_t)a.v.table_width) found = a.v.table[b * a.v.table_stride + page];
       number[t] = (uint32_t)found < (uint32_t)a.v.n_pages ? found : -1;
     }
   }
@@ -72,9 +88,9 @@ struct StepV {
 // Runs of V that stand for NaN take part in a step's products as zeros where not every row sees every key of the step, and the rows
 // that do see one get the NaN here.  So do runs whose scale is none that ams_kv_write stores (bits above kTopScale): they lie where no row has been
 // written, where a pool may hold anything, and a value that is no fp16 value any more would turn the 0 of a key that is not seen into a
-// NaN as well.  stage: the scales of the step's two tiles; begin, end: the keys that a lane's row sees.
-template <int RUNS, int G, int QT, int DT>
-__device__ __forceinline__ void nan_of_seen_keys(uint8_t* stage, int lane, int first_key, const int (&begin)[QT], const int (&end)[QT], f4 (&o)[DT][QT]) {
+// NaN as well.  stage: the scales of the step's two tiles; begin, end: the keys that a lane's row sees, beside those below `below`.
+template <int RUNS, int G, int QT, int DT, bool SCORED>
+__device__ __forceinline__ void nan_of_seen_keys(uint8_t* stage, int lane, int first_key, const int (&begin)[QT], const int (&end)[QT], const int (&below)[QT], f4 (&o)[DT][QT]) {
   const int g = lane >> 4;
   uint32_t bad[RUNS], any = 0;  // of the step's 32 keys those whose run stands for NaN; first a lane's eight
 #pragma unroll
@@ -100,7 +116,8 @@ __device__ __forceinline__ void nan_of_seen_keys(uint8_t* stage, int lane, int f
 #pragma unroll
     for (int t = 0; t < QT; t++) {
       const int from = min(max(begin[t] - first_key, 0), 32), to = min(max(end[t] - first_key, 0), 32);
-      const uint32_t seen = (uint32_t)((1ull << to) - 1) & ~(uint32_t)((1ull << from) - 1);
+      uint32_t seen = (uint32_t)((1ull << to) - 1) & ~(uint32_t)((1ull << from) - 1);
+      if constexpr (SCORED) seen |= (uint32_t)((1ull << min(max(below[t] - first_key, 0), 32)) - 1);
       if (bad[run] & seen) {
 #pragma unroll
         for (int d = run * G / 16; d < (run + 1) * G / 16; d++) o[d][t] = f4{NAN, NAN, NAN, NAN};
@@ -110,8 +127,9 @@ __device__ __forceinline__ void nan_of_seen_keys(uint8_t* stage, int lane, int f
   wave_sync();
 }
 
-template <int D, int G, int QT, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, stream_groups(D, QT, WAVES) * WAVES / 4) void stream_kernel(AttentionArgs a) {
+template <int D, int G, int QT, int WAVES, typename Args>
+__global__ __launch_bounds__(64 * WAVES, stream_groups(D, QT, WAVES) * WAVES / 4) void stream_kernel(Args a) {
+  constexpr bool SCORED = kScored<Args>;
   constexpr int ROWS = 16 * QT, RUNS = D / G, DT = D / 16, KB = D / 32, AT_ONCE = DT < 8 ? DT : 8;
   const int wave = uniform((int)threadIdx.x >> 6), lane = lane_id();
   const int share = (int)a.v.heads.quotient(blockIdx.x), head = blockIdx.x - share * a.v.kv_heads;
@@ -125,17 +143,17 @@ __global__ __launch_bounds__(64 * WAVES, stream_groups(D, QT, WAVES) * WAVES / 4
   uint8_t* const stage = shared + Q_BYTES + wave * STAGE;
   f4* const parts = (f4*)shared;
 
-  const Extent first_64 = extent_of<ROWS>(a, lane);
+  const auto first_64 = extent_of<ROWS>(a, lane);
   const Split split = split_of<ROWS>(a, first_64);
   uint32_t now = share * split.per;
   const uint32_t stop = min(now + split.per, split.total);
   const __amdgpu_buffer_rsrc_t left = __builtin_amdgcn_make_buffer_rsrc((void*)(a.parts + (int64_t)uniform(head) * 2 * a.shares * a.part_rows * (D + 4)), 0,
                                                                         a.cut ? 2 * a.shares * a.part_rows * (D + 4) * 4 : 0, 0x00020000);  // this head's parts
-  Place place;
+  Place<Args> place;
   Pending left_first = {}, left_last = {};
   int pending = 0;
   while (now < stop && place_of<ROWS>(a, first_64, split, now, &place)) {
-    const Extent& e = place.e;
+    const auto& e = place.e;
     const int rows = e.n * a.group, row0 = place.row_tile * ROWS;
     // the share's steps of the tile that some row sees, and the keys that every row sees
     const uint32_t then = min(place.first + place.cost, stop);
@@ -153,11 +171,26 @@ __global__ __launch_bounds__(64 * WAVES, stream_groups(D, QT, WAVES) * WAVES / 4
     const bool alone = begin_step == 0 && end_step == e.steps;
     const int last_row = min(row0 + ROWS, rows) - 1;
     const int p_first = e.len - e.n + (int)a.by_group.quotient((uint32_t)row0), p_last = e.len - e.n + (int)a.by_group.quotient((uint32_t)last_row);
-    const int from = uniform(max(e.lo / kStep + begin_step, key_begin(a, p_first) / kStep));
-    const int to = uniform(min(e.lo / kStep + end_step, (key_end(a, e.len, p_last) + kStep - 1) / kStep));
+    int from, to;
+    Steps<Args> steps;
+    if constexpr (SCORED) {
+      // of the share: steps with keys of the prefix, and those behind them that some row of the tile sees
+      const int pre = e.prefix_steps(), prefix_end = (e.prefix + kStep - 1) / kStep;
+      steps.first = uniform(begin_step), steps.before = uniform(max(min(end_step, prefix_end) - begin_step, 0));
+      steps.next = uniform(max(max(e.lo / kStep + max(begin_step, pre) - pre, key_begin(a, p_first) / kStep), prefix_end));
+      const int stop_at = min(e.lo / kStep + max(end_step, pre) - pre, (key_end(a, e.len, p_last) + kStep - 1) / kStep);
+      from = 0, to = uniform(steps.before + max(stop_at - steps.next, 0));
+    } else {
+      from = uniform(max(e.lo / kStep + begin_step, key_begin(a, p_first) / kStep));
+      to = uniform(min(e.lo / kStep + end_step, (key_end(a, e.len, p_last) + kStep - 1) / kStep));
+    }
     const int whole_begin = uniform(key_begin(a, p_last)), whole_end = uniform(key_end(a, e.len, p_first));
+    int prefix = 0;  // keys that every row with a position sees
+    if constexpr (SCORED) prefix = e.prefix;
+    const int whole_prefix = p_first >= 0 ? prefix : 0;
     Pages pages;
-    pages.look_up(a, place.b, from + wave + WAVES * hidden(lane), to);
+    auto look_up = [&](int i) { pages.look_up(a, place.b, steps.at(i), i < to); };
+    look_up(from + wave + WAVES * hidden(lane));
     // the tile's rows: a lane has one of each column tile
     const int load_lane = hidden(lane);
 #pragma unroll
@@ -197,6 +230,39 @@ __global__ __launch_bounds__(64 * WAVES, stream_groups(D, QT, WAVES) * WAVES / 4
         }
       }
     };
+    // Of scored calls S is the score in log2 already.
+    const float unit = SCORED ? 1.0f : a.scale2;
+    float slope[QT], place_of_row[QT];  // of a lane's row: its slope (log2), and its position less the lane's first key of a step from key 0 on
+    if constexpr (SCORED) {
+      const int mine = hidden(lane);
+#pragma unroll
+      for (int t = 0; t < QT; t++) {
+        const int r = min(row0 + 16 * t + (mine & 15), rows - 1), token = (int)a.by_group.quotient((uint32_t)r);
+        slope[t] = a.slopes ? a.slopes[head * a.group + r - token * a.group] * 1.44269504089f : 0.0f;
+        place_of_row[t] = (float)(e.len - e.n + token - 4 * (mine >> 4));
+      }
+    }
+    auto score = [&](f4(&s)[2][QT], int step) {
+      if constexpr (SCORED) {
+        if (a.cap2 > 0) {
+#pragma unroll
+          for (int t = 0; t < QT; t++)
+#pragma unroll
+            for (int i = 0; i < 8; i++) s[i / 4][t][i % 4] = capped(a, s[i / 4][t][i % 4]);
+        } else {
+#pragma unroll
+          for (int t = 0; t < QT; t++) s[0][t] *= a.scale2, s[1][t] *= a.scale2;
+        }
+        if (a.slopes) {
+#pragma unroll
+          for (int t = 0; t < QT; t++) {
+            const float ahead = place_of_row[t] - (float)(step * kStep);
+#pragma unroll
+            for (int i = 0; i < 8; i++) s[i / 4][t][i % 4] = __builtin_fmaf(-slope[t], fabsf(ahead - (float)(16 * (i / 4) + i % 4)), s[i / 4][t][i % 4]);
+          }
+        }
+      }
+    };
     // P from S, and the statistics.  The maximum is raised only where a score passes it by more than the slack, then for all lanes that
     // share the row.
     auto weights = [&](f4(&s)[2][QT], h8(&p)[QT]) {
@@ -205,7 +271,7 @@ __global__ __launch_bounds__(64 * WAVES, stream_groups(D, QT, WAVES) * WAVES / 4
         float top = s[0][t][0];
 #pragma unroll
         for (int i = 1; i < 8; i++) top = fmaxf(top, s[i / 4][t][i % 4]);
-        top *= a.scale2;
+        top *= unit;
         if (__ballot(top - m[t] > kSlack)) {
           top = fmaxf(top, m[t]);
           top = larger(with_32(larger(with_16(top))));
@@ -216,10 +282,10 @@ __global__ __launch_bounds__(64 * WAVES, stream_groups(D, QT, WAVES) * WAVES / 4
 #pragma unroll
           for (int d = 0; d < DT; d++) o[d][t] *= less;
         }
-        float scale2 = a.scale2, sub = m[t] == -INFINITY ? 0.0f : m[t] - kLift;
+        float scale2 = unit, sub = m[t] == -INFINITY ? 0.0f : m[t] - kLift;
         if (far) {
 #pragma unroll
-          for (int i = 0; i < 8; i++) s[i / 4][t][i % 4] = below_top(s[i / 4][t][i % 4], a.scale2, m[t]);
+          for (int i = 0; i < 8; i++) s[i / 4][t][i % 4] = below_top(s[i / 4][t][i % 4], unit, m[t]);
           scale2 = 1.0f, sub = -kLift;
         }
 #pragma unroll
@@ -258,30 +324,34 @@ __global__ __launch_bounds__(64 * WAVES, stream_groups(D, QT, WAVES) * WAVES / 4
     };
     // The next step's keys are asked for as soon as this one's have been used, and its values then; behind the last step that one's
     // again, so that what is waited for is always the older request.
-    int step = from + wave, at = 0;
-    if (step < to) {
+    int turn = from + wave, at = 0;
+    if (turn < to) {
+
       StepK<D, G> k;
       StepV<D, G> v;
 #pragma unroll
       for (int u = 0; u < 2; u++) {
-        const Tile tile(a, pages, head, step, u, 0);
+        const Tile tile(a, pages, head, steps.at(turn), u, 0);
         k.load(a, tile, u, lane), v.load(a, tile, u, lane);
       }
       for (;;) {
+        const int step = steps.at(turn);
         f4 s[2][QT];
         h8 p[QT];
         scores(k, s);
+        score(s, step);
         const bool held[2] = {of_lane(pages.number[0], at) >= 0, of_lane(pages.number[1], at) >= 0};
-        const bool whole = step * kStep >= whole_begin && (step + 1) * kStep <= whole_end && held[0] && held[1];  // every row sees every key
-        const bool more = step + WAVES < to;
+        const auto inside = [&] { return step * kStep >= whole_begin && (step + 1) * kStep <= whole_end; };
+        const bool whole = (SCORED ? inside() || (step + 1) * kStep <= whole_prefix : inside()) && held[0] && held[1];  // every row sees every key
+        const bool more = turn + WAVES < to;
         if (more && ++at == 64) {
           at = 0;
-          pages.look_up(a, place.b, step + WAVES + WAVES * hidden(lane), to);
+          look_up(turn + WAVES + WAVES * hidden(lane));
         }
-        const int next = more ? step + WAVES : step;
+        const int next_turn = more ? turn + WAVES : turn, next = steps.at(next_turn);
         const Tile t0(a, pages, head, next, 0, at), t1(a, pages, head, next, 1, at);
         k.load(a, t0, 0, lane), k.load(a, t1, 1, lane);
-        int begin[QT], end[QT];
+        int begin[QT], end[QT], below[QT];  // below: of the keys of the prefix
         if (!whole) {
           const int mine = hidden(lane), key = step * kStep + 4 * (mine >> 4);
 #pragma unroll
@@ -289,20 +359,21 @@ __global__ __launch_bounds__(64 * WAVES, stream_groups(D, QT, WAVES) * WAVES / 4
             const int r = row0 + 16 * t + (mine & 15), position = e.len - e.n + (int)a.by_group.quotient((uint32_t)r);
             begin[t] = r < rows ? key_begin(a, position) : 0;
             end[t] = r < rows ? key_end(a, e.len, position) : 0;
+            below[t] = SCORED && r < rows && position >= 0 ? prefix : 0;
 #pragma unroll
             for (int u = 0; u < 2; u++)
 #pragma unroll
               for (int i = 0; i < 4; i++)
-                if (key + 16 * u + i < begin[t] || key + 16 * u + i >= end[t] || !held[u]) s[u][t][i] = -INFINITY;
+                if (((key + 16 * u + i < begin[t] || key + 16 * u + i >= end[t]) && (!SCORED || key + 16 * u + i >= below[t])) || !held[u]) s[u][t][i] = -INFINITY;
           }
         }
         weights(s, p);
         put_scales(v);
-        if (!whole) nan_of_seen_keys<RUNS, G, QT, DT>(stage, hidden(lane), step * kStep, begin, end, o);
+        if (!whole) nan_of_seen_keys<RUNS, G, QT, DT, SCORED>(stage, hidden(lane), step * kStep, begin, end, below, o);
         multiply(v, p, [&](int u, int run) { return *(const u2*)(stage + ((u * 4 + (lane >> 4)) * RUNS + run) * 8); });
         v.load(a, t0, 0, lane), v.load(a, t1, 1, lane);
         if (!more) break;
-        step = next;
+        turn = next_turn;
       }
     }
 
@@ -366,24 +437,31 @@ __global__ __launch_bounds__(64 * WAVES, stream_groups(D, QT, WAVES) * WAVES / 4
   join_pending<D, 64 * WAVES, QT == 1 ? 1 : 4, QT == 1 ? 8 : 4>(a, pending, left_first, left_last, left, share, head, (float*)shared, all_there);
 }
 
-bool load_stream() { return loaded((const void*)stream_kernel<64, 32, 1, 4>); }
+#if AMS_KV_SCORED
+using Args = ScoredArgs;
+bool load_scored_stream() { return loaded((const void*)stream_kernel<64, 32, 1, 4, Args>); }
+#else
+using Args = AttentionArgs;
+bool load_stream() { return loaded((const void*)stream_kernel<64, 32, 1, 4, Args>); }
+#endif
 
-void launch_stream(const AttentionArgs& a, int head_dim, int scale_group, int qt, int waves, unsigned grid, hipStream_t stream) {
+template <>
+void launch_stream<Args>(const Args& a, int head_dim, int scale_group, int qt, int waves, unsigned grid, hipStream_t stream) {
   dispatch(head_dim, scale_group, [&](auto d, auto g) {
     constexpr int D = decltype(d)::value, G = decltype(g)::value;
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * waves), 0, stream, a); };
     if constexpr (D == 128) {
-      if (waves == 8 && qt == 2) return launch(stream_kernel<D, G, 2, 8>);
-      if (waves == 8 && qt == 3) return launch(stream_kernel<D, G, 3, 8>);
-      if (waves == 8 && qt == 4) return launch(stream_kernel<D, G, 4, 8>);
+      if (waves == 8 && qt == 2) return launch(stream_kernel<D, G, 2, 8, Args>);
+      if (waves == 8 && qt == 3) return launch(stream_kernel<D, G, 3, 8, Args>);
+      if (waves == 8 && qt == 4) return launch(stream_kernel<D, G, 4, 8, Args>);
     }
     if constexpr (D < 256) {
-      if (waves == 8 && qt == 1) return launch(stream_kernel<D, G, 1, 8>);
-      if (qt == 3) return launch(stream_kernel<D, G, 3, 4>);
-      if (qt == 4) return launch(stream_kernel<D, G, 4, 4>);  // 256 accumulators do not fit beside the rows
+      if (waves == 8 && qt == 1) return launch(stream_kernel<D, G, 1, 8, Args>);
+      if (qt == 3) return launch(stream_kernel<D, G, 3, 4, Args>);
+      if (qt == 4) return launch(stream_kernel<D, G, 4, 4, Args>);  // 256 accumulators do not fit beside the rows
     }
-    if (qt == 1) return launch(stream_kernel<D, G, 1, 4>);
-    launch(stream_kernel<D, G, 2, 4>);
+    if (qt == 1) return launch(stream_kernel<D, G, 1, 4, Args>);
+    launch(stream_kernel<D, G, 2, 4, Args>);
   });
 }
 

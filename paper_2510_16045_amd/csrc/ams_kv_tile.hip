@@ -12,6 +12,10 @@
 // tiles were joined through the workspace at 340 us.  With a window of 512, seven sequences of up to 1999 tokens, 16 heads of 64: 41 us.
 #include "ams_kv_attention.h"
 
+#ifndef AMS_KV_SCORED  // 1: the kernels for capped, biased and prefix scores
+#define AMS_KV_SCORED 0
+#endif
+
 namespace ams_kv {
 
 typedef float f16v __attribute__((ext_vector_type(16)));
@@ -116,25 +120,38 @@ struct Job {
   }
 };
 
-template <int D, int G, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, tile_waves(D, WAVES)) void tile_kernel(AttentionArgs a) {
+template <int D, int G, int WAVES, typename Args>
+__global__ __launch_bounds__(64 * WAVES, tile_waves(D, WAVES)) void tile_kernel(Args a) {
+  constexpr bool SCORED = kScored<Args>;
   constexpr int ROWS = 32 * WAVES, RUNS = D / G, KF = D / 16, DT = D / 32, JOBS = 2 * kBlockTiles / WAVES, AHEAD = ahead(D, WAVES);
   const int wave = uniform((int)threadIdx.x >> 6), lane = lane_id(), h = lane >> 5, col = lane & 31;
   const int share = (int)a.v.heads.quotient(blockIdx.x), head = blockIdx.x - share * a.v.kv_heads;
   __shared__ Block<D> blocks[2];
   __shared__ Notes<RUNS> notes[2];
-  const Extent first_64 = extent_of<ROWS>(a, lane);
+  const auto first_64 = extent_of<ROWS>(a, lane);
   const Split split = split_of<ROWS>(a, first_64);  // a tile each
-  Place place;
+  Place<Args> place;
   // the tiles with the most keys are a sequence's last: they go first
   if ((uint32_t)share < split.total && place_of<ROWS>(a, first_64, split, split.total - 1 - share, &place)) {
-    const Extent& e = place.e;
+    const auto& e = place.e;
     const int rows = e.n * a.group, tile_row = place.row_tile * ROWS, row0 = tile_row + 32 * wave;
     auto position = [&](int r) { return e.len - e.n + (int)a.by_group.quotient((uint32_t)r); };
     // the keys that some row of the tile sees, from a cache tile on
-    const int key_from = uniform(key_begin(a, position(tile_row)) & ~(kTile - 1));
+    int key_from = uniform(key_begin(a, position(tile_row)) & ~(kTile - 1));
     const int key_to = uniform(key_end(a, e.len, position(min(tile_row + ROWS, rows) - 1)));
-    const int n_blocks = max((key_to - key_from + kBlock - 1) / kBlock, 0);
+    int n_blocks = max((key_to - key_from + kBlock - 1) / kBlock, 0);
+    // A prefix that all rows see: its blocks come first, where there are keys between it and the others that no row sees.
+    int prefix = 0, prefix_blocks = 0, keys_end = key_to;
+    if constexpr (SCORED) {
+      prefix = uniform(position(min(tile_row + ROWS, rows) - 1) < 0 ? 0 : e.prefix), prefix_blocks = (prefix + kBlock - 1) / kBlock;
+      keys_end = max(key_to, prefix);
+      if (prefix > 0 && key_from <= prefix_blocks * kBlock) prefix_blocks = key_from = 0;
+      n_blocks = prefix_blocks + max((keys_end - key_from + kBlock - 1) / kBlock, 0);
+    }
+    auto first_key = [&](int block) {
+      if constexpr (SCORED) return block < prefix_blocks ? block * kBlock : key_from + (block - prefix_blocks) * kBlock;
+      return key_from + block * kBlock;
+    };
     // of those the ones that every row and that no row of the wavefront sees
     const bool idle = row0 >= rows;
     const int p_first = position(row0), p_last = position(min(row0 + 32, rows) - 1);
@@ -142,6 +159,16 @@ __global__ __launch_bounds__(64 * WAVES, tile_waves(D, WAVES)) void tile_kernel(
     const int some_begin = uniform(key_begin(a, p_first)), some_end = uniform(idle ? 0 : min(key_end(a, e.len, p_last), key_to));
     const int r = row0 + col;
     const int row_begin = key_begin(a, position(r)), row_end = r < rows ? min(key_end(a, e.len, position(r)), key_to) : 0;
+    // The prefix as the row sees it, as some and as every row of the wavefront does.
+    const int row_prefix = r < rows && position(r) >= 0 ? prefix : 0, some_prefix = uniform(idle || p_last < 0 ? 0 : prefix), whole_prefix = uniform(p_first >= 0 ? prefix : 0);
+    // Of scored calls S is the score in log2 already.
+    const float unit = SCORED ? 1.0f : a.scale2;
+    float slope = 0, place_of_row = 0;  // of the lane's row: its slope (log2), and its position less the lane's first key of a block from key 0 on
+    if constexpr (SCORED) {
+      const int mine = min(r, rows - 1), token = (int)a.by_group.quotient((uint32_t)mine);
+      if (a.slopes) slope = a.slopes[head * a.group + mine - token * a.group] * 1.44269504089f;
+      place_of_row = (float)(e.len - e.n + token - 4 * h);
+    }
 
     h8 q[KF];
     {
@@ -166,10 +193,10 @@ __global__ __launch_bounds__(64 * WAVES, tile_waves(D, WAVES)) void tile_kernel(
     const int my_tile = wave % kBlockTiles;
     int number = -1;  // the page of that tile in 64 blocks, one to a lane
     auto look_up = [&](int block) {
-      const int tile = key_from / kTile + (block + hidden(lane)) * kBlockTiles + my_tile;
+      const int tile = SCORED ? first_key(block + hidden(lane)) / kTile + my_tile : key_from / kTile + (block + hidden(lane)) * kBlockTiles + my_tile;
       const uint32_t page = a.v.page_tiles.quotient((uint32_t)tile);
       number = -1;
-      if (tile * kTile < key_to && page < (uint32_t)a.v.table_width) {
+      if (tile * kTile < keys_end && page < (uint32_t)a.v.table_width) {
         const int found = a.v.table[place.b * a.v.table_stride + page];
         if ((uint32_t)found < (uint32_t)a.v.n_pages) number = found;
       }
@@ -179,7 +206,7 @@ __global__ __launch_bounds__(64 * WAVES, tile_waves(D, WAVES)) void tile_kernel(
       if (block % 64 == 0) look_up(block);
 #pragma unroll
       for (int j = 0; j < JOBS; j++)
-        jobs[j].load(a, of_lane(number, block % 64), head, key_from / kTile + block * kBlockTiles + my_tile, JOBS == 1 ? wave >= kBlockTiles : j == 1, lane);
+        jobs[j].load(a, of_lane(number, block % 64), head, SCORED ? first_key(block) / kTile + my_tile : key_from / kTile + block * kBlockTiles + my_tile, JOBS == 1 ? wave >= kBlockTiles : j == 1, lane);
     };
     auto restore = [&](int buffer) {
 #pragma unroll
@@ -216,20 +243,34 @@ __global__ __launch_bounds__(64 * WAVES, tile_waves(D, WAVES)) void tile_kernel(
 #pragma unroll
       for (int n = 0; n < AHEAD; n++) f[n] = block.v[n % DT][n / DT][lane];
       const uint32_t anything = (uint32_t)uniform((int)(what[0] | what[1] | what[2] | what[3]));
-      if (key0 < whole_begin || key0 + kBlock > whole_end || (anything & kMissing)) {  // some row does not see some key
+      if constexpr (SCORED) {
+        if (a.cap2 > 0) {
+#pragma unroll
+          for (int i = 0; i < 32; i++) s[i / 16][i % 16] = capped(a, s[i / 16][i % 16]);
+        } else {
+          s[0] *= a.scale2, s[1] *= a.scale2;
+        }
+        if (a.slopes) {
+          const float ahead = place_of_row - (float)key0;
+#pragma unroll
+          for (int i = 0; i < 32; i++) s[i / 16][i % 16] = __builtin_fmaf(-slope, fabsf(ahead - (float)(32 * (i / 16) + 8 * (i % 16 / 4) + i % 4)), s[i / 16][i % 16]);
+        }
+      }
+      const bool outside = key0 < whole_begin || key0 + kBlock > whole_end;
+      if ((SCORED ? outside && key0 + kBlock > whole_prefix : outside) || (anything & kMissing)) {  // some row does not see some key
 #pragma unroll
         for (int kt = 0; kt < 2; kt++)
 #pragma unroll
           for (int i = 0; i < 16; i++) {
             const int key = key0 + 32 * kt + 8 * (i / 4) + 4 * h + i % 4;
-            if (key < row_begin || key >= row_end || (what[2 * kt + i / 8] & kMissing)) s[kt][i] = -INFINITY;
+            if (((key < row_begin || key >= row_end) && (!SCORED || key >= row_prefix)) || (what[2 * kt + i / 8] & kMissing)) s[kt][i] = -INFINITY;
           }
       }
       float top = s[0][0];
 #pragma unroll
       for (int i = 1; i < 32; i++) top = fmaxf(top, s[i / 16][i % 16]);
-      top *= a.scale2;
-      float scale2 = a.scale2;
+      top *= unit;
+      float scale2 = unit;
       if (far || __ballot(top - m > kSlack)) {  // the maximum is raised only where a score passes it by more than the slack
         top = fmaxf(top, m);
         top = larger(with_32(top));
@@ -241,7 +282,7 @@ __global__ __launch_bounds__(64 * WAVES, tile_waves(D, WAVES)) void tile_kernel(
         for (int d = 0; d < DT; d++) o[d] *= less;
         if (far) {
 #pragma unroll
-          for (int i = 0; i < 32; i++) s[i / 16][i % 16] = below_top(s[i / 16][i % 16], a.scale2, top);
+          for (int i = 0; i < 32; i++) s[i / 16][i % 16] = below_top(s[i / 16][i % 16], unit, top);
           scale2 = 1.0f;
         }
       }
@@ -272,6 +313,8 @@ __global__ __launch_bounds__(64 * WAVES, tile_waves(D, WAVES)) void tile_kernel(
           for (int t = 0; t < kBlockTiles; t++) {
             const int first = key0 + kTile * t, from = min(max(row_begin - first, 0), kTile), to = min(max(row_end - first, 0), kTile);
             if (what[t] & kBad) seen |= (notes[buffer].bad[t][run] & ((1u << to) - 1) & ~((1u << from) - 1)) != 0;
+            if constexpr (SCORED)
+              if (what[t] & kBad) seen |= (notes[buffer].bad[t][run] & ((1u << min(max(row_prefix - first, 0), kTile)) - 1)) != 0;
           }
           if (seen) {
 #pragma unroll
@@ -292,8 +335,8 @@ __global__ __launch_bounds__(64 * WAVES, tile_waves(D, WAVES)) void tile_kernel(
       for (int block = 0; block < n_blocks; block++) {
         if (block + 1 < n_blocks) restore((block + 1) & 1);
         if (block + 2 < n_blocks) request(block + 2);
-        const int key0 = key_from + block * kBlock;
-        if (key0 < some_end && key0 + kBlock > some_begin) compute(block & 1, key0);
+        const int key0 = first_key(block);
+        if ((key0 < some_end && key0 + kBlock > some_begin) || (SCORED && key0 < some_prefix)) compute(block & 1, key0);
         __syncthreads();
       }
     }
@@ -310,18 +353,25 @@ __global__ __launch_bounds__(64 * WAVES, tile_waves(D, WAVES)) void tile_kernel(
   }
 }
 
-bool load_tile() { return loaded((const void*)tile_kernel<64, 32, 4>); }
+#if AMS_KV_SCORED
+using Args = ScoredArgs;
+bool load_scored_tile() { return loaded((const void*)tile_kernel<64, 32, 4, Args>); }
+#else
+using Args = AttentionArgs;
+bool load_tile() { return loaded((const void*)tile_kernel<64, 32, 4, Args>); }
+#endif
 
-void launch_tile(const AttentionArgs& a, int head_dim, int scale_group, int waves, unsigned grid, hipStream_t stream) {
+template <>
+void launch_tile<Args>(const Args& a, int head_dim, int scale_group, int waves, unsigned grid, hipStream_t stream) {
   dispatch(head_dim, scale_group, [&](auto d, auto g) {
     constexpr int D = decltype(d)::value, G = decltype(g)::value;
     if constexpr (D < 256) {
       if (waves == 8) {
-        hipLaunchKernelGGL((tile_kernel<D, G, 8>), dim3(grid), dim3(512), 0, stream, a);
+        hipLaunchKernelGGL((tile_kernel<D, G, 8, Args>), dim3(grid), dim3(512), 0, stream, a);
         return;
       }
     }
-    hipLaunchKernelGGL((tile_kernel<D, G, 4>), dim3(grid), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((tile_kernel<D, G, 4, Args>), dim3(grid), dim3(256), 0, stream, a);
   });
 }
 
