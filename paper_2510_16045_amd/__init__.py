@@ -247,12 +247,27 @@ def _first_kv_call(*args):
 
 
 _kv_call = _first_kv_call
-_KV_WRITE, _KV_READ, _KV_ATTENTION = range(3)  # of csrc/ams_binding.cpp
+_KV_WRITE, _KV_READ, _KV_ATTENTION, _KV_SCORED = range(4)  # of csrc/ams_binding.cpp
+
+
+def _first_rope_call(*args):
+    """The same for ams_rope."""
+    _bind_call()
+    return _rope_call(*args)
+
+
+def _first_logprobs_call(*args):
+    """The same for ams_logprobs."""
+    _bind_call()
+    return _logprobs_call(*args)
+
+
+_rope_call, _logprobs_call = _first_rope_call, _first_logprobs_call
 
 
 def _bind_call():
-    global _call, _kv_call
-    _call = _kv_call = lambda *args: None  # the long way
+    global _call, _kv_call, _rope_call, _logprobs_call
+    _call = _kv_call = _rope_call = _logprobs_call = lambda *args: None  # the long way
     try:
         import torch  # its libraries first
     except ImportError:
@@ -271,7 +286,8 @@ def _bind_call():
     lib = load_library()
     _binding.bind(*(ctypes.cast(f, _vp).value for f in (lib.ams_packed_bytes, lib.ams_group_scales_count, lib.ams_linear, lib.ams_linear_ws, lib.ams_linear_static_ws, lib.ams_linear_grouped)))
     _binding.bind_kv(*(ctypes.cast(f, _vp).value for f in (lib.ams_kv_block_bytes, lib.ams_kv_write, lib.ams_kv_read, lib.ams_kv_attention)))
-    _call, _kv_call = _binding.linear, _binding.kv
+    _binding.bind_more(*(ctypes.cast(f, _vp).value for f in (lib.ams_kv_attention_scored, lib.ams_rope, lib.ams_logprobs)))
+    _call, _kv_call, _rope_call, _logprobs_call = _binding.linear, _binding.kv, _binding.rope, _binding.logprobs
 
 
 _PLAIN, _WORKSPACE, _STATIC, _GROUPED = range(4)  # of csrc/ams_binding.cpp
@@ -649,6 +665,8 @@ def ams_kv_attention(q, cache, block_table, kv_lens, scale_group: int = 32, q_st
     scored = bool(softcap) or slopes is not None or prefix_lens is not None
     if out is not None and not scored and _kv_call(_KV_ATTENTION, cache, block_table, kv_lens, scale_group, q_starts, q, out, max_q_len, softmax_scale, causal, window, workspace, lse):
         return out
+    if out is not None and scored and _kv_call(_KV_SCORED, cache, block_table, kv_lens, scale_group, q_starts, q, out, max_q_len, softmax_scale, causal, window, workspace, lse, softcap, slopes, prefix_lens):
+        return out
     import torch
 
     if q.dim() != 3:
@@ -703,6 +721,8 @@ def ams_rope(q, k, turns, positions=None, kv_lens=None, q_starts=None, magnitude
     turns: of ams_rope_frequencies, on the GPU; the first 2 * len(turns) channels of a head are rotated, halves of them paired or
     (interleaved) neighbours.  positions: int32 [rows]; else the rows are the last ones of sequences of kv_lens tokens, as in
     ams_kv_write, and rows that none has are left alone.  transposed: by the angles' negatives: takes a gradient back."""
+    if out is not None and _rope_call(q, k, turns, positions, kv_lens, q_starts, magnitude, interleaved, transposed, *out):
+        return out
     import torch
 
     if q.dim() != 3 or (k is not None and (k.dim() != 3 or k.shape[0] != q.shape[0] or k.shape[2] != q.shape[2])):
@@ -722,7 +742,7 @@ def ams_rope(q, k, turns, positions=None, kv_lens=None, q_starts=None, magnitude
     rotation = _Rotation(_dev_ptr(turns, torch.int64), index(positions), index(kv_lens), index(q_starts), batch, 2 * turns.shape[0], int(interleaved), int(transposed), magnitude)
     rows = [None if x is None else ctypes.byref(_rope_rows(x, y, name)) for x, y, name in ((q, out[0], "q"), (k, out[1], "k"))]
     _check(load_library().ams_rope(ctypes.byref(rotation), *rows, q.shape[0], q.shape[2], _stream()), "ams_rope")
-    return tuple(out)
+    return out
 
 
 LogProbs = collections.namedtuple("LogProbs", "logprob rank entropy top_logprobs top_tokens")
@@ -754,6 +774,8 @@ def ams_logprobs(logits, tokens=None, top: int = 0, temperature: float = 1.0, wo
     -1).  top: how many of the most likely tokens (up to MAX_TOP).  temperature divides the logits.
     workspace: a uint8 CUDA tensor, zero-filled once, as ams_kv_attention's (it may be the same); without one each row is
     one workgroup's.  out: a LogProbs of tensors to write; those that are None are not worked out."""
+    if out is not None and _logprobs_call(logits, tokens, top, temperature, workspace, *out):
+        return out
     import torch
 
     kind, (rows, vocab) = _logits_type(logits), logits.shape
@@ -778,4 +800,4 @@ def ams_logprobs(logits, tokens=None, top: int = 0, temperature: float = 1.0, wo
         _dev_ptr(workspace, torch.uint8) if workspace is not None else None, workspace.numel() if workspace is not None else 0, _stream()
     )
     _check(rc, "ams_logprobs")
-    return LogProbs(*out)
+    return out

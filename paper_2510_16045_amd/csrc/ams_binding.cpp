@@ -13,6 +13,7 @@
 
 #include <cxxabi.h>
 #include <math.h>
+#include <stddef.h>
 #include <string.h>
 
 #include "../../include/ams.h"
@@ -154,7 +155,24 @@ PyObject* bind_kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Py_RETURN_NONE;
 }
 
-enum KvEntry { kKvWrite, kKvRead, kKvAttention };
+// What was added beside them: bind_more(address of each).
+struct MoreLibrary {
+  decltype(&ams_kv_attention_scored) attention_scored;
+  decltype(&ams_rope) rope;
+  decltype(&ams_logprobs) logprobs;
+} more_lib;
+
+PyObject* bind_more(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  void* at[3];
+  if (n != 3) return PyErr_Format(PyExc_TypeError, "bind_more takes 3 addresses");
+  for (int i = 0; i < 3; i++)
+    if (!(at[i] = PyLong_AsVoidPtr(a[i]))) return PyErr_Occurred() ? nullptr : PyErr_Format(PyExc_ValueError, "no address");
+  static_assert(sizeof more_lib == sizeof at, "one address for each");
+  memcpy(&more_lib, at, sizeof more_lib);
+  Py_RETURN_NONE;
+}
+
+enum KvEntry { kKvWrite, kKvRead, kKvAttention, kKvScored };
 
 struct KvCall {
   int64_t entry;
@@ -165,10 +183,28 @@ struct KvCall {
   int64_t lse_stride, window, most;
   int heads, causal;
   float scale;
+  ams_kv_scores scores;
   void* ws;
   size_t ws_bytes;
   void* st;
 };
+
+// A float, or a whole number (of fewer digits than a float has).
+bool real(PyObject* o, double* v) {
+  if (PyFloat_CheckExact(o)) return *v = PyFloat_AS_DOUBLE(o), true;
+  int64_t w = 0;
+  if (!whole(o, &w) || w > (1 << 30) || w < -(1 << 30)) return false;
+  return *v = (double)w, true;
+}
+// A plain contiguous tensor of `n` values, or None; false for anything else.
+bool values(PyObject* o, c10::ScalarType type, int64_t n, c10::DeviceIndex device, void** at) {
+  *at = nullptr;
+  if (o == Py_None) return true;
+  const at::Tensor* const t = plain(o, type, device);
+  if (!t || t->dim() != 1 || t->size(0) != n) return false;
+  *at = t->data_ptr();
+  return true;
+}
 
 // [rows, heads, dim] in fp16 with the channels of a head side by side
 const at::Tensor* rows_of(PyObject* o, int64_t heads, int64_t dim, c10::DeviceIndex device, int64_t* strides) {
@@ -180,11 +216,12 @@ const at::Tensor* rows_of(PyObject* o, int64_t heads, int64_t dim, c10::DeviceIn
 
 // The arguments of the three calls, checked; false for those that are not taken.
 //   kv(entry, cache, block_table, kv_lens, scale_group, q_starts or None, ...)
-//     kKvWrite: k, v;  kKvRead: head_dim, out k, out v;  kKvAttention: q, out, max_q_len or None, softmax_scale or None, causal, window, workspace or None, lse or None
+//     kKvWrite: k, v;  kKvRead: head_dim, out k, out v;  kKvAttention: q, out, max_q_len or None, softmax_scale or None, causal, window, workspace or None, lse or None;
+//     kKvScored: as kKvAttention, and softcap, slopes or None, prefix_lens or None
 bool kv_arguments(PyObject* const* a, Py_ssize_t n, KvCall* c) try {
   *c = {};
   int64_t group = 0, dim = 0;
-  if (!kv_lib.attention || n < 8 || !whole(a[0], &c->entry) || !whole(a[4], &group) || n != (c->entry == kKvWrite ? 8 : c->entry == kKvRead ? 9 : 14)) return false;
+  if (!kv_lib.attention || n < 8 || !whole(a[0], &c->entry) || !whole(a[4], &group) || n != (c->entry == kKvWrite ? 8 : c->entry == kKvRead ? 9 : c->entry == kKvScored ? 17 : 14)) return false;
   if (at::impl::torch_function_mode_enabled() || c10::impl::TorchDispatchModeTLS::any_modes_set()) return false;
   const auto stream = c10::hip::getCurrentHIPStream();  // of the current device
   const c10::DeviceIndex dev = stream.device_index();
@@ -195,7 +232,7 @@ bool kv_arguments(PyObject* const* a, Py_ssize_t n, KvCall* c) try {
   const at::Tensor* starts = nullptr;
   if (a[5] != Py_None && (!(starts = plain(a[5], at::kInt, dev)) || starts->dim() != 1 || starts->size(0) != batch + 1)) return false;
   const at::Tensor *x = nullptr, *y = nullptr;
-  if (c->entry == kKvAttention) {
+  if (c->entry == kKvAttention || c->entry == kKvScored) {
     x = rows_of(a[6], 0, 0, dev, c->strides);
     if (!x || !(y = rows_of(a[7], x->size(1), x->size(2), dev, c->strides + 2))) return false;
     dim = x->size(2);
@@ -219,6 +256,12 @@ bool kv_arguments(PyObject* const* a, Py_ssize_t n, KvCall* c) try {
       const at::Tensor* const lse = plain(a[13], at::kFloat, dev, false);
       if (!lse || lse->dim() != 2 || lse->size(0) != x->size(0) || lse->size(1) != x->size(1) || (lse->size(1) > 1 && lse->stride(1) != 1)) return false;
       c->lse = (float*)lse->data_ptr(), c->lse_stride = lse->stride(0);
+    }
+    if (c->entry == kKvScored) {
+      double cap = 0;
+      void *slopes = nullptr, *prefixes = nullptr;
+      if (!more_lib.attention_scored || !real(a[14], &cap) || !values(a[15], at::kFloat, c->heads, dev, &slopes) || !values(a[16], at::kInt, batch, dev, &prefixes)) return false;
+      c->scores = {(const float*)slopes, (const int32_t*)prefixes, (float)cap};
     }
   } else {
     const int first = c->entry == kKvWrite ? 6 : 7;
@@ -244,6 +287,9 @@ int call(const KvCall& c) {
   switch (c.entry) {
     case kKvWrite: return kv_lib.write(&c.cache, (const uint16_t*)c.first, (const uint16_t*)c.second, c.rows, c.strides[0], c.strides[1], c.strides[2], c.strides[3], c.st);
     case kKvRead: return kv_lib.read(&c.cache, (uint16_t*)c.first, (uint16_t*)c.second, c.rows, c.strides[0], c.strides[1], c.strides[2], c.strides[3], c.st);
+    case kKvScored:
+      return more_lib.attention_scored(&c.cache, &c.scores, (const uint16_t*)c.first, (uint16_t*)c.second, c.lse, c.rows, c.heads, c.strides[0], c.strides[1], c.strides[2], c.strides[3], c.lse_stride, c.scale,
+                                       c.causal, c.window, c.most, c.ws, c.ws_bytes, c.st);
     case kKvAttention:
       return kv_lib.attention(&c.cache, (const uint16_t*)c.first, (uint16_t*)c.second, c.lse, c.rows, c.heads, c.strides[0], c.strides[1], c.strides[2], c.strides[3], c.lse_stride, c.scale, c.causal, c.window,
                               c.most, c.ws, c.ws_bytes, c.st);
@@ -258,10 +304,133 @@ PyObject* kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Py_RETURN_TRUE;
 }
 
+// ---- rotary positions ----------------------------------------------------------------------------------
+struct RopeCall {
+  ams_rotation rotation;
+  ams_rope_rows q, k;
+  bool has_k;
+  int64_t rows;
+  int head_dim;
+  void* st;
+};
+
+bool rope_arguments(PyObject* const* a, Py_ssize_t n, RopeCall* c) try {
+  *c = {};
+  if (!more_lib.rope || n != 11 || at::impl::torch_function_mode_enabled() || c10::impl::TorchDispatchModeTLS::any_modes_set()) return false;
+  const auto stream = c10::hip::getCurrentHIPStream();  // of the current device
+  const c10::DeviceIndex dev = stream.device_index();
+  auto rows = [&](PyObject* in, PyObject* out, int64_t dim, ams_rope_rows* r) -> const at::Tensor* {
+    const at::Tensor* const x = rows_of(in, 0, dim, dev, &r->in_stride);
+    if (!x || x->size(1) > AMS_KV_MAX_HEADS) return nullptr;
+    const at::Tensor* const y = rows_of(out, x->size(1), x->size(2), dev, &r->out_stride);
+    if (!y || y->size(0) != x->size(0)) return nullptr;
+    r->in = (const uint16_t*)x->const_data_ptr(), r->out = (uint16_t*)y->data_ptr(), r->heads = (int32_t)x->size(1);
+    return x;
+  };
+  static_assert(offsetof(ams_rope_rows, in_head_stride) == offsetof(ams_rope_rows, in_stride) + 8 && offsetof(ams_rope_rows, out_head_stride) == offsetof(ams_rope_rows, out_stride) + 8, "rows_of fills pairs");
+  const at::Tensor* const q = rows(a[0], a[9], 0, &c->q);
+  if (!q || q->size(2) > AMS_ROPE_MAX_DIM) return false;
+  c->has_k = a[1] != Py_None;
+  if (c->has_k) {
+    const at::Tensor* const k = rows(a[1], a[10], q->size(2), &c->k);
+    if (!k || k->size(0) != q->size(0)) return false;
+  } else if (a[10] != Py_None) {
+    return false;
+  }
+  const at::Tensor* const turns = plain(a[2], at::kLong, dev);
+  if (!turns || turns->dim() != 1 || turns->size(0) > AMS_ROPE_MAX_DIM || (a[3] == Py_None) == (a[4] == Py_None) || (a[5] != Py_None && a[4] == Py_None)) return false;
+  void *positions = nullptr, *starts = nullptr;
+  if (!values(a[3], at::kInt, q->size(0), dev, &positions)) return false;
+  int64_t batch = 0;
+  const int32_t* lens = nullptr;
+  if (a[4] != Py_None) {
+    const at::Tensor* const t = plain(a[4], at::kInt, dev);
+    if (!t || t->dim() != 1 || (batch = t->size(0)) > AMS_KV_MAX_BATCH) return false;
+    lens = (const int32_t*)t->const_data_ptr();
+  }
+  double magnitude = 1;
+  if (!values(a[5], at::kInt, batch + 1, dev, &starts) || !real(a[6], &magnitude) || !PyBool_Check(a[7]) || !PyBool_Check(a[8])) return false;
+  c->rotation = {(const uint64_t*)turns->const_data_ptr(), (const int32_t*)positions, lens, (const int32_t*)starts, (int32_t)batch, (int32_t)(2 * turns->size(0)), a[7] == Py_True, a[8] == Py_True, (float)magnitude};
+  c->rows = q->size(0), c->head_dim = (int)q->size(2), c->st = (void*)stream.stream();
+  return true;
+} catch (...) {  // torch's own checks; the long way meets them again
+  return false;
+}
+
+int call(const RopeCall& c) { return more_lib.rope(&c.rotation, &c.q, c.has_k ? &c.k : nullptr, c.rows, c.head_dim, c.st); }
+
+// rope(q, k or None, turns, positions or None, kv_lens or None, q_starts or None, magnitude, interleaved, transposed, out q, out k or None): True, or None
+PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  RopeCall c;
+  if (!rope_arguments(a, n, &c) || call_unlocked(c) != AMS_OK) Py_RETURN_NONE;
+  Py_RETURN_TRUE;
+}
+
+// ---- log probabilities ---------------------------------------------------------------------------------
+struct LogCall {
+  const void* logits;
+  int type, top;
+  int64_t rows, vocab, stride;
+  const int32_t* tokens;
+  float temperature;
+  void* out[5];
+  void* ws;
+  size_t ws_bytes;
+  void* st;
+};
+
+bool log_arguments(PyObject* const* a, Py_ssize_t n, LogCall* c) try {
+  *c = {};
+  int64_t top = 0;
+  double temperature = 0;
+  if (!more_lib.logprobs || n != 10 || !whole(a[2], &top) || !real(a[3], &temperature) || top < 0 || top > AMS_LOGPROBS_MAX_TOP) return false;
+  if (at::impl::torch_function_mode_enabled() || c10::impl::TorchDispatchModeTLS::any_modes_set()) return false;
+  const auto stream = c10::hip::getCurrentHIPStream();  // of the current device
+  const c10::DeviceIndex dev = stream.device_index();
+  const at::Tensor* x = plain(a[0], at::kHalf, dev, false);
+  if (!x) c->type = AMS_TYPE_FP32, x = plain(a[0], at::kFloat, dev, false);
+  if (!x || x->dim() != 2 || (x->size(1) > 1 && x->stride(1) != 1)) return false;
+  c->rows = x->size(0), c->vocab = x->size(1), c->stride = x->stride(0), c->top = (int)top, c->temperature = (float)temperature;
+  void* tokens = nullptr;
+  if (!values(a[1], at::kInt, c->rows, dev, &tokens)) return false;
+  for (int i = 0; i < 3; i++)
+    if (!values(a[5 + i], i == 1 ? at::kInt : at::kFloat, c->rows, dev, &c->out[i])) return false;
+  for (int i = 3; i < 5; i++) {
+    if (a[5 + i] == Py_None) continue;
+    const at::Tensor* const t = plain(a[5 + i], i == 3 ? at::kFloat : at::kInt, dev);
+    if (!t || t->dim() != 2 || t->size(0) != c->rows || t->size(1) != top) return false;
+    c->out[i] = t->data_ptr();
+  }
+  if (a[4] != Py_None) {
+    const at::Tensor* const ws = plain(a[4], at::kByte, dev);
+    if (!ws) return false;
+    c->ws = ws->data_ptr(), c->ws_bytes = (size_t)ws->numel();
+  }
+  c->logits = x->const_data_ptr(), c->tokens = (const int32_t*)tokens, c->st = (void*)stream.stream();
+  return true;
+} catch (...) {  // torch's own checks; the long way meets them again
+  return false;
+}
+
+int call(const LogCall& c) {
+  return more_lib.logprobs(c.logits, c.type, c.rows, c.vocab, c.stride, c.tokens, c.temperature, c.top, (float*)c.out[0], (int32_t*)c.out[1], (float*)c.out[2], (float*)c.out[3], (int32_t*)c.out[4], c.ws,
+                           c.ws_bytes, c.st);
+}
+
+// logprobs(logits, tokens or None, top, temperature, workspace or None, logprob, rank, entropy, top_logprobs, top_tokens (each or None)): True, or None
+PyObject* logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  LogCall c;
+  if (!log_arguments(a, n, &c) || call_unlocked(c) != AMS_OK) Py_RETURN_NONE;
+  Py_RETURN_TRUE;
+}
+
 PyMethodDef methods[] = {{"bind", (PyCFunction)(void (*)(void))bind, METH_FASTCALL, nullptr},
                          {"linear", (PyCFunction)(void (*)(void))linear, METH_FASTCALL, nullptr},
                          {"bind_kv", (PyCFunction)(void (*)(void))bind_kv, METH_FASTCALL, nullptr},
                          {"kv", (PyCFunction)(void (*)(void))kv, METH_FASTCALL, nullptr},
+                         {"bind_more", (PyCFunction)(void (*)(void))bind_more, METH_FASTCALL, nullptr},
+                         {"rope", (PyCFunction)(void (*)(void))rope, METH_FASTCALL, nullptr},
+                         {"logprobs", (PyCFunction)(void (*)(void))logprobs, METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
