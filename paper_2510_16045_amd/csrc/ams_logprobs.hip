@@ -4,8 +4,12 @@
 //
 // One read of the logits.  A wavefront walks pieces of a row with a running maximum m, S = sum 2^y and U = sum y 2^y, y = log2(e) / T (x - m):
 // the log probability is ln 2 (y - log2 S) and the entropy ln 2 (log2 S - U / S), sums of terms of one sign.  m is always the true maximum of
-// what has been seen, so neither difference cancels.  A wavefront's most likely tokens are a sorted list, one to a lane; what does not
-// pass the last of them, which is nearly everything, costs one comparison of a lane's maximum.
+// what has been seen, so neither difference cancels.
+//
+// The `top` most likely tokens.  The n-th largest of the maxima of disjoint pieces is a bound that n values reach, so nothing below it is among
+// the n largest.  A wavefront takes that of the 256 pieces of its first chunk, by bisection, and writes down what reaches it: a few more
+// than n values, from then on only larger ones.  (Where it has written down too much, it keeps the n largest and their last as the bound.)  At the
+// end what reaches the largest bound of all wavefronts is counted out: a value's place is the number of those ahead of it.
 //
 // A row is shared out to several workgroups where rows do not fill the chip: each leaves its statistics and list in the workspace and
 // counts itself in; the last one joins them, always in the same order, and clears the count.  Nobody waits for anybody.
@@ -18,9 +22,10 @@
 
 namespace ams_kv {
 
-constexpr int kLogWaves = 4;
+constexpr int kLogWaves = 8;
 constexpr size_t kLogCountBytes = 64 * 1024;  // of a workspace: one count for each row, at its front
-constexpr int kMaxRowParts = 64;
+constexpr int kMaxRowParts = 32;
+constexpr int kHeld = 256;  // values that a wavefront writes down at most
 
 struct LogArgs {
   const void* logits;
@@ -31,17 +36,40 @@ struct LogArgs {
   uint32_t* counts;
   uint8_t* left;  // [row][part][LogStats, top entries]
   int vocab, top;
-  float scale2;     // log2(e) / T
-  int part_chunks;  // of a workgroup
+  float scale2;    // log2(e) / T
+  int part_turns;  // of a workgroup: chunks of each of its wavefronts
   int part_bytes;
   uint32_t left_bytes;
-  Divisor parts;
+  Divisor parts, by_top;
 };
 
 struct LogStats {
   float top, sum, moment;
   int ahead;
 };
+// A token and its logit in one number that is the larger the further ahead the token is: the value's bits in the order of the values (of
+// both zeros the same), then the lower index.  0: none.
+typedef uint64_t Entry;
+__device__ __forceinline__ Entry entry_of(float value, int index) {
+  const uint32_t bits = __builtin_bit_cast(uint32_t, value + 0.0f);
+  return (uint64_t)(bits & 0x80000000u ? ~bits : bits | 0x80000000u) << 32 | ~(uint32_t)index;
+}
+__device__ __forceinline__ float value_of(uint32_t key) { return __builtin_bit_cast(float, key & 0x80000000u ? key & 0x7FFFFFFFu : ~key); }
+__device__ __forceinline__ float value_of(Entry e) { return value_of((uint32_t)(e >> 32)); }
+__device__ __forceinline__ int index_of(Entry e) { return (int)~(uint32_t)e; }
+// How many of the entries are ahead of one; they are `n` rounded up to a multiple of 8, the others 0.
+__device__ __forceinline__ int place_of(const Entry* entries, int n, Entry mine) {
+  int place = 0;
+#pragma unroll 1
+  for (int i = 0; i < n; i += 8) {
+    Entry e[8];
+#pragma unroll
+    for (int j = 0; j < 8; j++) e[j] = entries[i + j];
+#pragma unroll
+    for (int j = 0; j < 8; j++) place += e[j] > mine;
+  }
+  return place;
+}
 
 // Lanes' values joined over the wavefront, by lane patterns.
 template <typename Join>
@@ -62,49 +90,7 @@ __device__ __forceinline__ float max_over_wave(float x) {
 __device__ __forceinline__ float sum_over_wave(float x) {
   return over_wave(x, [](float a, float b) { return a + b; });
 }
-__device__ __forceinline__ float lane_value(float x, int lane) { return __builtin_bit_cast(float, of_lane(__builtin_bit_cast(int, x), lane)); }
-
-// The n-th largest (from 0 on) of the lanes' values, none of them NaN: sorted by a bitonic network.
-__device__ __forceinline__ float nth_of_lanes(float x, int n) {
-  const int lane = lane_id();
-#pragma unroll
-  for (int k = 2; k <= 64; k *= 2)
-#pragma unroll
-    for (int j = k / 2; j > 0; j /= 2) {
-      const float y = __shfl_xor(x, j, 64);
-      x = ((lane & j) == 0) == ((lane & k) == 0) ? fmaxf(x, y) : fminf(x, y);
-    }
-  return lane_value(x, n);
-}
-
-// The wavefront's best entries, the n-th in lane n: by value, of equal ones the lower index first.  Lanes without one: -inf and no index.
-struct TopList {
-  float value = -INFINITY;
-  int index = INT_MAX;
-  float last_value = -INFINITY;  // of the last one that counts
-  int last_index = INT_MAX;
-  __device__ __forceinline__ bool full() const { return last_index != INT_MAX; }
-  __device__ __forceinline__ bool takes(float v, int i) const { return v > last_value || (v == last_value && i < last_index); }
-  __device__ __forceinline__ void insert(float v, int i, int top) {
-    const int at = __builtin_popcountll(__ballot(value > v || (value == v && index < i)));
-    const float up_value = __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, value), 0x138, 0xF, 0xF, true));  // of the lane before
-    const int up_index = __builtin_amdgcn_update_dpp(0, index, 0x138, 0xF, 0xF, true);
-    const int lane = lane_id();
-    value = lane > at ? up_value : lane == at ? v : value;
-    index = lane > at ? up_index : lane == at ? i : index;
-    last_value = lane_value(value, top - 1), last_index = of_lane(index, top - 1);
-  }
-  // The lanes' values that belong in the list.
-  __device__ __forceinline__ void offer(float v, int i, float least, int top) {
-    for (;;) {
-      const unsigned long long some = __ballot(v >= least && i != INT_MAX && takes(v, i));
-      if (!some) return;
-      const int lane = __builtin_ctzll(some);
-      insert(lane_value(v, lane), of_lane(i, lane), top);
-      if (lane_id() == lane) i = INT_MAX;
-    }
-  }
-};
+__device__ __forceinline__ int lanes_before(unsigned long long some) { return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(some >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)some, 0)); }
 
 // Pieces of 16 bytes of a row, kPieces to a lane; those of a lane are 64 pieces apart.
 constexpr int kPieces = 4;
@@ -115,45 +101,127 @@ struct Chunk {
   u4 raw[kPieces];
   __device__ __forceinline__ static int index(int first, int piece, int j) { return first + (piece * 64 + lane_id()) * PER + j; }
   __device__ __forceinline__ void load(const T* row, int first, int vocab) {
+    if (first + VALUES <= vocab) {
+#pragma unroll
+      for (int u = 0; u < kPieces; u++) raw[u] = *(const u4_unaligned*)(row + index(first, u, 0));
+      return;
+    }
+    // The row's end: behind it -inf.  One piece may lie on it, for one lane in its middle.
+    T edge __attribute__((ext_vector_type(PER)));
+    const int whole = max(vocab - first, 0) / (64 * PER), at = index(first, whole, 0);
+    u4 none;
+#pragma unroll
+    for (int j = 0; j < PER; j++) edge[j] = -INFINITY;
+    none = __builtin_bit_cast(u4, edge);
+    u4 last = none;
+    if (at + PER <= vocab) {
+      last = *(const u4_unaligned*)(row + at);
+    } else if (at < vocab) {
+#pragma unroll
+      for (int j = 0; j < PER - 1; j++)
+        if (at + j < vocab) edge[j] = row[at + j];
+      last = __builtin_bit_cast(u4, edge);
+    }
 #pragma unroll
     for (int u = 0; u < kPieces; u++) {
-      const int at = index(first, u, 0);
-      if (first + VALUES <= vocab || at + PER <= vocab) {
-        raw[u] = *(const u4_unaligned*)(row + at);
-      } else {
-        T x __attribute__((ext_vector_type(PER)));
-#pragma unroll
-        for (int j = 0; j < PER; j++) {
-          x[j] = -INFINITY;
-          if (at + j < vocab) x[j] = row[at + j];
-        }
-        raw[u] = __builtin_bit_cast(u4, x);
-      }
+      raw[u] = u == whole ? last : none;
+      if (u < whole) raw[u] = *(const u4_unaligned*)(row + index(first, u, 0));
     }
   }
-  __device__ __forceinline__ float value(int piece, int j) const {
+  __device__ __forceinline__ T value(int piece, int j) const {
+    typedef T Vector __attribute__((ext_vector_type(PER)));
+    return __builtin_bit_cast(Vector, raw[piece])[j];
+  }
+  // The compiler is to convert the values again: kept from one use to the next they take 32 registers.
+  __device__ __forceinline__ void forget() {
+#pragma unroll
+    for (int u = 0; u < kPieces; u++) asm volatile("" : "+v"(raw[u]));
+  }
+  // The largest of a piece; NaN is left out.
+  __device__ __forceinline__ float largest(int piece) const {
     if constexpr (PER == 4) {
-      return __builtin_bit_cast(f4, raw[piece])[j];
+      const f4 x = __builtin_bit_cast(f4, raw[piece]);
+      return fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), -INFINITY);
     } else {
-      return (float)__builtin_bit_cast(h8, raw[piece])[j];
+      const u4 r = raw[piece];
+      const h2 x = __builtin_elementwise_max(__builtin_elementwise_max(halves(r[0]), halves(r[1])), __builtin_elementwise_max(halves(r[2]), halves(r[3])));
+      return fmaxf(fmaxf((float)x[0], (float)x[1]), -INFINITY);
+    }
+  }
+};
+
+// A bound that n of the wavefront's 256 values reach, as near to the n-th largest as 19 bits of it are; -inf where fewer are above
+// that.  Bisection of the bits in the order of the values.
+__device__ __forceinline__ float bound_of(const float (&x)[kPieces], int n) {
+  uint32_t key = 0;
+#pragma unroll 1
+  for (uint32_t bit = 0x80000000u; bit >= 0x2000u; bit >>= 1) {  // 19 bits: of fp16 values all
+    const float at = value_of(key | bit);
+    int reach = 0;
+#pragma unroll
+    for (int u = 0; u < kPieces; u++) reach += __builtin_popcountll(__ballot(x[u] >= at));
+    if (reach >= n) key |= bit;
+  }
+  return key < 0x00800000u ? -INFINITY : value_of(key);  // below: nothing but NaN and -inf
+}
+
+// What a wavefront has written down.
+struct Held {
+  Entry *entries, *spare;  // LDS, kHeld of them each
+  int count = 0;
+  float bound = -INFINITY;  // what is among the best is as large or larger; of later chunks larger
+  Entry last = 0;           // and ahead of this one
+  // Keeps the n first.  A place is the number of entries ahead.
+  __device__ __forceinline__ void keep_best(int n) {
+    if (lane_id() < 8) entries[count + lane_id()] = 0;
+    wave_sync();
+#pragma unroll 1
+    for (int i = lane_id(); i < count; i += 64) {
+      const Entry mine = entries[i];
+      const int place = place_of(entries, count, mine);
+      if (place < n) spare[place] = mine;
+    }
+    wave_sync();
+    count = min(count, n);
+    if (lane_id() < count) entries[lane_id()] = spare[lane_id()];
+    wave_sync();
+    if (count == n) last = entries[n - 1], bound = value_of(last);
+  }
+  // Writes down the lanes' values in order of `bits`, each lane's lowest first.
+  template <typename Value, typename Index>
+  __device__ __forceinline__ void add(uint32_t bits, int n, float least, Value value, Index index) {
+#pragma unroll 1
+    while (__ballot(bits != 0)) {
+      if (count + 64 + 8 > kHeld) keep_best(n);
+      const int j = __builtin_ctz(bits | 0x80000000u);
+      const float v = value(j);
+      const Entry e = entry_of(v, index(j));
+      const bool some = bits != 0 && v >= least && e > last;
+      const unsigned long long lanes = __ballot(some);
+      if (some) entries[count + lanes_before(lanes)] = e;
+      count += __builtin_popcountll(lanes);
+      bits &= bits - 1;
     }
   }
 };
 
 template <typename T>
-__global__ __launch_bounds__(64 * kLogWaves) void logprobs_kernel(LogArgs a) {
-  constexpr int PER = Chunk<T>::PER, VALUES = Chunk<T>::VALUES;
+__global__ __launch_bounds__(64 * kLogWaves, 4) void logprobs_kernel(LogArgs a) {
+  constexpr int PER = Chunk<T>::PER, VALUES = Chunk<T>::VALUES, THREADS = 64 * kLogWaves;
   const int wave = uniform((int)threadIdx.x >> 6), lane = lane_id();
   const uint32_t row = a.parts.quotient(blockIdx.x), part = blockIdx.x - row * a.parts.by;
   const T* const x = (const T*)a.logits + (int64_t)row * a.stride;
+  __shared__ __align__(16) Entry entries[2 * kLogWaves * kHeld + 8];  // of the wavefronts; those that are left of all
   __shared__ LogStats wave_stats[kLogWaves];
-  __shared__ float list_values[kLogWaves][64];
-  __shared__ int list_indexes[kLogWaves][64];
+  __shared__ float bounds[kLogWaves];
+  __shared__ Entry best[64];
+  __shared__ Entry least_entry;
+  __shared__ int left_count;
   __shared__ bool is_last;
-  const int n_chunks = (a.vocab - 1) / VALUES + 1, end = min((int)(part + 1) * a.part_chunks, n_chunks);
   const int token = a.tokens ? a.tokens[row] : -1;
   const bool has_token = (uint32_t)token < (uint32_t)a.vocab;
-  const float given = has_token ? (float)x[token] : 0;
+  const T given = has_token ? x[token] : (T)0;
+  const bool ranked = has_token && a.rank;
 
   // x's scaled distance from m.  In 32 bits x may be as large as that type's values are: the difference first.
   auto scaled = [&](float v, float m) {
@@ -169,23 +237,22 @@ __global__ __launch_bounds__(64 * kLogWaves) void logprobs_kernel(LogArgs a) {
     const float from = before * a.scale2, to = m * a.scale2;
     return from - to;
   };
-  float m = -INFINITY, sums[4] = {0, 0, 0, 0}, moments[4] = {0, 0, 0, 0};
+  float m = -INFINITY, sums[4] = {0, 0, 0, 0}, moments[4] = {0, 0, 0, 0}, maxima[kPieces];
+#pragma unroll
+  for (int u = 0; u < kPieces; u++) maxima[u] = -INFINITY;
   int ahead = 0;
-  TopList list;
-  int chunk = (int)part * a.part_chunks + wave;
-  Chunk<T> now, next;
-  if (chunk < end) now.load(x, chunk * VALUES, a.vocab);
-  for (; chunk < end; chunk += kLogWaves) {
+  Held held = {entries + wave * kHeld, entries + (kLogWaves + wave) * kHeld};
+  // A wavefront's chunks lie kLogWaves apart: a workgroup's form one window.
+  const int begin = (int)part * a.part_turns * kLogWaves + wave, n_chunks = (a.vocab - 1) / VALUES + 1, end = min((int)(part + 1) * a.part_turns * kLogWaves, n_chunks);
+  // Nothing is asked for ahead: four workgroups to a compute unit ask for 128 KiB at a time.
+  for (int chunk = begin; chunk < end; chunk += kLogWaves) {
     const int first = chunk * VALUES;
-    if (chunk + kLogWaves < end) next.load(x, (chunk + kLogWaves) * VALUES, a.vocab);
-    float most[kPieces], top = -INFINITY;
+    Chunk<T> now;
+    now.load(x, first, a.vocab);
+    float most[kPieces];
 #pragma unroll
-    for (int u = 0; u < kPieces; u++) {
-      most[u] = -INFINITY;
-#pragma unroll
-      for (int j = 0; j < PER; j++) most[u] = fmaxf(most[u], now.value(u, j));
-      top = fmaxf(top, most[u]);
-    }
+    for (int u = 0; u < kPieces; u++) most[u] = now.largest(u), maxima[u] = fmaxf(maxima[u], most[u]);
+    const float top = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
     if (__ballot(top > m)) {
       const float before = m;
       m = max_over_wave(fmaxf(top, m));
@@ -196,113 +263,185 @@ __global__ __launch_bounds__(64 * kLogWaves) void logprobs_kernel(LogArgs a) {
       }
     }
     const float m_or_0 = m == -INFINITY ? 0.0f : m;
+    now.forget();
 #pragma unroll
-    for (int u = 0; u < kPieces; u++)
+    for (int u = 0; u < kPieces; u++) {
+      __builtin_amdgcn_sched_barrier(0);  // eight values at a time: more take registers
 #pragma unroll
       for (int j = 0; j < PER; j++) {
-        const float y = scaled(now.value(u, j), m_or_0), e = __builtin_amdgcn_exp2f(y);
+        const float y = scaled((float)now.value(u, j), m_or_0), e = __builtin_amdgcn_exp2f(y);
         sums[j & 3] += e;
         moments[j & 3] = __builtin_fmaf(e, fmaxf(y, -256.0f), moments[j & 3]);  // 2^y is 0 far above: so that 0 times an infinity is not asked for
       }
-    if (has_token && __ballot(top >= given)) {
-#pragma unroll
-      for (int u = 0; u < kPieces; u++)
-#pragma unroll
-        for (int j = 0; j < PER; j++) {
-          const float v = now.value(u, j);
-          const int i = Chunk<T>::index(first, u, j);
-          ahead += __builtin_popcountll(__ballot(i < a.vocab && (v > given || (v == given && i < token))));
-        }
     }
-    if (a.top > 0) {
-      const unsigned long long some = __ballot(!list.full() || top > list.last_value);
-      if (some) {
-        // where many lanes have candidates most of them are not among the best: as many lanes' maxima as there are places say so
-        const float least = __builtin_popcountll(some) > 6 ? nth_of_lanes(top, a.top - 1) : -INFINITY;
+    __builtin_amdgcn_sched_barrier(0);
+    if (ranked && __ballot(top >= (float)given)) {
+      auto count = [&](auto is_ahead) {
 #pragma unroll
-        for (int u = 0; u < kPieces; u++) {
-          if (!__ballot(most[u] >= least && most[u] >= list.last_value)) continue;
+        for (int u = 0; u < kPieces; u++)
 #pragma unroll
-          for (int j = 0; j < PER; j++) {
-            const int i = Chunk<T>::index(first, u, j);
-            list.offer(now.value(u, j), i < a.vocab ? i : INT_MAX, least, a.top);
-          }
-        }
+          for (int j = 0; j < PER; j++) ahead += __builtin_popcountll(__ballot(is_ahead(now.value(u, j), u, j)));
+      };
+      // of equal logits those that come before the token
+      now.forget();
+      if (first > token)
+        count([&](T v, int, int) { return v > given; });
+      else if (first + VALUES <= token)
+        count([&](T v, int, int) { return v >= given; });
+      else {
+        const int before = token - first - hidden(lane) * PER;  // values of the lane's first piece that come before it
+        count([&](T v, int u, int j) { return v > given || (v == given && j < before - u * 64 * PER); });
       }
     }
-    now = next;
+    if (a.top > 0 && __ballot(top > held.bound)) {
+      // the first chunk, or much that passes the bound: a better one, of all that has been seen
+      float least = -INFINITY;
+      if (chunk == begin || __builtin_popcountll(__ballot(top > held.bound)) > 24) least = a.top == 1 ? m : bound_of(maxima, a.top);
+      uint32_t pieces = 0;
+#pragma unroll
+      for (int u = 0; u < kPieces; u++) pieces |= __ballot(most[u] >= held.bound && most[u] >= least) ? 1u << u : 0u;
+#pragma unroll 1
+      for (; pieces; pieces &= pieces - 1) {
+        const int u = __builtin_ctz(pieces);
+        Chunk<T> piece;  // that one in place 0
+        now.forget();
+        piece.raw[0] = now.raw[0];
+#pragma unroll
+        for (int i = 1; i < kPieces; i++) piece.raw[0] = u == i ? now.raw[i] : piece.raw[0];
+        const float from = fmaxf(fmaxf(least, held.bound), -FLT_MAX);  // never -inf
+        uint32_t bits = 0;
+#pragma unroll
+        for (int j = 0; j < PER; j++) bits |= (float)piece.value(0, j) >= from ? 1u << j : 0u;
+        held.add(bits, a.top, least, [&](int j) {
+          T v = piece.value(0, 0);
+#pragma unroll
+          for (int i = 1; i < PER; i++) v = j == i ? piece.value(0, i) : v;
+          return (float)v;
+        }, [&](int j) { return Chunk<T>::index(first, u, j); });
+      }
+      if (least > held.bound) held.bound = least, held.last = entry_of(least, 0);  // equal ones that come later are not
+    }
   }
 
-  // The workgroup's wavefronts, then the row's workgroups: wave 0 joins statistics and lists, in order.
-  auto combine = [&](LogStats& s, LogStats t) {
-    const float most = fmaxf(s.top, t.top);
-    auto take = [&](const LogStats& p, float* sum, float* moment) {
-      if (p.top == -INFINITY) return *sum = p.sum, *moment = p.moment, void();  // 0, unless something was a NaN
-      const float less = moved(p.top, most), by = __builtin_amdgcn_exp2f(less);
-      *moment = by > 0 || by != by ? by * __builtin_fmaf(less, p.sum, p.moment) : 0.0f, *sum = p.sum * by;
-    };
-    float sum[2], moment[2];
-    take(s, &sum[0], &moment[0]), take(t, &sum[1], &moment[1]);
-    s = {most, sum[0] + sum[1], moment[0] + moment[1], s.ahead + t.ahead};
+  // Statistics of the workgroup's wavefronts, then of the row's workgroups, one to a lane: all of them for the largest maximum.
+  auto joined = [&](const LogStats& s) {
+    const float most = max_over_wave(s.top);
+    float sum = s.sum, moment = s.moment;
+    if (s.top != -INFINITY) {  // else 0, unless something was a NaN
+      const float less = moved(s.top, most), by = __builtin_amdgcn_exp2f(less);
+      moment = by > 0 ? by * __builtin_fmaf(less, sum, moment) : 0.0f, sum *= by;
+    }
+    return LogStats{most, sum_over_wave(sum), sum_over_wave(moment), (int)wave_sum((uint32_t)s.ahead)};
   };
-  LogStats mine = {m, sum_over_wave(sums[0] + sums[1] + (sums[2] + sums[3])), sum_over_wave(moments[0] + moments[1] + (moments[2] + moments[3])), ahead};
-  auto join_waves = [&] {
-    if (wave > 0) {
-      if (lane == 0) wave_stats[wave] = mine;
-      list_values[wave][lane] = list.value, list_indexes[wave][lane] = lane < a.top ? list.index : INT_MAX;
+  // What is left of several lists goes to `left`, and from there to its place.
+  Entry* const left = entries + kLogWaves * kHeld;
+  auto leave = [&](bool some, Entry e) {
+    const unsigned long long lanes = __ballot(some);
+    int at = 0;
+    if (lane == 0 && lanes) at = atomicAdd(&left_count, __builtin_popcountll(lanes));
+    at = uniform(at);
+    if (some) left[at + lanes_before(lanes)] = e;
+  };
+  auto count_out = [&] {
+    __syncthreads();
+    const int n = left_count;
+    if (threadIdx.x < 8) left[n + threadIdx.x] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += THREADS) {
+      const Entry e = left[i];
+      const int place = place_of(left, n, e);
+      if (place < a.top) best[place] = e;
     }
     __syncthreads();
-    if (wave == 0) {
-      for (int w = 1; w < kLogWaves; w++) {
-        combine(mine, wave_stats[w]);
-        if (a.top > 0) list.offer(list_values[w][lane], list_indexes[w][lane], -INFINITY, a.top);
-      }
-    }
   };
-  join_waves();
+  LogStats mine = {m, sum_over_wave(sums[0] + sums[1] + (sums[2] + sums[3])), sum_over_wave(moments[0] + moments[1] + (moments[2] + moments[3])), ahead};
+  if (lane == 0) wave_stats[wave] = mine, bounds[wave] = held.bound;
+  if (threadIdx.x < 64) best[threadIdx.x] = 0;
+  if (threadIdx.x == 0) left_count = 0;
+  __syncthreads();
+  if (a.top > 0) {
+    float bound = bounds[0];
+#pragma unroll
+    for (int w = 1; w < kLogWaves; w++) bound = fmaxf(bound, bounds[w]);
+    for (int i0 = 0; i0 < held.count; i0 += 64) {
+      const Entry e = held.entries[min(i0 + lane, held.count - 1)];
+      leave(i0 + lane < held.count && value_of(e) >= bound, e);
+    }
+    count_out();
+  }
+  const LogStats no_stats = {-INFINITY, 0, 0, 0};
+  if (wave == 0) mine = joined(lane < kLogWaves ? wave_stats[lane] : no_stats);
 
   if (a.parts.by > 1) {
-    const __amdgpu_buffer_rsrc_t left = __builtin_amdgcn_make_buffer_rsrc((void*)a.left, 0, a.left_bytes, 0x00020000);
+    const __amdgpu_buffer_rsrc_t share = __builtin_amdgcn_make_buffer_rsrc((void*)a.left, 0, a.left_bytes, 0x00020000);
     const int first = (int)(row * a.parts.by) * a.part_bytes;
     if (wave == 0) {
       const int at = first + (int)part * a.part_bytes;
-      if (lane == 0) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4, mine), left, at, 0, kDeviceScope);
-      if (lane < a.top) __builtin_amdgcn_raw_buffer_store_b64(u2{__builtin_bit_cast(uint32_t, list.value), (uint32_t)list.index}, left, at + 16 + 8 * lane, 0, kDeviceScope);
+      if (lane == 0) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4, mine), share, at, 0, kDeviceScope);
+      if (lane < a.top) __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u2, (Entry)best[lane]), share, at + 16 + 8 * lane, 0, kDeviceScope);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     if (threadIdx.x == 0) {
       is_last = __hip_atomic_fetch_add(a.counts + row, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == a.parts.by - 1;
       if (is_last) __hip_atomic_store(a.counts + row, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      left_count = 0, least_entry = 0;
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     if (!is_last) return;
-    list = TopList();
-    mine = {-INFINITY, 0, 0, 0};
-    for (int p = wave; p < (int)a.parts.by; p += kLogWaves) {
-      const int at = first + p * a.part_bytes;
-      combine(mine, __builtin_bit_cast(LogStats, (u4)__builtin_bit_cast(u4, __builtin_amdgcn_raw_buffer_load_b128(left, at, 0, kDeviceScope))));
-      if (a.top > 0) {
-        u2 entry = {0, INT_MAX};
-        if (lane < a.top) entry = __builtin_bit_cast(u2, __builtin_amdgcn_raw_buffer_load_b64(left, at + 16 + 8 * lane, 0, kDeviceScope));
-        list.offer(__builtin_bit_cast(float, (uint32_t)entry[0]), (int)entry[1], -INFINITY, a.top);
-      }
+    // what reaches the last of a whole list of some part
+    if (threadIdx.x < 64) best[threadIdx.x] = 0;
+    const int n = (int)a.parts.by * a.top;
+    Entry theirs_best[kMaxRowParts * AMS_LOGPROBS_MAX_TOP / THREADS], bound = 0;
+#pragma unroll
+    for (int k = 0; k < kMaxRowParts * AMS_LOGPROBS_MAX_TOP / THREADS; k++) {
+      const int i = k * THREADS + (int)threadIdx.x, p = (int)a.by_top.quotient((uint32_t)i);
+      theirs_best[k] = 0;
+      if (k * THREADS < n) theirs_best[k] = __builtin_bit_cast(Entry, __builtin_amdgcn_raw_buffer_load_b64(share, i < n ? first + p * a.part_bytes + 16 + 8 * (i - p * a.top) : 0x7FFE0000, 0, kDeviceScope));
     }
-    join_waves();
+    LogStats theirs = no_stats;
+    if (wave == 0 && lane < (int)a.parts.by) theirs = __builtin_bit_cast(LogStats, (u4)__builtin_bit_cast(u4, __builtin_amdgcn_raw_buffer_load_b128(share, first + lane * a.part_bytes, 0, kDeviceScope)));
+    if (a.top > 0) {
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < kMaxRowParts * AMS_LOGPROBS_MAX_TOP / THREADS; k++) {
+        const int i = k * THREADS + (int)threadIdx.x;
+        if (i < n && (i + 1) % a.top == 0 && theirs_best[k]) atomicMax((unsigned long long*)&least_entry, (unsigned long long)theirs_best[k]);
+      }
+      __syncthreads();
+      bound = least_entry;
+#pragma unroll
+      for (int k = 0; k < kMaxRowParts * AMS_LOGPROBS_MAX_TOP / THREADS; k++)
+        if (k * THREADS < n) leave(theirs_best[k] != 0 && theirs_best[k] >= bound, theirs_best[k]);
+      count_out();
+    }
+    if (wave > 0) return;
+    mine = joined(theirs);
   }
   if (wave > 0) return;
   const float total = __log2f(mine.sum);
   auto log_probability = [&](float v) { return v == -INFINITY && mine.sum == mine.sum ? -INFINITY : (scaled(v, mine.top) - total) * 0.69314718056f; };
   if (lane == 0) {
-    if (a.logprob) a.logprob[row] = has_token ? log_probability(given) : 0.0f;
+    if (a.logprob) a.logprob[row] = has_token ? log_probability((float)given) : 0.0f;
     if (a.rank) a.rank[row] = has_token ? mine.ahead : -1;
     if (a.entropy) a.entropy[row] = mine.top == -INFINITY && mine.sum == 0 ? 0.0f : (total - mine.moment / mine.sum) * 0.69314718056f;
   }
+  if (a.top == 0) return;
+  // Fewer logits above -inf than places: then the first tokens with -inf; behind them none.
+  const int found = min(__builtin_popcountll(__ballot(best[lane] != 0)), a.top);
+  int filled = found;
+  for (int i0 = 0; i0 < a.vocab && filled < a.top; i0 += 64) {
+    const unsigned long long some = __ballot(i0 + lane < a.vocab && (float)x[min(i0 + lane, a.vocab - 1)] == -INFINITY);
+    const int place = filled + lanes_before(some);
+    if ((some >> lane & 1) && place < a.top) best[place] = entry_of(-INFINITY, i0 + lane);
+    filled += __builtin_popcountll(some);
+  }
+  wave_sync();
   if (lane < a.top) {
-    const bool there = list.index != INT_MAX;  // fewer tokens than places: none
-    a.top_logprobs[(int64_t)row * a.top + lane] = there ? log_probability(list.value) : -INFINITY;
-    a.top_tokens[(int64_t)row * a.top + lane] = there ? list.index : -1;
+    const Entry e = best[lane];
+    a.top_logprobs[(int64_t)row * a.top + lane] = e ? log_probability(value_of(e)) : -INFINITY;
+    a.top_tokens[(int64_t)row * a.top + lane] = e ? index_of(e) : -1;
   }
 }
 
@@ -310,24 +449,24 @@ bool load_logprobs() { return loaded((const void*)logprobs_kernel<float>); }
 
 // Workgroups of a row.
 struct LogPlan {
-  int parts, part_chunks, part_bytes;
+  int parts, part_turns, part_bytes;
   size_t workspace;
 };
 static LogPlan log_plan(int type, int64_t rows, int64_t vocab, int top, size_t workspace) {
-  const int64_t values = type == AMS_TYPE_FP32 ? Chunk<float>::VALUES : Chunk<_Float16>::VALUES;
-  const int64_t chunks = std::max<int64_t>((vocab + values - 1) / values, 1);
-  LogPlan p = {1, (int)chunks, 16 + 8 * top, 0};
-  constexpr int64_t kWorkgroups = 1024;
-  int64_t parts = std::min<int64_t>(std::min<int64_t>((chunks + kLogWaves - 1) / kLogWaves, kMaxRowParts), rows > 0 ? kWorkgroups / rows : 1);
-  if (rows * (int64_t)sizeof(uint32_t) > (int64_t)kLogCountBytes) parts = 1;
-  if (parts < 2) return p;
-  p.part_chunks = (int)((chunks + parts - 1) / parts);
-  p.parts = (int)((chunks + p.part_chunks - 1) / p.part_chunks);
-  p.part_bytes = (p.part_bytes + 15) / 16 * 16;
+  const int64_t values = kLogWaves * (type == AMS_TYPE_FP32 ? Chunk<float>::VALUES : Chunk<_Float16>::VALUES), turns = std::max<int64_t>((vocab + values - 1) / values, 1);
+  const LogPlan whole = {1, (int)turns, 0, 0};
+  constexpr int64_t kWorkgroups = 512;
+  const int64_t parts = std::min<int64_t>(std::min<int64_t>(turns, kMaxRowParts), rows > 0 ? kWorkgroups / rows : 1);
+  if (parts < 2) return whole;
+  LogPlan p = whole;
+  p.part_turns = (int)((turns + parts - 1) / parts);
+  p.parts = (int)((turns + p.part_turns - 1) / p.part_turns);
+  p.part_bytes = (16 + 8 * top + 15) / 16 * 16;
   p.workspace = kLogCountBytes + (size_t)(rows * p.parts) * p.part_bytes;
-  if (p.parts < 2 || workspace < p.workspace) return {1, (int)chunks, 16 + 8 * top, 0};
-  return p;
+  return p.parts < 2 || workspace < p.workspace ? whole : p;
 }
+static_assert(512 * sizeof(uint32_t) <= kLogCountBytes, "a count for each row that is shared out");
+static_assert(kMaxRowParts * AMS_LOGPROBS_MAX_TOP <= kLogWaves * kHeld, "the parts' lists fit in LDS");
 static bool log_sizes_ok(int type, int64_t rows, int64_t vocab, int top) {
   return (type == AMS_TYPE_FP16 || type == AMS_TYPE_FP32) && rows >= 0 && rows <= AMS_KV_MAX_TOKENS && vocab >= 1 && vocab <= AMS_LOGPROBS_MAX_VOCAB && top >= 0 && top <= AMS_LOGPROBS_MAX_TOP;
 }
@@ -359,7 +498,7 @@ int ams_logprobs(const void* logits, int type, int64_t rows, int64_t vocab, int6
   a.logits = logits, a.stride = stride, a.tokens = tokens, a.logprob = logprob, a.entropy = entropy, a.rank = rank, a.top_logprobs = top_logprobs, a.top_tokens = top_tokens;
   a.counts = (uint32_t*)workspace, a.left = (uint8_t*)workspace + kLogCountBytes;
   a.vocab = (int)vocab, a.top = top, a.scale2 = (float)(1.4426950408889634 / temperature);
-  a.part_chunks = p.part_chunks, a.part_bytes = p.part_bytes, a.left_bytes = (uint32_t)(p.workspace ? p.workspace - kLogCountBytes : 0), a.parts = divisor((uint32_t)p.parts);
+  a.part_turns = p.part_turns, a.part_bytes = p.part_bytes, a.left_bytes = (uint32_t)(p.workspace ? p.workspace - kLogCountBytes : 0), a.parts = divisor((uint32_t)p.parts), a.by_top = divisor((uint32_t)std::max(top, 1));
   const unsigned grid = (unsigned)(rows * p.parts);
   if (type == AMS_TYPE_FP32)
     hipLaunchKernelGGL(logprobs_kernel<float>, dim3(grid), dim3(64 * kLogWaves), 0, (hipStream_t)stream, a);
