@@ -22,9 +22,9 @@
 
 namespace ams_kv {
 
-constexpr int kLogWaves = 8;
 constexpr size_t kLogCountBytes = 64 * 1024;  // of a workspace: one count for each row, at its front
 constexpr int kMaxRowParts = 32;
+constexpr int kWholeWaves = 4, kPartWaves = 8;  // of a workgroup that has a whole row of many, or a part of one
 constexpr int kHeld = 256;  // values that a wavefront writes down at most
 
 struct LogArgs {
@@ -57,17 +57,20 @@ __device__ __forceinline__ Entry entry_of(float value, int index) {
 __device__ __forceinline__ float value_of(uint32_t key) { return __builtin_bit_cast(float, key & 0x80000000u ? key & 0x7FFFFFFFu : ~key); }
 __device__ __forceinline__ float value_of(Entry e) { return value_of((uint32_t)(e >> 32)); }
 __device__ __forceinline__ int index_of(Entry e) { return (int)~(uint32_t)e; }
-// How many of the entries are ahead of one; they are `n` rounded up to a multiple of 8, the others 0.
+// How many of n entries are ahead of one; up to seven behind them are read, too.
+template <int AT_ONCE>
 __device__ __forceinline__ int place_of(const Entry* entries, int n, Entry mine) {
-  int place = 0;
+  int place = 0, i = 0;
+  auto batch = [&](auto there) {
+    Entry e[AT_ONCE];
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; j++) e[j] = entries[i + j];
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; j++) place += (int)(e[j] > mine) & (int)there(j);
+  };
 #pragma unroll 1
-  for (int i = 0; i < n; i += 8) {
-    Entry e[8];
-#pragma unroll
-    for (int j = 0; j < 8; j++) e[j] = entries[i + j];
-#pragma unroll
-    for (int j = 0; j < 8; j++) place += e[j] > mine;
-  }
+  for (; i + AT_ONCE <= n; i += AT_ONCE) batch([](int) { return true; });
+  if (i < n) batch([&](int j) { return i + j < n; });
   return place;
 }
 
@@ -150,17 +153,30 @@ struct Chunk {
   }
 };
 
-// A bound that n of the wavefront's 256 values reach, as near to the n-th largest as 19 bits of it are; -inf where fewer are above
-// that.  Bisection of the bits in the order of the values.
+// The next smaller value of a type (of -inf and NaN themselves).
+__device__ __forceinline__ float next_below(float x) {
+  const int bits = __builtin_bit_cast(int, x);
+  if (x == 0) return __builtin_bit_cast(float, 0x80000001u);
+  return x > -INFINITY ? __builtin_bit_cast(float, bits < 0 ? bits + 1 : bits - 1) : x;
+}
+__device__ __forceinline__ _Float16 next_below(_Float16 x) {
+  const short bits = __builtin_bit_cast(short, x);
+  if (x == (_Float16)0) return __builtin_bit_cast(_Float16, (short)0x8001);
+  return x > (_Float16)-INFINITY ? __builtin_bit_cast(_Float16, (short)(bits < 0 ? bits + 1 : bits - 1)) : x;
+}
+
+// A bound that n of the wavefront's 256 values reach and few others, -inf where fewer are above that.  Bisection of the bits in the order of
+// the values, of 19 at most (all that fp16 values have), until no more than n reach it.
 __device__ __forceinline__ float bound_of(const float (&x)[kPieces], int n) {
   uint32_t key = 0;
 #pragma unroll 1
-  for (uint32_t bit = 0x80000000u; bit >= 0x2000u; bit >>= 1) {  // 19 bits: of fp16 values all
+  for (uint32_t bit = 0x80000000u; bit >= 0x2000u; bit >>= 1) {
     const float at = value_of(key | bit);
     int reach = 0;
 #pragma unroll
     for (int u = 0; u < kPieces; u++) reach += __builtin_popcountll(__ballot(x[u] >= at));
     if (reach >= n) key |= bit;
+    if (reach == n) break;
   }
   return key < 0x00800000u ? -INFINITY : value_of(key);  // below: nothing but NaN and -inf
 }
@@ -173,12 +189,11 @@ struct Held {
   Entry last = 0;           // and ahead of this one
   // Keeps the n first.  A place is the number of entries ahead.
   __device__ __forceinline__ void keep_best(int n) {
-    if (lane_id() < 8) entries[count + lane_id()] = 0;
     wave_sync();
 #pragma unroll 1
     for (int i = lane_id(); i < count; i += 64) {
       const Entry mine = entries[i];
-      const int place = place_of(entries, count, mine);
+      const int place = place_of<2>(entries, count, mine);
       if (place < n) spare[place] = mine;
     }
     wave_sync();
@@ -192,7 +207,7 @@ struct Held {
   __device__ __forceinline__ void add(uint32_t bits, int n, float least, Value value, Index index) {
 #pragma unroll 1
     while (__ballot(bits != 0)) {
-      if (count + 64 + 8 > kHeld) keep_best(n);
+      if (count + 64 > kHeld) keep_best(n);
       const int j = __builtin_ctz(bits | 0x80000000u);
       const float v = value(j);
       const Entry e = entry_of(v, index(j));
@@ -205,22 +220,27 @@ struct Held {
   }
 };
 
-template <typename T>
-__global__ __launch_bounds__(64 * kLogWaves, 4) void logprobs_kernel(LogArgs a) {
-  constexpr int PER = Chunk<T>::PER, VALUES = Chunk<T>::VALUES, THREADS = 64 * kLogWaves;
+template <typename T, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 4) void logprobs_kernel(LogArgs a) {
+  constexpr int PER = Chunk<T>::PER, VALUES = Chunk<T>::VALUES, THREADS = 64 * WAVES;
   const int wave = uniform((int)threadIdx.x >> 6), lane = lane_id();
   const uint32_t row = a.parts.quotient(blockIdx.x), part = blockIdx.x - row * a.parts.by;
   const T* const x = (const T*)a.logits + (int64_t)row * a.stride;
-  __shared__ __align__(16) Entry entries[2 * kLogWaves * kHeld + 8];  // of the wavefronts; those that are left of all
-  __shared__ LogStats wave_stats[kLogWaves];
-  __shared__ float bounds[kLogWaves];
+  __shared__ __align__(16) Entry entries[2 * WAVES * kHeld + 8];  // of the wavefronts; those that are left of all
+  __shared__ LogStats wave_stats[WAVES], row_stats;
+  __shared__ float bounds[WAVES];
   __shared__ Entry best[64];
   __shared__ Entry least_entry;
   __shared__ int left_count;
   __shared__ bool is_last;
+  if (threadIdx.x < 64) best[threadIdx.x] = 0;
+  if (threadIdx.x < WAVES) bounds[threadIdx.x] = -INFINITY;
+  if (threadIdx.x == 0) left_count = 0;
+  __syncthreads();
   const int token = a.tokens ? a.tokens[row] : -1;
   const bool has_token = (uint32_t)token < (uint32_t)a.vocab;
   const T given = has_token ? x[token] : (T)0;
+  const T below_given = next_below(given);
   const bool ranked = has_token && a.rank;
 
   // x's scaled distance from m.  In 32 bits x may be as large as that type's values are: the difference first.
@@ -241,11 +261,12 @@ __global__ __launch_bounds__(64 * kLogWaves, 4) void logprobs_kernel(LogArgs a) 
 #pragma unroll
   for (int u = 0; u < kPieces; u++) maxima[u] = -INFINITY;
   int ahead = 0;
-  Held held = {entries + wave * kHeld, entries + (kLogWaves + wave) * kHeld};
-  // A wavefront's chunks lie kLogWaves apart: a workgroup's form one window.
-  const int begin = (int)part * a.part_turns * kLogWaves + wave, n_chunks = (a.vocab - 1) / VALUES + 1, end = min((int)(part + 1) * a.part_turns * kLogWaves, n_chunks);
+  int enough = 0;  // entries from which on a nearer bound is worth finding
+  Held held = {entries + wave * kHeld, entries + (WAVES + wave) * kHeld};
+  // A wavefront's chunks lie WAVES apart: a workgroup's form one window.
+  const int begin = (int)part * a.part_turns * WAVES + wave, n_chunks = (a.vocab - 1) / VALUES + 1, end = min((int)(part + 1) * a.part_turns * WAVES, n_chunks);
   // Nothing is asked for ahead: four workgroups to a compute unit ask for 128 KiB at a time.
-  for (int chunk = begin; chunk < end; chunk += kLogWaves) {
+  for (int chunk = begin; chunk < end; chunk += WAVES) {
     const int first = chunk * VALUES;
     Chunk<T> now;
     now.load(x, first, a.vocab);
@@ -275,28 +296,36 @@ __global__ __launch_bounds__(64 * kLogWaves, 4) void logprobs_kernel(LogArgs a) 
       }
     }
     __builtin_amdgcn_sched_barrier(0);
+    now.forget();
     if (ranked && __ballot(top >= (float)given)) {
-      auto count = [&](auto is_ahead) {
+      // larger ones; of equal logits those that come before the token
+      const T above = first + VALUES <= token ? below_given : given;
+#pragma unroll
+      for (int u = 0; u < kPieces; u++)
+#pragma unroll
+        for (int j = 0; j < PER; j++) ahead += __builtin_popcountll(__ballot(now.value(u, j) > above));
+      if (first <= token && (token < first + VALUES || given == (T)-INFINITY)) {  // nothing is below -inf
+        const int before = token - first - hidden(lane) * PER;  // values of the lane's first piece that come before it
 #pragma unroll
         for (int u = 0; u < kPieces; u++)
 #pragma unroll
-          for (int j = 0; j < PER; j++) ahead += __builtin_popcountll(__ballot(is_ahead(now.value(u, j), u, j)));
-      };
-      // of equal logits those that come before the token
-      now.forget();
-      if (first > token)
-        count([&](T v, int, int) { return v > given; });
-      else if (first + VALUES <= token)
-        count([&](T v, int, int) { return v >= given; });
-      else {
-        const int before = token - first - hidden(lane) * PER;  // values of the lane's first piece that come before it
-        count([&](T v, int u, int j) { return v > given || (v == given && j < before - u * 64 * PER); });
+          for (int j = 0; j < PER; j++) ahead += __builtin_popcountll(__ballot(now.value(u, j) == given && j < before - u * 64 * PER));
       }
     }
-    if (a.top > 0 && __ballot(top > held.bound)) {
-      // the first chunk, or much that passes the bound: a better one, of all that has been seen
-      float least = -INFINITY;
-      if (chunk == begin || __builtin_popcountll(__ballot(top > held.bound)) > 24) least = a.top == 1 ? m : bound_of(maxima, a.top);
+    now.forget();
+    float least = -INFINITY;
+    if (a.top > 0) {  // what the other wavefronts know: n values of theirs reach it
+#pragma unroll
+      for (int w = 0; w < WAVES; w++) least = fmaxf(least, __hip_atomic_load(&bounds[w], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP));
+    }
+    if (a.top > 0 && __ballot(top > held.bound && top >= least)) {
+      // the first chunk, much that passes the bound or much written down since: a better one, of all that has been seen
+      float own = -INFINITY;
+      if (chunk == begin || held.count >= enough || __builtin_popcountll(__ballot(top > held.bound && top >= least)) > 24) {
+        own = a.top == 1 ? m : bound_of(maxima, a.top);
+        least = fmaxf(least, own);
+        enough = held.count + max(a.top, 16);
+      }
       uint32_t pieces = 0;
 #pragma unroll
       for (int u = 0; u < kPieces; u++) pieces |= __ballot(most[u] >= held.bound && most[u] >= least) ? 1u << u : 0u;
@@ -304,22 +333,22 @@ __global__ __launch_bounds__(64 * kLogWaves, 4) void logprobs_kernel(LogArgs a) 
       for (; pieces; pieces &= pieces - 1) {
         const int u = __builtin_ctz(pieces);
         Chunk<T> piece;  // that one in place 0
-        now.forget();
         piece.raw[0] = now.raw[0];
 #pragma unroll
         for (int i = 1; i < kPieces; i++) piece.raw[0] = u == i ? now.raw[i] : piece.raw[0];
         const float from = fmaxf(fmaxf(least, held.bound), -FLT_MAX);  // never -inf
-        uint32_t bits = 0;
+        uint32_t some = 0;
 #pragma unroll
-        for (int j = 0; j < PER; j++) bits |= (float)piece.value(0, j) >= from ? 1u << j : 0u;
-        held.add(bits, a.top, least, [&](int j) {
+        for (int j = 0; j < PER; j++) some |= (float)piece.value(0, j) >= from ? 1u << j : 0u;
+        held.add(some, a.top, least, [&](int j) {
           T v = piece.value(0, 0);
 #pragma unroll
           for (int i = 1; i < PER; i++) v = j == i ? piece.value(0, i) : v;
           return (float)v;
         }, [&](int j) { return Chunk<T>::index(first, u, j); });
       }
-      if (least > held.bound) held.bound = least, held.last = entry_of(least, 0);  // equal ones that come later are not
+      if (own > held.bound) held.bound = own, held.last = entry_of(own, 0);  // equal ones that come later are not
+      if (lane == 0) __hip_atomic_store(&bounds[wave], held.bound, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
     }
   }
 
@@ -334,7 +363,7 @@ __global__ __launch_bounds__(64 * kLogWaves, 4) void logprobs_kernel(LogArgs a) 
     return LogStats{most, sum_over_wave(sum), sum_over_wave(moment), (int)wave_sum((uint32_t)s.ahead)};
   };
   // What is left of several lists goes to `left`, and from there to its place.
-  Entry* const left = entries + kLogWaves * kHeld;
+  Entry* const left = entries + WAVES * kHeld;
   auto leave = [&](bool some, Entry e) {
     const unsigned long long lanes = __ballot(some);
     int at = 0;
@@ -345,32 +374,34 @@ __global__ __launch_bounds__(64 * kLogWaves, 4) void logprobs_kernel(LogArgs a) 
   auto count_out = [&] {
     __syncthreads();
     const int n = left_count;
-    if (threadIdx.x < 8) left[n + threadIdx.x] = 0;
-    __syncthreads();
     for (int i = threadIdx.x; i < n; i += THREADS) {
       const Entry e = left[i];
-      const int place = place_of(left, n, e);
+      const int place = place_of<8>(left, n, e);
       if (place < a.top) best[place] = e;
     }
     __syncthreads();
   };
+  const LogStats no_stats = {-INFINITY, 0, 0, 0};
   LogStats mine = {m, sum_over_wave(sums[0] + sums[1] + (sums[2] + sums[3])), sum_over_wave(moments[0] + moments[1] + (moments[2] + moments[3])), ahead};
-  if (lane == 0) wave_stats[wave] = mine, bounds[wave] = held.bound;
-  if (threadIdx.x < 64) best[threadIdx.x] = 0;
-  if (threadIdx.x == 0) left_count = 0;
+  if (lane == 0) wave_stats[wave] = mine;
   __syncthreads();
+  // wave 0 joins the statistics; where lists are joined too the last one does so meanwhile
+  const int joins = a.top > 0 ? WAVES - 1 : 0;
+  if (wave == joins) {
+    mine = joined(lane < WAVES ? wave_stats[lane] : no_stats);
+    if (lane == 0) row_stats = mine;
+  }
   if (a.top > 0) {
     float bound = bounds[0];
 #pragma unroll
-    for (int w = 1; w < kLogWaves; w++) bound = fmaxf(bound, bounds[w]);
+    for (int w = 1; w < WAVES; w++) bound = fmaxf(bound, bounds[w]);
     for (int i0 = 0; i0 < held.count; i0 += 64) {
       const Entry e = held.entries[min(i0 + lane, held.count - 1)];
       leave(i0 + lane < held.count && value_of(e) >= bound, e);
     }
     count_out();
   }
-  const LogStats no_stats = {-INFINITY, 0, 0, 0};
-  if (wave == 0) mine = joined(lane < kLogWaves ? wave_stats[lane] : no_stats);
+  if (a.top > 0) mine = row_stats;
 
   if (a.parts.by > 1) {
     const __amdgpu_buffer_rsrc_t share = __builtin_amdgcn_make_buffer_rsrc((void*)a.left, 0, a.left_bytes, 0x00020000);
@@ -400,24 +431,29 @@ __global__ __launch_bounds__(64 * kLogWaves, 4) void logprobs_kernel(LogArgs a) 
       theirs_best[k] = 0;
       if (k * THREADS < n) theirs_best[k] = __builtin_bit_cast(Entry, __builtin_amdgcn_raw_buffer_load_b64(share, i < n ? first + p * a.part_bytes + 16 + 8 * (i - p * a.top) : 0x7FFE0000, 0, kDeviceScope));
     }
-    LogStats theirs = no_stats;
-    if (wave == 0 && lane < (int)a.parts.by) theirs = __builtin_bit_cast(LogStats, (u4)__builtin_bit_cast(u4, __builtin_amdgcn_raw_buffer_load_b128(share, first + lane * a.part_bytes, 0, kDeviceScope)));
+    LogStats theirs = no_stats;  // of the parts
+    if (wave == joins && lane < (int)a.parts.by) theirs = __builtin_bit_cast(LogStats, (u4)__builtin_bit_cast(u4, __builtin_amdgcn_raw_buffer_load_b128(share, first + lane * a.part_bytes, 0, kDeviceScope)));
+    if (wave == joins) {
+      mine = joined(theirs);
+      if (lane == 0) row_stats = mine;
+    }
     if (a.top > 0) {
-      __syncthreads();
+      if (n > 256) __syncthreads();
 #pragma unroll
       for (int k = 0; k < kMaxRowParts * AMS_LOGPROBS_MAX_TOP / THREADS; k++) {
         const int i = k * THREADS + (int)threadIdx.x;
-        if (i < n && (i + 1) % a.top == 0 && theirs_best[k]) atomicMax((unsigned long long*)&least_entry, (unsigned long long)theirs_best[k]);
+        if (n > 256 && i < n && (i + 1) % a.top == 0 && theirs_best[k]) atomicMax((unsigned long long*)&least_entry, (unsigned long long)theirs_best[k]);
       }
-      __syncthreads();
-      bound = least_entry;
+      if (n > 256) {
+        __syncthreads();
+        bound = least_entry;
+      }
 #pragma unroll
       for (int k = 0; k < kMaxRowParts * AMS_LOGPROBS_MAX_TOP / THREADS; k++)
         if (k * THREADS < n) leave(theirs_best[k] != 0 && theirs_best[k] >= bound, theirs_best[k]);
       count_out();
+      mine = row_stats;
     }
-    if (wave > 0) return;
-    mine = joined(theirs);
   }
   if (wave > 0) return;
   const float total = __log2f(mine.sum);
@@ -445,28 +481,28 @@ __global__ __launch_bounds__(64 * kLogWaves, 4) void logprobs_kernel(LogArgs a) 
   }
 }
 
-bool load_logprobs() { return loaded((const void*)logprobs_kernel<float>); }
+bool load_logprobs() { return loaded((const void*)logprobs_kernel<float, 8>); }
 
-// Workgroups of a row.
+// Workgroups of a row.  Eight wavefronts to a workgroup up to as many as the chip holds, beyond that four.
+constexpr int64_t kWorkgroups = 512;
 struct LogPlan {
-  int parts, part_turns, part_bytes;
+  int waves, parts, part_turns, part_bytes;
   size_t workspace;
 };
 static LogPlan log_plan(int type, int64_t rows, int64_t vocab, int top, size_t workspace) {
-  const int64_t values = kLogWaves * (type == AMS_TYPE_FP32 ? Chunk<float>::VALUES : Chunk<_Float16>::VALUES), turns = std::max<int64_t>((vocab + values - 1) / values, 1);
-  const LogPlan whole = {1, (int)turns, 0, 0};
-  constexpr int64_t kWorkgroups = 512;
+  const int64_t values = type == AMS_TYPE_FP32 ? Chunk<float>::VALUES : Chunk<_Float16>::VALUES, chunks = (vocab + values - 1) / values;
+  const int waves = rows > kWorkgroups ? kWholeWaves : kPartWaves;
+  const LogPlan whole = {waves, 1, (int)((chunks + waves - 1) / waves), 0, 0};
+  const int64_t turns = (chunks + kPartWaves - 1) / kPartWaves;
   const int64_t parts = std::min<int64_t>(std::min<int64_t>(turns, kMaxRowParts), rows > 0 ? kWorkgroups / rows : 1);
   if (parts < 2) return whole;
-  LogPlan p = whole;
-  p.part_turns = (int)((turns + parts - 1) / parts);
+  LogPlan p = {kPartWaves, 0, (int)((turns + parts - 1) / parts), (16 + 8 * top + 15) / 16 * 16, 0};
   p.parts = (int)((turns + p.part_turns - 1) / p.part_turns);
-  p.part_bytes = (16 + 8 * top + 15) / 16 * 16;
   p.workspace = kLogCountBytes + (size_t)(rows * p.parts) * p.part_bytes;
-  return p.parts < 2 || workspace < p.workspace ? whole : p;
+  return workspace < p.workspace ? whole : p;
 }
 static_assert(512 * sizeof(uint32_t) <= kLogCountBytes, "a count for each row that is shared out");
-static_assert(kMaxRowParts * AMS_LOGPROBS_MAX_TOP <= kLogWaves * kHeld, "the parts' lists fit in LDS");
+static_assert(kMaxRowParts * AMS_LOGPROBS_MAX_TOP <= kPartWaves * kHeld, "the parts' lists fit in LDS");
 static bool log_sizes_ok(int type, int64_t rows, int64_t vocab, int top) {
   return (type == AMS_TYPE_FP16 || type == AMS_TYPE_FP32) && rows >= 0 && rows <= AMS_KV_MAX_TOKENS && vocab >= 1 && vocab <= AMS_LOGPROBS_MAX_VOCAB && top >= 0 && top <= AMS_LOGPROBS_MAX_TOP;
 }
@@ -500,10 +536,11 @@ int ams_logprobs(const void* logits, int type, int64_t rows, int64_t vocab, int6
   a.vocab = (int)vocab, a.top = top, a.scale2 = (float)(1.4426950408889634 / temperature);
   a.part_turns = p.part_turns, a.part_bytes = p.part_bytes, a.left_bytes = (uint32_t)(p.workspace ? p.workspace - kLogCountBytes : 0), a.parts = divisor((uint32_t)p.parts), a.by_top = divisor((uint32_t)std::max(top, 1));
   const unsigned grid = (unsigned)(rows * p.parts);
+  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * p.waves), 0, (hipStream_t)stream, a); };
   if (type == AMS_TYPE_FP32)
-    hipLaunchKernelGGL(logprobs_kernel<float>, dim3(grid), dim3(64 * kLogWaves), 0, (hipStream_t)stream, a);
+    p.waves == kWholeWaves ? launch(logprobs_kernel<float, kWholeWaves>) : launch(logprobs_kernel<float, kPartWaves>);
   else
-    hipLaunchKernelGGL(logprobs_kernel<_Float16>, dim3(grid), dim3(64 * kLogWaves), 0, (hipStream_t)stream, a);
+    p.waves == kWholeWaves ? launch(logprobs_kernel<_Float16, kWholeWaves>) : launch(logprobs_kernel<_Float16, kPartWaves>);
   return hipGetLastError() == hipSuccess ? AMS_OK : AMS_ERR_LAUNCH;
 }
 
