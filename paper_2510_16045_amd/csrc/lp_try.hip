@@ -50,10 +50,11 @@ struct LogStats {
 // A token and its logit in one number that is the larger the further ahead the token is: the value's bits in the order of the values (of
 // both zeros the same), then the lower index.  0: none.
 typedef uint64_t Entry;
-__device__ __forceinline__ Entry entry_of(float value, int index) {
-  const uint32_t bits = __builtin_bit_cast(uint32_t, value + 0.0f);
-  return (uint64_t)(bits & 0x80000000u ? ~bits : bits | 0x80000000u) << 32 | ~(uint32_t)index;
+__device__ __forceinline__ uint32_t key_of(float value) {
+  const int bits = __builtin_bit_cast(int, value + 0.0f);
+  return (uint32_t)(bits ^ (bits >> 31 | (int)0x80000000));
 }
+__device__ __forceinline__ Entry entry_of(float value, int index) { return (uint64_t)key_of(value) << 32 | ~(uint32_t)index; }
 __device__ __forceinline__ float value_of(uint32_t key) { return __builtin_bit_cast(float, key & 0x80000000u ? key & 0x7FFFFFFFu : ~key); }
 __device__ __forceinline__ float value_of(Entry e) { return value_of((uint32_t)(e >> 32)); }
 __device__ __forceinline__ int index_of(Entry e) { return (int)~(uint32_t)e; }
@@ -165,20 +166,26 @@ __device__ __forceinline__ _Float16 next_below(_Float16 x) {
   return x > (_Float16)-INFINITY ? __builtin_bit_cast(_Float16, (short)(bits < 0 ? bits + 1 : bits - 1)) : x;
 }
 
-// A bound that n of the wavefront's 256 values reach and few others, -inf where fewer are above that.  Bisection of the bits in the order of
-// the values, of 19 at most (all that fp16 values have), until no more than n reach it.
-__device__ __forceinline__ float bound_of(const float (&x)[kPieces], int n) {
-  uint32_t key = 0;
+// A bound that n of the wavefront's 256 values reach and few others, -inf where fewer are above that; `most` is the largest of them.  Bisection
+// of the bits in the order of the values, from the first in which they differ on, of 19 at most (all that fp16 values have), until no more
+// than n reach it.
+__device__ __forceinline__ float bound_of(const float (&x)[kPieces], float most, int n) {
+  uint32_t keys[kPieces];
+#pragma unroll
+  for (int u = 0; u < kPieces; u++) keys[u] = key_of(x[u]);
+  const uint32_t high = (uint32_t)uniform((int)key_of(most)), low = (uint32_t)uniform((int)key_of(-max_over_wave(-fminf(fminf(x[0], x[1]), fminf(x[2], x[3])))));
+  const int first = high == low ? 0 : 31 - __builtin_clz(high ^ low);
+  uint32_t key = high == low ? high : high & ~((2u << first) - 1);
 #pragma unroll 1
-  for (uint32_t bit = 0x80000000u; bit >= 0x2000u; bit >>= 1) {
-    const float at = value_of(key | bit);
+  for (int bit = first; bit >= 13; bit--) {
+    const uint32_t at = key | 1u << bit;
     int reach = 0;
 #pragma unroll
-    for (int u = 0; u < kPieces; u++) reach += __builtin_popcountll(__ballot(x[u] >= at));
-    if (reach >= n) key |= bit;
+    for (int u = 0; u < kPieces; u++) reach += __builtin_popcountll(__ballot(keys[u] >= at));
+    if (reach >= n) key = at;
     if (reach == n) break;
   }
-  return key < 0x00800000u ? -INFINITY : value_of(key);  // below: nothing but NaN and -inf
+  return key < 0x00800000u ? -INFINITY : value_of(key);  // below: nothing but -inf
 }
 
 // What a wavefront has written down.
@@ -221,7 +228,7 @@ struct Held {
 };
 
 template <typename T, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 6) void logprobs_kernel(LogArgs a) {
+__global__ __launch_bounds__(64 * WAVES, 4) void logprobs_kernel(LogArgs a) {
   constexpr int PER = Chunk<T>::PER, VALUES = Chunk<T>::VALUES, THREADS = 64 * WAVES;
   const int wave = uniform((int)threadIdx.x >> 6), lane = lane_id();
   const uint32_t row = a.parts.quotient(blockIdx.x), part = blockIdx.x - row * a.parts.by;
@@ -322,25 +329,25 @@ __global__ __launch_bounds__(64 * WAVES, 6) void logprobs_kernel(LogArgs a) {
       // the first chunk, much that passes the bound or much written down since: a better one, of all that has been seen
       float own = -INFINITY;
       if (chunk == begin || held.count >= enough || __builtin_popcountll(__ballot(top > held.bound && top >= least)) > 24) {
-        own = a.top == 1 ? m : bound_of(maxima, a.top);
+        own = a.top == 1 ? m : bound_of(maxima, m, a.top);
         least = fmaxf(least, own);
         enough = held.count + max(a.top, 16);
       }
-      uint32_t pieces = 0;
+      const float from = fmaxf(fmaxf(least, held.bound), -FLT_MAX);  // never -inf
+      uint32_t pieces = 0;  // of the lane; it takes one after the other, all lanes at once
 #pragma unroll
-      for (int u = 0; u < kPieces; u++) pieces |= __ballot(most[u] >= held.bound && most[u] >= least) ? 1u << u : 0u;
+      for (int u = 0; u < kPieces; u++) pieces |= most[u] >= from ? 1u << u : 0u;
 #pragma unroll 1
-      for (; pieces; pieces &= pieces - 1) {
-        const int u = __builtin_ctz(pieces);
+      for (; __ballot(pieces != 0); pieces &= pieces - 1) {
+        const int u = __builtin_ctz(pieces | 1u << kPieces);
         Chunk<T> piece;  // that one in place 0
         piece.raw[0] = now.raw[0];
 #pragma unroll
         for (int i = 1; i < kPieces; i++) piece.raw[0] = u == i ? now.raw[i] : piece.raw[0];
-        const float from = fmaxf(fmaxf(least, held.bound), -FLT_MAX);  // never -inf
         uint32_t some = 0;
 #pragma unroll
         for (int j = 0; j < PER; j++) some |= (float)piece.value(0, j) >= from ? 1u << j : 0u;
-        held.add(some, a.top, least, [&](int j) {
+        held.add(pieces ? some : 0, a.top, least, [&](int j) {
           T v = piece.value(0, 0);
 #pragma unroll
           for (int i = 1; i < PER; i++) v = j == i ? piece.value(0, i) : v;
@@ -438,13 +445,13 @@ __global__ __launch_bounds__(64 * WAVES, 6) void logprobs_kernel(LogArgs a) {
       if (lane == 0) row_stats = mine;
     }
     if (a.top > 0) {
-      if (n > 256) __syncthreads();
+      if (n > 64) __syncthreads();
 #pragma unroll
       for (int k = 0; k < kMaxRowParts * AMS_LOGPROBS_MAX_TOP / THREADS; k++) {
         const int i = k * THREADS + (int)threadIdx.x;
-        if (n > 256 && i < n && (i + 1) % a.top == 0 && theirs_best[k]) atomicMax((unsigned long long*)&least_entry, (unsigned long long)theirs_best[k]);
+        if (n > 64 && i < n && (i + 1) % a.top == 0 && theirs_best[k]) atomicMax((unsigned long long*)&least_entry, (unsigned long long)theirs_best[k]);
       }
-      if (n > 256) {
+      if (n > 64) {
         __syncthreads();
         bound = least_entry;
       }
