@@ -243,6 +243,8 @@ bool load_stream();
 bool load_tile();
 bool load_scored_stream();
 bool load_scored_tile();
+bool load_prefix_stream();
+bool load_prefix_tile();
 bool load_rope();
 bool load_logprobs();
 

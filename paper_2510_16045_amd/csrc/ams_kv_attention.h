@@ -56,37 +56,61 @@ struct AttentionArgs {
   int causal, window, vec;
 };
 
-// Scores other than softmax_scale q . k: capped, biased by distance, or with keys at the sequence's beginning that every row sees.  Kernels
-// for them are instances of their own, so that the others keep their registers and instructions.
+// Scores other than softmax_scale q . k: capped or biased by distance; and besides, keys at the sequence's beginning that every row sees.
+// Kernels for them are instances of their own, so that the others keep their registers and instructions.
 struct ScoredArgs : AttentionArgs {
-  const float* slopes;       // [heads], or null
-  const int32_t* prefixes;   // [batch], or null
-  float cap2, to_cap;        // cap log2(e), 0 without one; 2 log2(e) softmax_scale / cap
+  const float* slopes;  // [heads], or null
+  float cap2, to_cap;   // cap log2(e), 0 without one; 2 log2(e) softmax_scale / cap
+};
+struct PrefixArgs : ScoredArgs {
+  const int32_t* prefixes;  // [batch]
 };
 template <typename Args>
-constexpr bool kScored = __is_same(Args, ScoredArgs);
+constexpr bool kScored = std::is_base_of_v<ScoredArgs, Args>;
+template <typename Args>
+constexpr bool kPrefix = std::is_same_v<Args, PrefixArgs>;
 
 // Keys from the first on that every row with a position sees.
-__device__ __forceinline__ int prefix_of(const ScoredArgs& a, int b, int len) { return a.prefixes ? min(max(a.prefixes[b], 0), len) : 0; }
+__device__ __forceinline__ int prefix_of(const PrefixArgs& a, int b, int len) { return min(max(a.prefixes[b], 0), len); }
 
-// The score, in log2, of a row's product with a key.  cap tanh(x / cap) = cap - 2 cap / (exp(2 x / cap) + 1): off by 2^-23 of the cap, which is
-// less than the rounding of a weight to fp16 (2^-11) by far, and right at both ends, where the exponential is 0 or infinite.
-__device__ __forceinline__ float capped(const ScoredArgs& a, float x) {
-  const float e = __builtin_amdgcn_exp2f(x * a.to_cap);
-  return __builtin_fmaf(-2.0f * a.cap2, __builtin_amdgcn_rcpf(e + 1.0f), a.cap2);
+// Scores of N products s of a lane's row with keys, in place, in units of 1 / unit_of (log2): the i-th key lies `first` + key(i) from the
+// row; `behind`: none of them behind the row's position.
+//   cap tanh(x / cap) = cap - 2 cap / (exp(2 x / cap) + 1): off by 2^-22 of the cap, less by far than the rounding of a weight to fp16
+//   (2^-11), and right at both ends, where the exponential is 0 or infinite.  The first term, which all scores have, is left out: weights do
+//   not change with it, and log-sum-exps get it at the end (left_out).
+__device__ __forceinline__ float scale_of(const ScoredArgs& a) { return a.cap2 > 0 ? 2 * a.cap2 : a.scale2; }
+__device__ __forceinline__ float unit_of(const ScoredArgs& a) { return a.slopes ? 1.0f : scale_of(a); }
+__device__ __forceinline__ float unit_of(const AttentionArgs& a) { return a.scale2; }
+template <int N, typename Key>
+__device__ __forceinline__ void score(const ScoredArgs& a, float (&s)[N], float slope, float first, bool behind, Key key) {
+  if (a.cap2 > 0) {
+#pragma unroll
+    for (int i = 0; i < N; i++) s[i] = __builtin_amdgcn_rcpf(-1.0f - __builtin_amdgcn_exp2f(s[i] * a.to_cap));
+  }
+  if (!a.slopes) return;
+  const float scale = scale_of(a);
+  if (behind) {
+    const float base = slope * first;
+#pragma unroll
+    for (int i = 0; i < N; i++) s[i] = __builtin_fmaf(s[i], scale, __builtin_fmaf(slope, (float)key(i), base));
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; i++) s[i] = __builtin_fmaf(s[i], scale, -slope * fabsf(first + (float)key(i)));
+  }
 }
+__device__ __forceinline__ float left_out(const ScoredArgs& a) { return a.cap2; }
 
 // What one sequence contributes: rows, row tiles and steps of keys.
 struct Extent {
   int start, n, len, lo, row_tiles, steps;  // lo: first key (a multiple of kStep) that any row may see
 };
-struct ScoredExtent : Extent {
+struct PrefixExtent : Extent {
   int prefix;  // keys that every row sees; lo is the first of the others
   // Steps of the prefix that lie before lo: a sequence's steps are these, and those from lo on.
   __device__ __forceinline__ int prefix_steps() const { return min((prefix + kStep - 1) / kStep, lo / kStep); }
 };
 template <typename Args>
-using ExtentOf = std::conditional_t<kScored<Args>, ScoredExtent, Extent>;
+using ExtentOf = std::conditional_t<kPrefix<Args>, PrefixExtent, Extent>;
 template <int ROWS, typename Args>
 __device__ __forceinline__ ExtentOf<Args> extent_of(const Args& a, int b) {
   ExtentOf<Args> e = {};
@@ -98,7 +122,7 @@ __device__ __forceinline__ ExtentOf<Args> extent_of(const Args& a, int b) {
   e.lo = a.window > 0 ? max(first + 1 - a.window, 0) & ~(kStep - 1) : 0;
   e.row_tiles = (int)(((uint32_t)e.n * (uint32_t)a.group + ROWS - 1) / ROWS);
   e.steps = (e.len - e.lo + kStep - 1) / kStep;
-  if constexpr (kScored<Args>) e.prefix = prefix_of(a, b, e.len), e.steps += e.prefix_steps();
+  if constexpr (kPrefix<Args>) e.prefix = prefix_of(a, b, e.len), e.steps += e.prefix_steps();
   e.steps = max(e.steps, 1);  // one also where there is no key: somebody has to say so
   return e;
 }
@@ -210,7 +234,7 @@ __device__ __forceinline__ bool place_of(const Args& a, ExtentOf<Args> e, const 
       out->row_tile = (at - first) / out->cost;
       out->first = first + out->row_tile * out->cost;
       (Extent&)out->e = {of_lane(e.start, lane), of_lane(e.n, lane), of_lane(e.len, lane), of_lane(e.lo, lane), of_lane(e.row_tiles, lane), of_lane(e.steps, lane)};
-      if constexpr (kScored<Args>) out->e.prefix = of_lane(e.prefix, lane);
+      if constexpr (kPrefix<Args>) out->e.prefix = of_lane(e.prefix, lane);
       return true;
     }
     before = of_lane(end, 63);
@@ -249,8 +273,10 @@ __device__ __forceinline__ void store_out(const AttentionArgs& a, int start, int
     for (int j = 0; j < 4; j++) dst[j] = y[j];
   }
 }
-__device__ __forceinline__ void store_lse(const AttentionArgs& a, int start, int head, int r, float top, float sum) {
+template <typename Args>
+__device__ __forceinline__ void store_lse(const Args& a, int start, int head, int r, float top, float sum) {
   if (!a.lse) return;
+  if constexpr (kScored<Args>) top += left_out(a);
   const int token = (int)a.by_group.quotient((uint32_t)r);
   a.lse[(int64_t)(start + token) * a.lse_stride + head * a.group + r - token * a.group] = sum > 0 || sum != sum ? (top - kLift + __log2f(sum)) * 0.69314718056f : -INFINITY;
 }
@@ -259,8 +285,8 @@ __device__ __forceinline__ void store_lse(const AttentionArgs& a, int start, int
 // as there are (a power of two), U rows each at once, and the others share the parts of a row, P of them at once: U P parts of rows are
 // asked for before the first is used.  The parts are those of every APARTth share from `from` on; the sum becomes the tile's result, or
 // takes the place of the first of them.
-template <int D, int THREADS, int U, int P, int APART = 1, bool RESULT = true>
-__device__ __forceinline__ void join_parts(const AttentionArgs& a, const Pending& tile, __amdgpu_buffer_rsrc_t left, int head, float* lds, int from, int count) {
+template <int D, int THREADS, int U, int P, int APART = 1, bool RESULT = true, typename Args>
+__device__ __forceinline__ void join_parts(const Args& a, const Pending& tile, __amdgpu_buffer_rsrc_t left, int head, float* lds, int from, int count) {
   constexpr int LANES = D / 4, GROUPS = THREADS / LANES;
   f4* const xs = (f4*)lds;                // [group][lane]
   f2* const stats = (f2*)(xs + THREADS);  // [group]
@@ -330,8 +356,8 @@ __device__ __forceinline__ void join_parts(const AttentionArgs& a, const Pending
 // times, the last of every kNear shares adds up theirs, and the last of those workgroups the sums: 64 rows of one sequence of 131071
 // and one kv head 137 -> 52 us, with 8 kv heads 116 -> 84.  Where that rule says one, two would cost a second count: 16 sequences of
 // 3001 with 40 rows 33 -> 40, one of 131071 with 4 rows 36 -> 38.
-template <int D, int THREADS, int U, int P>
-__device__ __forceinline__ void join_pending(const AttentionArgs& a, int pending, const Pending& first, const Pending& last, __amdgpu_buffer_rsrc_t left, int share, int head, float* lds, bool* all_there) {
+template <int D, int THREADS, int U, int P, typename Args>
+__device__ __forceinline__ void join_pending(const Args& a, int pending, const Pending& first, const Pending& last, __amdgpu_buffer_rsrc_t left, int share, int head, float* lds, bool* all_there) {
   if (pending == 0) return;
   auto in_two = [](const Pending& tile) { return tile.rows * tile.count > kTrips * (THREADS / (D / 4)) * U * P; };
   auto count_in = [&](uint32_t* counts, int at, int of) {  // whether this workgroup is the last
@@ -390,6 +416,10 @@ template <>
 void launch_tile<AttentionArgs>(const AttentionArgs&, int, int, int, unsigned, hipStream_t);
 template <>
 void launch_tile<ScoredArgs>(const ScoredArgs&, int, int, int, unsigned, hipStream_t);
+template <>
+void launch_stream<PrefixArgs>(const PrefixArgs&, int, int, int, int, unsigned, hipStream_t);
+template <>
+void launch_tile<PrefixArgs>(const PrefixArgs&, int, int, int, unsigned, hipStream_t);
 
 }  // namespace ams_kv
 #endif

@@ -15,7 +15,7 @@
 // 16 sequences of 3001 tokens, 64 and 8 heads, tiles of 40 rows: 57 MB in 27 us; 560 instructions a step, 11 us of them.
 #include "ams_kv_attention.h"
 
-#ifndef AMS_KV_SCORED  // 1: the kernels for capped, biased and prefix scores
+#ifndef AMS_KV_SCORED  // 1: the kernels for capped and biased scores, 2: with prefixes, too
 #define AMS_KV_SCORED 0
 #endif
 
@@ -28,7 +28,7 @@ struct Steps {
   __device__ __forceinline__ int at(int i) const { return i; }
 };
 template <>
-struct Steps<ScoredArgs> {
+struct Steps<PrefixArgs> {
   int first, before, next;
   __device__ __forceinline__ int at(int i) const { return i < before ? first + i : next + i - before; }
 };
@@ -89,7 +89,7 @@ struct StepV {
 // that do see one get the NaN here.  So do runs whose scale is none that ams_kv_write stores (bits above kTopScale): they lie where no row has been
 // written, where a pool may hold anything, and a value that is no fp16 value any more would turn the 0 of a key that is not seen into a
 // NaN as well.  stage: the scales of the step's two tiles; begin, end: the keys that a lane's row sees, beside those below `below`.
-template <int RUNS, int G, int QT, int DT, bool SCORED>
+template <int RUNS, int G, int QT, int DT, bool PREFIX>
 __device__ __forceinline__ void nan_of_seen_keys(uint8_t* stage, int lane, int first_key, const int (&begin)[QT], const int (&end)[QT], const int (&below)[QT], f4 (&o)[DT][QT]) {
   const int g = lane >> 4;
   uint32_t bad[RUNS], any = 0;  // of the step's 32 keys those whose run stands for NaN; first a lane's eight
@@ -117,7 +117,7 @@ __device__ __forceinline__ void nan_of_seen_keys(uint8_t* stage, int lane, int f
     for (int t = 0; t < QT; t++) {
       const int from = min(max(begin[t] - first_key, 0), 32), to = min(max(end[t] - first_key, 0), 32);
       uint32_t seen = (uint32_t)((1ull << to) - 1) & ~(uint32_t)((1ull << from) - 1);
-      if constexpr (SCORED) seen |= (uint32_t)((1ull << min(max(below[t] - first_key, 0), 32)) - 1);
+      if constexpr (PREFIX) seen |= (uint32_t)((1ull << min(max(below[t] - first_key, 0), 32)) - 1);
       if (bad[run] & seen) {
 #pragma unroll
         for (int d = run * G / 16; d < (run + 1) * G / 16; d++) o[d][t] = f4{NAN, NAN, NAN, NAN};
@@ -129,7 +129,7 @@ __device__ __forceinline__ void nan_of_seen_keys(uint8_t* stage, int lane, int f
 
 template <int D, int G, int QT, int WAVES, typename Args>
 __global__ __launch_bounds__(64 * WAVES, stream_groups(D, QT, WAVES) * WAVES / 4) void stream_kernel(Args a) {
-  constexpr bool SCORED = kScored<Args>;
+  constexpr bool SCORED = kScored<Args>, PREFIX = kPrefix<Args>;
   constexpr int ROWS = 16 * QT, RUNS = D / G, DT = D / 16, KB = D / 32, AT_ONCE = DT < 8 ? DT : 8;
   const int wave = uniform((int)threadIdx.x >> 6), lane = lane_id();
   const int share = (int)a.v.heads.quotient(blockIdx.x), head = blockIdx.x - share * a.v.kv_heads;
@@ -173,7 +173,7 @@ __global__ __launch_bounds__(64 * WAVES, stream_groups(D, QT, WAVES) * WAVES / 4
     const int p_first = e.len - e.n + (int)a.by_group.quotient((uint32_t)row0), p_last = e.len - e.n + (int)a.by_group.quotient((uint32_t)last_row);
     int from, to;
     Steps<Args> steps;
-    if constexpr (SCORED) {
+    if constexpr (PREFIX) {
       // of the share: steps with keys of the prefix, and those behind them that some row of the tile sees
       const int pre = e.prefix_steps(), prefix_end = (e.prefix + kStep - 1) / kStep;
       steps.first = uniform(begin_step), steps.before = uniform(max(min(end_step, prefix_end) - begin_step, 0));
@@ -186,7 +186,7 @@ __global__ __launch_bounds__(64 * WAVES, stream_groups(D, QT, WAVES) * WAVES / 4
     }
     const int whole_begin = uniform(key_begin(a, p_last)), whole_end = uniform(key_end(a, e.len, p_first));
     int prefix = 0;  // keys that every row with a position sees
-    if constexpr (SCORED) prefix = e.prefix;
+    if constexpr (PREFIX) prefix = e.prefix;
     const int whole_prefix = p_first >= 0 ? prefix : 0;
     Pages pages;
     auto look_up = [&](int i) { pages.look_up(a, place.b, steps.at(i), i < to); };
@@ -230,36 +230,28 @@ __global__ __launch_bounds__(64 * WAVES, stream_groups(D, QT, WAVES) * WAVES / 4
         }
       }
     };
-    // Of scored calls S is the score in log2 already.
-    const float unit = SCORED ? 1.0f : a.scale2;
-    float slope[QT], place_of_row[QT];  // of a lane's row: its slope (log2), and its position less the lane's first key of a step from key 0 on
+    const float unit = unit_of(a);  // of S, in log2
+    float slope[QT];  // of a lane's row, in log2
+    int of_row[QT];   // the row's position less what the lane's first key lies from that of the step
     if constexpr (SCORED) {
       const int mine = hidden(lane);
 #pragma unroll
       for (int t = 0; t < QT; t++) {
         const int r = min(row0 + 16 * t + (mine & 15), rows - 1), token = (int)a.by_group.quotient((uint32_t)r);
         slope[t] = a.slopes ? a.slopes[head * a.group + r - token * a.group] * 1.44269504089f : 0.0f;
-        place_of_row[t] = (float)(e.len - e.n + token - 4 * (mine >> 4));
+        of_row[t] = e.len - e.n + token - 4 * (mine >> 4);
       }
     }
-    auto score = [&](f4(&s)[2][QT], int step) {
+    auto scored = [&](f4(&s)[2][QT], int step) {
       if constexpr (SCORED) {
-        if (a.cap2 > 0) {
 #pragma unroll
-          for (int t = 0; t < QT; t++)
+        for (int t = 0; t < QT; t++) {
+          float x[8];
 #pragma unroll
-            for (int i = 0; i < 8; i++) s[i / 4][t][i % 4] = capped(a, s[i / 4][t][i % 4]);
-        } else {
+          for (int i = 0; i < 8; i++) x[i] = s[i / 4][t][i % 4];
+          score(a, x, slope[t], (float)(step * kStep - of_row[t]), (step + 1) * kStep <= p_first + 1, [](int i) { return 16 * (i / 4) + i % 4; });
 #pragma unroll
-          for (int t = 0; t < QT; t++) s[0][t] *= a.scale2, s[1][t] *= a.scale2;
-        }
-        if (a.slopes) {
-#pragma unroll
-          for (int t = 0; t < QT; t++) {
-            const float ahead = place_of_row[t] - (float)(step * kStep);
-#pragma unroll
-            for (int i = 0; i < 8; i++) s[i / 4][t][i % 4] = __builtin_fmaf(-slope[t], fabsf(ahead - (float)(16 * (i / 4) + i % 4)), s[i / 4][t][i % 4]);
-          }
+          for (int i = 0; i < 8; i++) s[i / 4][t][i % 4] = x[i];
         }
       }
     };
@@ -339,10 +331,10 @@ __global__ __launch_bounds__(64 * WAVES, stream_groups(D, QT, WAVES) * WAVES / 4
         f4 s[2][QT];
         h8 p[QT];
         scores(k, s);
-        score(s, step);
+        scored(s, step);
         const bool held[2] = {of_lane(pages.number[0], at) >= 0, of_lane(pages.number[1], at) >= 0};
         const auto inside = [&] { return step * kStep >= whole_begin && (step + 1) * kStep <= whole_end; };
-        const bool whole = (SCORED ? inside() || (step + 1) * kStep <= whole_prefix : inside()) && held[0] && held[1];  // every row sees every key
+        const bool whole = (PREFIX ? inside() || (step + 1) * kStep <= whole_prefix : inside()) && held[0] && held[1];  // every row sees every key
         const bool more = turn + WAVES < to;
         if (more && ++at == 64) {
           at = 0;
@@ -359,17 +351,17 @@ __global__ __launch_bounds__(64 * WAVES, stream_groups(D, QT, WAVES) * WAVES / 4
             const int r = row0 + 16 * t + (mine & 15), position = e.len - e.n + (int)a.by_group.quotient((uint32_t)r);
             begin[t] = r < rows ? key_begin(a, position) : 0;
             end[t] = r < rows ? key_end(a, e.len, position) : 0;
-            below[t] = SCORED && r < rows && position >= 0 ? prefix : 0;
+            below[t] = PREFIX && r < rows && position >= 0 ? prefix : 0;
 #pragma unroll
             for (int u = 0; u < 2; u++)
 #pragma unroll
               for (int i = 0; i < 4; i++)
-                if (((key + 16 * u + i < begin[t] || key + 16 * u + i >= end[t]) && (!SCORED || key + 16 * u + i >= below[t])) || !held[u]) s[u][t][i] = -INFINITY;
+                if (((key + 16 * u + i < begin[t] || key + 16 * u + i >= end[t]) && (!PREFIX || key + 16 * u + i >= below[t])) || !held[u]) s[u][t][i] = -INFINITY;
           }
         }
         weights(s, p);
         put_scales(v);
-        if (!whole) nan_of_seen_keys<RUNS, G, QT, DT, SCORED>(stage, hidden(lane), step * kStep, begin, end, below, o);
+        if (!whole) nan_of_seen_keys<RUNS, G, QT, DT, PREFIX>(stage, hidden(lane), step * kStep, begin, end, below, o);
         multiply(v, p, [&](int u, int run) { return *(const u2*)(stage + ((u * 4 + (lane >> 4)) * RUNS + run) * 8); });
         v.load(a, t0, 0, lane), v.load(a, t1, 1, lane);
         if (!more) break;
@@ -437,7 +429,10 @@ __global__ __launch_bounds__(64 * WAVES, stream_groups(D, QT, WAVES) * WAVES / 4
   join_pending<D, 64 * WAVES, QT == 1 ? 1 : 4, QT == 1 ? 8 : 4>(a, pending, left_first, left_last, left, share, head, (float*)shared, all_there);
 }
 
-#if AMS_KV_SCORED
+#if AMS_KV_SCORED == 2
+using Args = PrefixArgs;
+bool load_prefix_stream() { return loaded((const void*)stream_kernel<64, 32, 1, 4, Args>); }
+#elif AMS_KV_SCORED == 1
 using Args = ScoredArgs;
 bool load_scored_stream() { return loaded((const void*)stream_kernel<64, 32, 1, 4, Args>); }
 #else

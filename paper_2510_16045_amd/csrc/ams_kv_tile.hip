@@ -12,7 +12,7 @@
 // tiles were joined through the workspace at 340 us.  With a window of 512, seven sequences of up to 1999 tokens, 16 heads of 64: 41 us.
 #include "ams_kv_attention.h"
 
-#ifndef AMS_KV_SCORED  // 1: the kernels for capped, biased and prefix scores
+#ifndef AMS_KV_SCORED  // 1: the kernels for capped and biased scores, 2: with prefixes, too
 #define AMS_KV_SCORED 0
 #endif
 
@@ -122,7 +122,8 @@ struct Job {
 
 template <int D, int G, int WAVES, typename Args>
 __global__ __launch_bounds__(64 * WAVES, tile_waves(D, WAVES)) void tile_kernel(Args a) {
-  constexpr bool SCORED = kScored<Args>;
+  constexpr bool SCORED = kScored<Args>, PREFIX = kPrefix<Args>;
+  constexpr int kScores = D == 64 && WAVES == 4 ? 16 : 32;  // that are worked out at once
   constexpr int ROWS = 32 * WAVES, RUNS = D / G, KF = D / 16, DT = D / 32, JOBS = 2 * kBlockTiles / WAVES, AHEAD = ahead(D, WAVES);
   const int wave = uniform((int)threadIdx.x >> 6), lane = lane_id(), h = lane >> 5, col = lane & 31;
   const int share = (int)a.v.heads.quotient(blockIdx.x), head = blockIdx.x - share * a.v.kv_heads;
@@ -142,14 +143,14 @@ __global__ __launch_bounds__(64 * WAVES, tile_waves(D, WAVES)) void tile_kernel(
     int n_blocks = max((key_to - key_from + kBlock - 1) / kBlock, 0);
     // A prefix that all rows see: its blocks come first, where there are keys between it and the others that no row sees.
     int prefix = 0, prefix_blocks = 0, keys_end = key_to;
-    if constexpr (SCORED) {
+    if constexpr (PREFIX) {
       prefix = uniform(position(min(tile_row + ROWS, rows) - 1) < 0 ? 0 : e.prefix), prefix_blocks = (prefix + kBlock - 1) / kBlock;
       keys_end = max(key_to, prefix);
       if (prefix > 0 && key_from <= prefix_blocks * kBlock) prefix_blocks = key_from = 0;
       n_blocks = prefix_blocks + max((keys_end - key_from + kBlock - 1) / kBlock, 0);
     }
     auto first_key = [&](int block) {
-      if constexpr (SCORED) return block < prefix_blocks ? block * kBlock : key_from + (block - prefix_blocks) * kBlock;
+      if constexpr (PREFIX) return block < prefix_blocks ? block * kBlock : key_from + (block - prefix_blocks) * kBlock;
       return key_from + block * kBlock;
     };
     // of those the ones that every row and that no row of the wavefront sees
@@ -160,14 +161,14 @@ __global__ __launch_bounds__(64 * WAVES, tile_waves(D, WAVES)) void tile_kernel(
     const int r = row0 + col;
     const int row_begin = key_begin(a, position(r)), row_end = r < rows ? min(key_end(a, e.len, position(r)), key_to) : 0;
     // The prefix as the row sees it, as some and as every row of the wavefront does.
-    const int row_prefix = r < rows && position(r) >= 0 ? prefix : 0, some_prefix = uniform(idle || p_last < 0 ? 0 : prefix), whole_prefix = uniform(p_first >= 0 ? prefix : 0);
-    // Of scored calls S is the score in log2 already.
-    const float unit = SCORED ? 1.0f : a.scale2;
-    float slope = 0, place_of_row = 0;  // of the lane's row: its slope (log2), and its position less the lane's first key of a block from key 0 on
+    const int some_prefix = uniform(idle || p_last < 0 ? 0 : prefix), whole_prefix = uniform(p_first >= 0 ? prefix : 0);
+    const float unit = unit_of(a);  // of S, in log2
+    float slope = 0;  // of the lane's row, in log2
+    int of_row = 0;   // the row's position less what the lane's first key lies from that of the block
     if constexpr (SCORED) {
       const int mine = min(r, rows - 1), token = (int)a.by_group.quotient((uint32_t)mine);
       if (a.slopes) slope = a.slopes[head * a.group + mine - token * a.group] * 1.44269504089f;
-      place_of_row = (float)(e.len - e.n + token - 4 * h);
+      of_row = position(r) - 4 * h;
     }
 
     h8 q[KF];
@@ -193,7 +194,7 @@ __global__ __launch_bounds__(64 * WAVES, tile_waves(D, WAVES)) void tile_kernel(
     const int my_tile = wave % kBlockTiles;
     int number = -1;  // the page of that tile in 64 blocks, one to a lane
     auto look_up = [&](int block) {
-      const int tile = SCORED ? first_key(block + hidden(lane)) / kTile + my_tile : key_from / kTile + (block + hidden(lane)) * kBlockTiles + my_tile;
+      const int tile = PREFIX ? first_key(block + hidden(lane)) / kTile + my_tile : key_from / kTile + (block + hidden(lane)) * kBlockTiles + my_tile;
       const uint32_t page = a.v.page_tiles.quotient((uint32_t)tile);
       number = -1;
       if (tile * kTile < keys_end && page < (uint32_t)a.v.table_width) {
@@ -206,7 +207,7 @@ __global__ __launch_bounds__(64 * WAVES, tile_waves(D, WAVES)) void tile_kernel(
       if (block % 64 == 0) look_up(block);
 #pragma unroll
       for (int j = 0; j < JOBS; j++)
-        jobs[j].load(a, of_lane(number, block % 64), head, SCORED ? first_key(block) / kTile + my_tile : key_from / kTile + block * kBlockTiles + my_tile, JOBS == 1 ? wave >= kBlockTiles : j == 1, lane);
+        jobs[j].load(a, of_lane(number, block % 64), head, PREFIX ? first_key(block) / kTile + my_tile : key_from / kTile + block * kBlockTiles + my_tile, JOBS == 1 ? wave >= kBlockTiles : j == 1, lane);
     };
     auto restore = [&](int buffer) {
 #pragma unroll
@@ -244,26 +245,32 @@ __global__ __launch_bounds__(64 * WAVES, tile_waves(D, WAVES)) void tile_kernel(
       for (int n = 0; n < AHEAD; n++) f[n] = block.v[n % DT][n / DT][lane];
       const uint32_t anything = (uint32_t)uniform((int)(what[0] | what[1] | what[2] | what[3]));
       if constexpr (SCORED) {
-        if (a.cap2 > 0) {
 #pragma unroll
-          for (int i = 0; i < 32; i++) s[i / 16][i % 16] = capped(a, s[i / 16][i % 16]);
-        } else {
-          s[0] *= a.scale2, s[1] *= a.scale2;
-        }
-        if (a.slopes) {
-          const float ahead = place_of_row - (float)key0;
+        for (int i0 = 0; i0 < 32; i0 += kScores) {
+          float x[kScores];
 #pragma unroll
-          for (int i = 0; i < 32; i++) s[i / 16][i % 16] = __builtin_fmaf(-slope, fabsf(ahead - (float)(32 * (i / 16) + 8 * (i % 16 / 4) + i % 4)), s[i / 16][i % 16]);
+          for (int i = 0; i < kScores; i++) x[i] = s[(i0 + i) / 16][(i0 + i) % 16];
+          score(a, x, slope, (float)(key0 - of_row), key0 + kBlock <= p_first + 1, [&](int i) { return 32 * ((i0 + i) / 16) + 8 * ((i0 + i) % 16 / 4) + i % 4; });
+#pragma unroll
+          for (int i = 0; i < kScores; i++) s[(i0 + i) / 16][(i0 + i) % 16] = x[i];
         }
       }
+      // The keys that the lane's row sees; of scored calls from its position each time, which keeps three registers free.
+      int row_from = row_begin, row_to = row_end, row_prefix = 0;
+      auto limits = [&] {
+        const int at = hidden(of_row) + 4 * h;
+        const bool is_row = row0 + col < rows;
+        row_from = key_begin(a, at), row_to = is_row ? min(key_end(a, e.len, at), key_to) : 0, row_prefix = is_row && at >= 0 ? prefix : 0;
+      };
       const bool outside = key0 < whole_begin || key0 + kBlock > whole_end;
-      if ((SCORED ? outside && key0 + kBlock > whole_prefix : outside) || (anything & kMissing)) {  // some row does not see some key
+      if ((PREFIX ? outside && key0 + kBlock > whole_prefix : outside) || (anything & kMissing)) {  // some row does not see some key
+        if constexpr (SCORED) limits();
 #pragma unroll
         for (int kt = 0; kt < 2; kt++)
 #pragma unroll
           for (int i = 0; i < 16; i++) {
             const int key = key0 + 32 * kt + 8 * (i / 4) + 4 * h + i % 4;
-            if (((key < row_begin || key >= row_end) && (!SCORED || key >= row_prefix)) || (what[2 * kt + i / 8] & kMissing)) s[kt][i] = -INFINITY;
+            if (((key < row_from || key >= row_to) && (!PREFIX || key >= row_prefix)) || (what[2 * kt + i / 8] & kMissing)) s[kt][i] = -INFINITY;
           }
       }
       float top = s[0][0];
@@ -307,13 +314,14 @@ __global__ __launch_bounds__(64 * WAVES, tile_waves(D, WAVES)) void tile_kernel(
         if (n + AHEAD < NV) __builtin_amdgcn_sched_group_barrier(kReads, 1, 1);
       }
       if (anything & kBad) {
+        if constexpr (SCORED) limits();
 #pragma unroll
         for (int run = 0; run < RUNS; run++) {
           bool seen = false;
           for (int t = 0; t < kBlockTiles; t++) {
-            const int first = key0 + kTile * t, from = min(max(row_begin - first, 0), kTile), to = min(max(row_end - first, 0), kTile);
+            const int first = key0 + kTile * t, from = min(max(row_from - first, 0), kTile), to = min(max(row_to - first, 0), kTile);
             if (what[t] & kBad) seen |= (notes[buffer].bad[t][run] & ((1u << to) - 1) & ~((1u << from) - 1)) != 0;
-            if constexpr (SCORED)
+            if constexpr (PREFIX)
               if (what[t] & kBad) seen |= (notes[buffer].bad[t][run] & ((1u << min(max(row_prefix - first, 0), kTile)) - 1)) != 0;
           }
           if (seen) {
@@ -336,7 +344,7 @@ __global__ __launch_bounds__(64 * WAVES, tile_waves(D, WAVES)) void tile_kernel(
         if (block + 1 < n_blocks) restore((block + 1) & 1);
         if (block + 2 < n_blocks) request(block + 2);
         const int key0 = first_key(block);
-        if ((key0 < some_end && key0 + kBlock > some_begin) || (SCORED && key0 < some_prefix)) compute(block & 1, key0);
+        if ((key0 < some_end && key0 + kBlock > some_begin) || (PREFIX && key0 < some_prefix)) compute(block & 1, key0);
         __syncthreads();
       }
     }
@@ -353,7 +361,10 @@ __global__ __launch_bounds__(64 * WAVES, tile_waves(D, WAVES)) void tile_kernel(
   }
 }
 
-#if AMS_KV_SCORED
+#if AMS_KV_SCORED == 2
+using Args = PrefixArgs;
+bool load_prefix_tile() { return loaded((const void*)tile_kernel<64, 32, 4, Args>); }
+#elif AMS_KV_SCORED == 1
 using Args = ScoredArgs;
 bool load_scored_tile() { return loaded((const void*)tile_kernel<64, 32, 4, Args>); }
 #else

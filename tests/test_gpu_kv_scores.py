@@ -111,7 +111,7 @@ def test_every_kernel_for_few_rows(D, G, columns, waves, split):
     prefix = [[0, 40, 1, 333, 64, 7, 1100][b % 7] for b in range(n)]
     c = Scored(lens, counts, heads=kv_heads, kv_heads=kv_heads, D=D, G=G, page=64, prefix=prefix, **ALL)
     ws = torch.zeros(ams.KV_WORKSPACE_BYTES, dtype=torch.uint8, device="cuda")
-    for c.softcap, c.window in ((c.softcap, 0), (0.0, 200)):
+    for c.softcap, c.window, c.prefix in ((c.softcap, 0, prefix), (0.0, 200, prefix), (c.softcap, 0, None)):
         plan = plan_of(c)
         assert (plan["kernel"], plan["rows"], plan["waves"]) == ("stream", 16 * columns, waves), plan
         c.check(heads=[0, kv_heads - 1], max_q_len=count, workspace=ws)
