@@ -419,7 +419,7 @@ typedef struct ams_rope_rows {
 
 /*
  * ams_rope  rotates rows of Q and, if it is not NULL, of K (heads of the same size) in one launch.  Any strides and any 2-byte alignment;
- * 16-byte aligned rows and multiples of 16 rotated channels (interleaved: 8) are faster.  Positions, lengths and starts are read by the
+ * 16-byte aligned rows, strides of whole 16 bytes and multiples of 16 rotated channels (interleaved: 8) are faster.  Positions, lengths and starts are read by the
  * kernel only: a captured call follows them.  Errors: NULL, SHAPE, ALIGN, DEVICE, LAUNCH.
  */
 int ams_rope(const ams_rotation* rotation, const ams_rope_rows* Q, const ams_rope_rows* K, int64_t rows, int head_dim, void* stream);

@@ -83,11 +83,30 @@ __device__ __forceinline__ void turn_pair(_Float16& a, _Float16& b, float c, flo
   b = (_Float16)(y * c + x * s);
 }
 
-// A wavefront takes heads of one row, `at_once` of them side by side; its lanes keep their angles for all of them.  WIDE: a lane
-// has pieces of eight channels (two where they are halves of pairs); else one pair, or one channel that is copied.
-template <bool WIDE, bool INTERLEAVED>
+// VEC values that lie together.
+template <int VEC>
+struct Piece {
+  typedef _Float16 Values __attribute__((ext_vector_type(VEC)));
+  Values x;
+  // STREAMED: what is read once and written once stays out of the caches.
+  template <bool STREAMED>
+  __device__ __forceinline__ void load(const uint16_t* from) {
+    x = STREAMED ? __builtin_nontemporal_load((const Values*)from) : *(const Values*)from;
+  }
+  template <bool STREAMED>
+  __device__ __forceinline__ void store(uint16_t* to) const {
+    if constexpr (STREAMED)
+      __builtin_nontemporal_store(x, (Values*)to);
+    else
+      *(Values*)to = x;
+  }
+};
+
+// A wavefront takes heads of one row, `at_once` of them side by side; its lanes keep their angles for all of them.  A lane has pieces of
+// VEC channels: two where they are halves of pairs, one of neighbours or of channels that are copied.
+template <int VEC, bool INTERLEAVED, bool STREAMED>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
-  constexpr int PAIRS = !WIDE ? 1 : INTERLEAVED ? 4 : 8;
+  constexpr int PAIRS = INTERLEAVED && VEC > 1 ? VEC / 2 : VEC;
   const int lane = lane_id();
   const uint32_t unit = blockIdx.x * 4 + (uint32_t)__builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const uint32_t row = a.by_parts.quotient(unit), part = unit - row * a.by_parts.by;
@@ -110,44 +129,36 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
       const int h = head < a.heads ? head : head - a.heads;
       const uint16_t* const in = t.in + (int64_t)row * t.in_stride + (int64_t)h * t.in_head;
       uint16_t* const out = t.out + (int64_t)row * t.out_stride + (int64_t)h * t.out_head;
-      if constexpr (WIDE) {
-        if (chunk >= turned) {
-          const int at = 2 * a.pairs + (chunk - turned) * 8;
-          *(u4*)(out + at) = *(const u4*)(in + at);
-        } else if constexpr (INTERLEAVED) {
-          h8 x = *(const h8*)(in + chunk * 8);
+      Piece<VEC> x, y;
+      if (chunk >= turned) {
+        const int at = 2 * a.pairs + (chunk - turned) * VEC;
+        x.template load<STREAMED>(in + at);
+        x.template store<STREAMED>(out + at);
+      } else if constexpr (INTERLEAVED && VEC > 1) {
+        x.template load<STREAMED>(in + chunk * VEC);
 #pragma unroll
-          for (int i = 0; i < 4; i++) {
-            _Float16 p = x[2 * i], q = x[2 * i + 1];
-            turn_pair(p, q, c[i], s[i]);
-            x[2 * i] = p, x[2 * i + 1] = q;
-          }
-          *(h8*)(out + chunk * 8) = x;
-        } else {
-          h8 x = *(const h8*)(in + chunk * 8), y = *(const h8*)(in + a.pairs + chunk * 8);
-#pragma unroll
-          for (int i = 0; i < 8; i++) {
-            _Float16 p = x[i], q = y[i];
-            turn_pair(p, q, c[i], s[i]);
-            x[i] = p, y[i] = q;
-          }
-          *(h8*)(out + chunk * 8) = x, *(h8*)(out + a.pairs + chunk * 8) = y;
+        for (int i = 0; i < PAIRS; i++) {
+          _Float16 p = x.x[2 * i], q = x.x[2 * i + 1];
+          turn_pair(p, q, c[i], s[i]);
+          x.x[2 * i] = p, x.x[2 * i + 1] = q;
         }
+        x.template store<STREAMED>(out + chunk * VEC);
       } else {
-        if (chunk >= turned) {
-          out[a.pairs + chunk] = in[a.pairs + chunk];
-        } else {
-          const int i = INTERLEAVED ? 2 * chunk : chunk, j = INTERLEAVED ? i + 1 : i + a.pairs;
-          _Float16 x = __builtin_bit_cast(_Float16, in[i]), y = __builtin_bit_cast(_Float16, in[j]);
-          turn_pair(x, y, c[0], s[0]);
-          out[i] = __builtin_bit_cast(uint16_t, x), out[j] = __builtin_bit_cast(uint16_t, y);
+        const int i = INTERLEAVED ? 2 * chunk : VEC * chunk, j = INTERLEAVED ? i + 1 : i + a.pairs;
+        x.template load<STREAMED>(in + i), y.template load<STREAMED>(in + j);
+#pragma unroll
+        for (int k = 0; k < VEC; k++) {
+          _Float16 p = x.x[k], q = y.x[k];
+          turn_pair(p, q, c[k], s[k]);
+          x.x[k] = p, y.x[k] = q;
         }
+        x.template store<STREAMED>(out + i), y.template store<STREAMED>(out + j);
       }
     }
   }
 }
 
-bool load_rope() { return loaded((const void*)rope_kernel<true, false>); }
+bool load_rope() { return loaded((const void*)rope_kernel<8, false, false>); }
 
 }  // namespace ams_kv
 
@@ -190,11 +201,13 @@ int ams_rope(const ams_rotation* rotation, const ams_rope_rows* Q, const ams_rop
   if (!(fabsf(r.magnitude) <= FLT_MAX) || (!r.positions && !r.q_starts && rows != r.batch)) return AMS_ERR_SHAPE;
   if (!r.turns || (rows > 0 && (!Q->in || !Q->out || (K && (!K->in || !K->out)))) || (!r.positions && r.batch > 0 && !r.kv_lens)) return AMS_ERR_NULL;
   if (!aligned(r.turns, 8) || !aligned(r.positions, 4) || !aligned(r.kv_lens, 4) || !aligned(r.q_starts, 4)) return AMS_ERR_ALIGN;
-  bool wide = (r.interleaved ? r.rotary_dim : r.rotary_dim / 2) % 8 == 0, in_place = true;
+  bool in_place = true;
+  // what a lane may take at once, in values: as many as divide the pairs (neighbours: the rotated channels), the strides and, in bytes, the addresses
+  uint64_t common = r.interleaved ? r.rotary_dim : r.rotary_dim / 2;
   for (const ams_rope_rows* t : {Q, K}) {
     if (!t) continue;
     if (!aligned(t->in, 2) || !aligned(t->out, 2)) return AMS_ERR_ALIGN;
-    wide = wide && aligned(t->in, 16) && aligned(t->out, 16) && (t->in_stride | t->in_head_stride | t->out_stride | t->out_head_stride) % 8 == 0;
+    common |= (uintptr_t)t->in / 2 | (uintptr_t)t->out / 2 | (uint64_t)(t->in_stride | t->in_head_stride | t->out_stride | t->out_head_stride);
     in_place = in_place && t->in == t->out && t->in_stride == t->out_stride && t->in_head_stride == t->out_head_stride;
   }
   if (const int rc = device_status(); rc != AMS_OK) return rc;
@@ -205,9 +218,13 @@ int ams_rope(const ams_rotation* rotation, const ams_rope_rows* Q, const ams_rop
   a.turns = r.turns, a.positions = r.positions, a.lens = r.kv_lens, a.starts = r.q_starts, a.rows = rows, a.magnitude = r.magnitude;
   a.batch = r.batch, a.heads = Q->heads, a.all_heads = Q->heads + (K ? K->heads : 0);
   a.pairs = r.rotary_dim / 2, a.rest = in_place ? 0 : head_dim - r.rotary_dim;
-  wide = wide && a.rest % 8 == 0;
-  const int pairs = !wide ? 1 : r.interleaved ? 4 : 8;
-  a.chunks = a.pairs / pairs + a.rest / (wide ? 8 : 1);
+  common |= (uint64_t)a.rest;
+  const int vec = common % 8 == 0 ? 8 : common % 4 == 0 ? 4 : common % 2 == 0 ? 2 : 1;
+  a.chunks = a.pairs / (r.interleaved && vec > 1 ? vec / 2 : vec) + a.rest / vec;
+  // Where a wavefront's stores fill whole lines of 128 bytes and the rows are more than the caches hold for whoever reads them next: past the
+  // caches (16384 rows of 72 heads of 128 125 -> 116 us, 3104 of 32 of 256 25.5 -> 23.0; 2048 of 40 of 128 11.3 and 11.5; lines in parts,
+  // 8000 rows of 40 heads of 80, 28 -> 36).
+  const bool streamed = vec == 8 && (r.interleaved ? r.rotary_dim : r.rotary_dim / 2) % 64 == 0 && a.rest % 64 == 0 && rows * (Q->heads + (K ? K->heads : 0)) * head_dim >= (int64_t)16 << 20;
   a.at_once = std::max(64 / a.chunks, 1);
   const int64_t turns = (a.all_heads + a.at_once - 1) / a.at_once;
   constexpr int64_t kWavefronts = 8192;
@@ -217,10 +234,15 @@ int ams_rope(const ams_rotation* rotation, const ams_rope_rows* Q, const ams_rop
   a.interleaved = r.interleaved != 0, a.transposed = r.transposed != 0;
   const unsigned grid = (unsigned)((rows * a.by_parts.by + 3) / 4);
   auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, (hipStream_t)stream, a); };
-  if (wide)
-    r.interleaved ? launch(rope_kernel<true, true>) : launch(rope_kernel<true, false>);
-  else
-    r.interleaved ? launch(rope_kernel<false, true>) : launch(rope_kernel<false, false>);
+  auto of_layout = [&](auto interleaved) {
+    constexpr bool I = decltype(interleaved)::value;
+    if (streamed) return launch(rope_kernel<8, I, true>);
+    if (vec == 8) return launch(rope_kernel<8, I, false>);
+    if (vec == 4) return launch(rope_kernel<4, I, false>);
+    if (vec == 2) return launch(rope_kernel<2, I, false>);
+    launch(rope_kernel<1, I, false>);
+  };
+  r.interleaved ? of_layout(Int<1>()) : of_layout(Int<0>());
   return hipGetLastError() == hipSuccess ? AMS_OK : AMS_ERR_LAUNCH;
 }
 
