@@ -1,8 +1,11 @@
-"""The attention block of a decoder layer on packed weights and a 4-bit KV cache: how the library's calls go together.
+"""The attention block of a decoder layer on packed weights and a 4-bit KV cache, and what comes behind the last layer: how the library's
+calls go together.
 
-    qkv = ams_linear(x);  ams_kv_write(k, v);  ams_kv_attention(q);  ams_linear(o)
+    qkv = ams_linear(x);  ams_rope(q, k);  ams_kv_write(k, v);  ams_kv_attention(q);  ams_linear(o)
+    logits = ams_linear(x);  ams_logprobs(logits, tokens)
 
-q and k are used as the projection gives them: a model with rotary embeddings rotates them between the projection and ams_kv_write.
+q and k are rotated where the model has rotary embeddings, and used as the projection gives them otherwise; scores are capped or biased by
+distance where it was trained so.
 Projections of up to MAX_M rows run on the packed weights; those of prompts restore a matrix to fp16 once and multiply with the
 library GEMM; captured ones of more rows run MAX_M rows at a time.  A decode step of fixed batch is captured as a HIP graph: the sequences' lengths lie on the GPU and grow from replay to
 replay.  ``python -m paper_2510_16045_amd.attention_layer`` runs a prompt and decode steps of a Llama-3-8B-shaped block on
@@ -13,7 +16,7 @@ from __future__ import annotations
 
 import numpy as np
 
-from . import FP425, KV_WORKSPACE_BYTES, MAX_M, ams_dequant, ams_init, ams_kv_attention, ams_kv_cache, ams_kv_write, ams_linear, ams_pack, synth
+from . import FP425, KV_WORKSPACE_BYTES, MAX_M, ams_dequant, ams_init, ams_kv_attention, ams_kv_cache, ams_kv_write, ams_linear, ams_logprobs, ams_pack, ams_rope, ams_rope_frequencies, synth
 
 
 class PackedLinear:
@@ -44,11 +47,30 @@ class PackedLinear:
         return y if out is None else out.copy_(y)
 
 
-class AttentionLayer:
-    """Projections, cache and attention of one layer; sequence b owns the pages block_table[b], int32 [batch, pages]."""
+class Rotary:
+    """A model's rotary embedding: the arguments of ams_rope_frequencies, and whether neighbours are paired."""
 
-    def __init__(self, qkv: np.ndarray, o: np.ndarray, heads: int, kv_heads: int, n_pages: int, block_table, page_size: int = 64, scale_group: int = 32, fmt: int = FP425, workspace=None):
+    def __init__(self, *frequencies, interleaved: bool = False, **more):
         import torch
+
+        turns, self.magnitude = ams_rope_frequencies(*frequencies, **more)
+        self.turns, self.interleaved = torch.from_numpy(turns).cuda(), interleaved
+
+    def __call__(self, q, k, kv_lens, q_starts=None):
+        """Rotates rows of q and k, the last of sequences of kv_lens tokens, where they lie."""
+        ams_rope(q, k, self.turns, kv_lens=kv_lens, q_starts=q_starts, magnitude=self.magnitude, interleaved=self.interleaved, out=(q, k))
+
+
+class AttentionLayer:
+    """Projections, cache and attention of one layer; sequence b owns the pages block_table[b], int32 [batch, pages].
+
+    rotary: a Rotary, or None.  scores: what ams_kv_attention takes of window, softcap, slopes, prefix_lens and softmax_scale."""
+
+    def __init__(self, qkv: np.ndarray, o: np.ndarray, heads: int, kv_heads: int, n_pages: int, block_table, page_size: int = 64, scale_group: int = 32, fmt: int = FP425, workspace=None,
+                 rotary: Rotary = None, **scores):
+        import torch
+
+        self.rotary, self.scores = rotary, scores
 
         self.head_dim = qkv.shape[0] // (heads + 2 * kv_heads)
         self.heads, self.kv_heads, self.page_size, self.scale_group = heads, kv_heads, page_size, scale_group
@@ -64,9 +86,25 @@ class AttentionLayer:
         max_q_len: the most rows of any of them, where the caller knows (drafts are faster with it)."""
         rows = self.qkv(x).view(-1, self.heads + 2 * self.kv_heads, self.head_dim)
         q, k, v = rows[:, : self.heads], rows[:, self.heads : self.heads + self.kv_heads], rows[:, self.heads + self.kv_heads :]
+        if self.rotary is not None:
+            self.rotary(q, k, kv_lens, q_starts)
         ams_kv_write(self.cache, k, v, self.block_table, kv_lens, self.scale_group, q_starts=q_starts)
-        y = ams_kv_attention(q, self.cache, self.block_table, kv_lens, self.scale_group, q_starts=q_starts, max_q_len=max_q_len, workspace=self.workspace)
+        y = ams_kv_attention(q, self.cache, self.block_table, kv_lens, self.scale_group, q_starts=q_starts, max_q_len=max_q_len, workspace=self.workspace, **self.scores)
         return self.o(y.view(-1, self.heads * self.head_dim), out=out)
+
+
+class Vocabulary:
+    """The vocabulary projection and what is reported of its logits."""
+
+    def __init__(self, weights: np.ndarray, fmt: int = FP425, workspace=None):
+        import torch
+
+        self.linear = PackedLinear(weights, fmt)
+        self.workspace = torch.zeros(KV_WORKSPACE_BYTES, dtype=torch.uint8, device="cuda") if workspace is None else workspace
+
+    def __call__(self, x, tokens=None, top: int = 0, temperature: float = 1.0, out=None):
+        """x fp16 [rows, hidden]: LogProbs of tokens, int32 [rows], and of the `top` most likely ones."""
+        return ams_logprobs(self.linear(x), tokens, top=top, temperature=temperature, workspace=self.workspace, out=out)
 
 
 class DecodeStep:
@@ -113,7 +151,8 @@ def main(batch: int = 8, prompt: int = 2000, steps: int = 64, page_size: int = 6
     hidden, heads, kv_heads, dim = 4096, 32, 8, 128  # Llama-3-8B
     pages = -(-(prompt + steps + 1) // page_size)
     table = torch.arange(batch * pages, dtype=torch.int32, device="cuda").view(batch, pages)
-    layer = AttentionLayer(synth.gaussian_weights((heads + 2 * kv_heads) * dim, hidden, 0), synth.gaussian_weights(hidden, heads * dim, 1), heads, kv_heads, batch * pages, table, page_size)
+    layer = AttentionLayer(synth.gaussian_weights((heads + 2 * kv_heads) * dim, hidden, 0), synth.gaussian_weights(hidden, heads * dim, 1), heads, kv_heads, batch * pages, table, page_size,
+                           rotary=Rotary(dim, 500000.0))
     lens = torch.full((batch,), prompt, dtype=torch.int32, device="cuda")
     starts = torch.arange(batch + 1, dtype=torch.int32, device="cuda") * prompt
     layer(torch.randn((batch * prompt, hidden), device="cuda").half(), lens, q_starts=starts, max_q_len=prompt)
