@@ -57,7 +57,8 @@ struct AttentionArgs {
 };
 
 // Scores other than softmax_scale q . k: capped or biased by distance; and besides, keys at the sequence's beginning that every row sees.
-// Kernels for them are instances of their own, so that the others keep their registers and instructions.
+// Kernels for them are instances of their own, so that the others keep their registers and instructions: with one kind for all, capped scores of
+// 32 sequences of up to 8192 took 38.4 us instead of 37.4, of 24 of up to 1000 30.3 instead of 28.6.
 struct ScoredArgs : AttentionArgs {
   const float* slopes;  // [heads], or null
   float cap2, to_cap;   // cap log2(e), 0 without one; 2 log2(e) softmax_scale / cap
@@ -78,6 +79,9 @@ __device__ __forceinline__ int prefix_of(const PrefixArgs& a, int b, int len) { 
 //   cap tanh(x / cap) = cap - 2 cap / (exp(2 x / cap) + 1): off by 2^-22 of the cap, less by far than the rounding of a weight to fp16
 //   (2^-11), and right at both ends, where the exponential is 0 or infinite.  The first term, which all scores have, is left out: weights do
 //   not change with it, and log-sum-exps get it at the end (left_out).
+// Their issue is what they cost: 2048 rows over 8192 keys, 32 and 8 heads of 128 channels: plain 267 us, with a cap 325 (two transcendental
+// operations a score and two others), a bias 304 (two others), both 377; before the first term and a product were left out 341, 319 and 391.
+// One sequence's rows each of 32 sequences of up to 8192: 35, 37.5, 39.6, 42.5.
 __device__ __forceinline__ float scale_of(const ScoredArgs& a) { return a.cap2 > 0 ? 2 * a.cap2 : a.scale2; }
 __device__ __forceinline__ float unit_of(const ScoredArgs& a) { return a.slopes ? 1.0f : scale_of(a); }
 __device__ __forceinline__ float unit_of(const AttentionArgs& a) { return a.scale2; }

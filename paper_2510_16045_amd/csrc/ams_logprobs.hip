@@ -13,6 +13,12 @@
 //
 // A row is shared out to several workgroups where rows do not fill the chip: each leaves its statistics and list in the workspace and
 // counts itself in; the last one joins them, always in the same order, and clears the count.  Nobody waits for anybody.
+//
+// What bounds it.  Many rows: instruction issue beside memory: per value an exponential, four more operations and one for the rank, 2048 rows
+// of 128256 (525 MB) 91 us without tokens, 98 with, 108 with the most likely one, 127 with 20 (4.1 to 5.8 TB/s; a bare read takes 74).  Few rows: trips
+// that follow one another: 1 row 5.7 us, with 5 tokens 10, with 20 13.9; of 32 rows with 20 (15 us) 1 is loading, 1 bisection, 1.5 writing down,
+// 2.5 joining the wavefronts, 1.5 the way to memory and its count, 3 joining the parts.  Instructions that run once cost their way through
+// the instruction cache: the same kernel with 20 KB of code instead of 15 took a third longer wherever a list was asked for.
 #include <float.h>
 #include <limits.h>
 
@@ -227,6 +233,7 @@ struct Held {
   }
 };
 
+// Four wavefronts to a SIMD: six or eight make the compiler spill (2048 rows: 101, 105 and 277 us).
 template <typename T, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 4) void logprobs_kernel(LogArgs a) {
   constexpr int PER = Chunk<T>::PER, VALUES = Chunk<T>::VALUES, THREADS = 64 * WAVES;
@@ -272,7 +279,8 @@ __global__ __launch_bounds__(64 * WAVES, 4) void logprobs_kernel(LogArgs a) {
   Held held = {entries + wave * kHeld, entries + (WAVES + wave) * kHeld};
   // A wavefront's chunks lie WAVES apart: a workgroup's form one window.
   const int begin = (int)part * a.part_turns * WAVES + wave, n_chunks = (a.vocab - 1) / VALUES + 1, end = min((int)(part + 1) * a.part_turns * WAVES, n_chunks);
-  // Nothing is asked for ahead: four workgroups to a compute unit ask for 128 KiB at a time.
+  // Nothing is asked for ahead: sixteen wavefronts of a compute unit ask for 64 KiB at a time, and registers for the next chunk would cost
+  // some of them (2048 rows 124 -> 108 us without).
   for (int chunk = begin; chunk < end; chunk += WAVES) {
     const int first = chunk * VALUES;
     Chunk<T> now;
@@ -490,7 +498,8 @@ __global__ __launch_bounds__(64 * WAVES, 4) void logprobs_kernel(LogArgs a) {
 
 bool load_logprobs() { return loaded((const void*)logprobs_kernel<float, 8>); }
 
-// Workgroups of a row.  Eight wavefronts to a workgroup up to as many as the chip holds, beyond that four.
+// Workgroups of a row.  Eight wavefronts to a workgroup up to as many as the chip holds at once, beyond that four, whose ends others cover (rows
+// of 50001, 8 tokens: 300 rows 27 us with eight, 31 with four; 500 29 and 34; 600 41 and 38; 2048 95 and 77).
 constexpr int64_t kWorkgroups = 512;
 struct LogPlan {
   int waves, parts, part_turns, part_bytes;
