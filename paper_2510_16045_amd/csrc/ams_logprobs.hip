@@ -511,7 +511,9 @@ static LogPlan log_plan(int type, int64_t rows, int64_t vocab, int top, size_t w
   const LogPlan whole = {waves, 1, (int)((chunks + waves - 1) / waves), 0, 0};
   const int64_t turns = (chunks + kPartWaves - 1) / kPartWaves;
   const int64_t parts = std::min<int64_t>(std::min<int64_t>(turns, kMaxRowParts), rows > 0 ? kWorkgroups / rows : 1);
-  if (parts < 2) return whole;
+  // More than half as many rows as compute units: two parts have to be long to pay for their join (256 rows, 20 tokens, whole and in two: of 20000
+  // 13.7 us and 16.8, 50001 19.4 and 22.9, 128256 33.5 and 32.1; 128 rows of 50001 19.0, in four 17.2).
+  if (parts < 2 || (rows > 128 && turns < 4 * parts)) return whole;
   LogPlan p = {kPartWaves, 0, (int)((turns + parts - 1) / parts), (16 + 8 * top + 15) / 16 * 16, 0};
   p.parts = (int)((turns + p.part_turns - 1) / p.part_turns);
   p.workspace = kLogCountBytes + (size_t)(rows * p.parts) * p.part_bytes;
