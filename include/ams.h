@@ -67,7 +67,7 @@ const char* ams_strerror(int code);
 /*
  * Optional one-time set-up for the current device: checks that it is a gfx950 (else
  * AMS_ERR_DEVICE), raises the dynamic-LDS limit of every Linear kernel (they use up to
- * 160 KiB) and loads those of the KV cache.  Every device entry point does the same for itself on its first call, so this
+ * 160 KiB) and loads the others.  Every device entry point does the same for itself on its first call, so this
  * is only REQUIRED before the first call of an entry point happens inside a HIP stream
  * capture (function attributes should not be changed while capturing).  Allocates nothing,
  * enqueues nothing; may be called any number of times, once per device that is used (the first call
@@ -402,7 +402,7 @@ int ams_rope_frequencies(int rotary_dim, double base, int scaling, double factor
 typedef struct ams_rotation {
   const uint64_t* turns;    /* device, [rotary_dim / 2] */
   const int32_t* positions; /* device, [rows], or NULL: the rows are the last ones of their sequences, as those of the KV cache's calls are */
-  const int32_t* kv_lens;   /* device, [batch] (a negative length is taken as 0) */
+  const int32_t* kv_lens;   /* device, [batch]; a negative length is taken as 0, one beyond the cache's room, which is not known here, as it is */
   const int32_t* q_starts;  /* device, [batch + 1], or NULL: one row per sequence (rows = batch).  Rows that no sequence has are left alone */
   int32_t batch;
   int32_t rotary_dim;  /* even, up to head_dim */

@@ -15,7 +15,7 @@
 // counts itself in; the last one joins them, always in the same order, and clears the count.  Nobody waits for anybody.
 //
 // What bounds it.  Many rows: instruction issue beside memory: per value an exponential, four more operations and one for the rank, 2048 rows
-// of 128256 (525 MB) 91 us without tokens, 98 with, 108 with the most likely one, 127 with 20 (4.1 to 5.8 TB/s; a bare read takes 74).  Few rows: trips
+// of 128256 (525 MB) 91 us without tokens, 96 with, 102 with the most likely one, 125 with 20 (4.2 to 5.8 TB/s; a bare read takes 74).  Few rows: trips
 // that follow one another: 1 row 5.7 us, with 5 tokens 10, with 20 13.9; of 32 rows with 20 (15 us) 1 is loading, 1 bisection, 1.5 writing down,
 // 2.5 joining the wavefronts, 1.5 the way to memory and its count, 3 joining the parts.  Instructions that run once cost their way through
 // the instruction cache: the same kernel with 20 KB of code instead of 15 took a third longer wherever a list was asked for.
@@ -30,7 +30,7 @@ namespace ams_kv {
 
 constexpr size_t kLogCountBytes = 64 * 1024;  // of a workspace: one count for each row, at its front
 constexpr int kMaxRowParts = 32;
-constexpr int kWholeWaves = 4, kPartWaves = 8;  // of a workgroup that has a whole row of many, or a part of one
+constexpr int kWholeWaves = 4, kPartWaves = 8, kShortWaves = 16;  // of a workgroup that has a whole row of many, a part of one, or a short row
 constexpr int kHeld = 256;  // values that a wavefront writes down at most
 
 struct LogArgs {
@@ -279,12 +279,17 @@ __global__ __launch_bounds__(64 * WAVES, 4) void logprobs_kernel(LogArgs a) {
   Held held = {entries + wave * kHeld, entries + (WAVES + wave) * kHeld};
   // A wavefront's chunks lie WAVES apart: a workgroup's form one window.
   const int begin = (int)part * a.part_turns * WAVES + wave, n_chunks = (a.vocab - 1) / VALUES + 1, end = min((int)(part + 1) * a.part_turns * WAVES, n_chunks);
-  // Nothing is asked for ahead: sixteen wavefronts of a compute unit ask for 64 KiB at a time, and registers for the next chunk would cost
-  // some of them (2048 rows 124 -> 108 us without).
+  // Workgroups of whole rows ask for the next chunk as soon as there is one (2048 rows of 128256 108 -> 101 us); others have few (300 rows of 49999
+  // in 32 bits 15.9 us, 19 with the registers for it).
+  constexpr bool AHEAD = WAVES == kWholeWaves;
+  Chunk<T> now, next;
+  if (AHEAD && begin < end) now.load(x, begin * VALUES, a.vocab);
   for (int chunk = begin; chunk < end; chunk += WAVES) {
     const int first = chunk * VALUES;
-    Chunk<T> now;
-    now.load(x, first, a.vocab);
+    if (!AHEAD)
+      now.load(x, first, a.vocab);
+    else if (chunk + WAVES < end)
+      next.load(x, first + WAVES * VALUES, a.vocab);
     float most[kPieces];
 #pragma unroll
     for (int u = 0; u < kPieces; u++) most[u] = now.largest(u), maxima[u] = fmaxf(maxima[u], most[u]);
@@ -365,6 +370,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void logprobs_kernel(LogArgs a) {
       if (own > held.bound) held.bound = own, held.last = entry_of(own, 0);  // equal ones that come later are not
       if (lane == 0) __hip_atomic_store(&bounds[wave], held.bound, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
     }
+    if (AHEAD) now = next;
   }
 
   // Statistics of the workgroup's wavefronts, then of the row's workgroups, one to a lane: all of them for the largest maximum.
@@ -499,7 +505,9 @@ __global__ __launch_bounds__(64 * WAVES, 4) void logprobs_kernel(LogArgs a) {
 bool load_logprobs() { return loaded((const void*)logprobs_kernel<float, 8>); }
 
 // Workgroups of a row.  Eight wavefronts to a workgroup up to as many as the chip holds at once, beyond that four, whose ends others cover (rows
-// of 50001, 8 tokens: 300 rows 27 us with eight, 31 with four; 500 29 and 34; 600 41 and 38; 2048 95 and 77).
+// of 50001, 8 tokens: 300 rows 27 us with eight, 31 with four; 500 29 and 34; 600 41 and 38; 2048 95 and 77).  Where sixteen have a chunk of the
+// row each, as of 32000 tokens in fp16, and every workgroup has a compute unit, they take it whole (rows of 20000 with 20 tokens: 1 row in two
+// parts 11.7 us, whole 9.8; 128 rows 13.8 and 12.3; 200 rows with eight 13.3, sixteen 12.8; 300 rows 16.4 and 21.6).
 constexpr int64_t kWorkgroups = 512;
 struct LogPlan {
   int waves, parts, part_turns, part_bytes;
@@ -507,13 +515,14 @@ struct LogPlan {
 };
 static LogPlan log_plan(int type, int64_t rows, int64_t vocab, int top, size_t workspace) {
   const int64_t values = type == AMS_TYPE_FP32 ? Chunk<float>::VALUES : Chunk<_Float16>::VALUES, chunks = (vocab + values - 1) / values;
-  const int waves = rows > kWorkgroups ? kWholeWaves : kPartWaves;
+  const bool is_short = chunks > kPartWaves && chunks <= kShortWaves && rows <= 256;
+  const int waves = rows > kWorkgroups ? kWholeWaves : is_short ? kShortWaves : kPartWaves;
   const LogPlan whole = {waves, 1, (int)((chunks + waves - 1) / waves), 0, 0};
   const int64_t turns = (chunks + kPartWaves - 1) / kPartWaves;
   const int64_t parts = std::min<int64_t>(std::min<int64_t>(turns, kMaxRowParts), rows > 0 ? kWorkgroups / rows : 1);
   // More than half as many rows as compute units: two parts have to be long to pay for their join (256 rows, 20 tokens, whole and in two: of 20000
   // 13.7 us and 16.8, 50001 19.4 and 22.9, 128256 33.5 and 32.1; 128 rows of 50001 19.0, in four 17.2).
-  if (parts < 2 || (rows > 128 && turns < 4 * parts)) return whole;
+  if (parts < 2 || is_short || (rows > 128 && turns < 4 * parts)) return whole;
   LogPlan p = {kPartWaves, 0, (int)((turns + parts - 1) / parts), (16 + 8 * top + 15) / 16 * 16, 0};
   p.parts = (int)((turns + p.part_turns - 1) / p.part_turns);
   p.workspace = kLogCountBytes + (size_t)(rows * p.parts) * p.part_bytes;
@@ -555,10 +564,13 @@ int ams_logprobs(const void* logits, int type, int64_t rows, int64_t vocab, int6
   a.part_turns = p.part_turns, a.part_bytes = p.part_bytes, a.left_bytes = (uint32_t)(p.workspace ? p.workspace - kLogCountBytes : 0), a.parts = divisor((uint32_t)p.parts), a.by_top = divisor((uint32_t)std::max(top, 1));
   const unsigned grid = (unsigned)(rows * p.parts);
   auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * p.waves), 0, (hipStream_t)stream, a); };
-  if (type == AMS_TYPE_FP32)
-    p.waves == kWholeWaves ? launch(logprobs_kernel<float, kWholeWaves>) : launch(logprobs_kernel<float, kPartWaves>);
-  else
-    p.waves == kWholeWaves ? launch(logprobs_kernel<_Float16, kWholeWaves>) : launch(logprobs_kernel<_Float16, kPartWaves>);
+  auto of_type = [&](auto zero) {
+    typedef decltype(zero) T;
+    if (p.waves == kWholeWaves) return launch(logprobs_kernel<T, kWholeWaves>);
+    if (p.waves == kShortWaves) return launch(logprobs_kernel<T, kShortWaves>);
+    launch(logprobs_kernel<T, kPartWaves>);
+  };
+  type == AMS_TYPE_FP32 ? of_type(0.0f) : of_type((_Float16)0);
   return hipGetLastError() == hipSuccess ? AMS_OK : AMS_ERR_LAUNCH;
 }
 

@@ -13,6 +13,12 @@
 //
 // A row is shared out to several workgroups where rows do not fill the chip: each leaves its statistics and list in the workspace and
 // counts itself in; the last one joins them, always in the same order, and clears the count.  Nobody waits for anybody.
+//
+// What bounds it.  Many rows: instruction issue beside memory: per value an exponential, four more operations and one for the rank, 2048 rows
+// of 128256 (525 MB) 91 us without tokens, 98 with, 108 with the most likely one, 127 with 20 (4.1 to 5.8 TB/s; a bare read takes 74).  Few rows: trips
+// that follow one another: 1 row 5.7 us, with 5 tokens 10, with 20 13.9; of 32 rows with 20 (15 us) 1 is loading, 1 bisection, 1.5 writing down,
+// 2.5 joining the wavefronts, 1.5 the way to memory and its count, 3 joining the parts.  Instructions that run once cost their way through
+// the instruction cache: the same kernel with 20 KB of code instead of 15 took a third longer wherever a list was asked for.
 #include <float.h>
 #include <limits.h>
 
@@ -227,8 +233,9 @@ struct Held {
   }
 };
 
+// Four wavefronts to a SIMD: six or eight make the compiler spill (2048 rows: 101, 105 and 277 us).
 template <typename T, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 4) void logprobs_kernel(LogArgs a) {
+__global__ __launch_bounds__(64 * WAVES, 8) void logprobs_kernel(LogArgs a) {
   constexpr int PER = Chunk<T>::PER, VALUES = Chunk<T>::VALUES, THREADS = 64 * WAVES;
   const int wave = uniform((int)threadIdx.x >> 6), lane = lane_id();
   const uint32_t row = a.parts.quotient(blockIdx.x), part = blockIdx.x - row * a.parts.by;
@@ -272,11 +279,12 @@ __global__ __launch_bounds__(64 * WAVES, 4) void logprobs_kernel(LogArgs a) {
   Held held = {entries + wave * kHeld, entries + (WAVES + wave) * kHeld};
   // A wavefront's chunks lie WAVES apart: a workgroup's form one window.
   const int begin = (int)part * a.part_turns * WAVES + wave, n_chunks = (a.vocab - 1) / VALUES + 1, end = min((int)(part + 1) * a.part_turns * WAVES, n_chunks);
-  // Nothing is asked for ahead: four workgroups to a compute unit ask for 128 KiB at a time.
+  // The next chunk is asked for as soon as there is one.
+  Chunk<T> now, next;
+  if (begin < end) now.load(x, begin * VALUES, a.vocab);
   for (int chunk = begin; chunk < end; chunk += WAVES) {
     const int first = chunk * VALUES;
-    Chunk<T> now;
-    now.load(x, first, a.vocab);
+    if (chunk + WAVES < end) next.load(x, first + WAVES * VALUES, a.vocab);
     float most[kPieces];
 #pragma unroll
     for (int u = 0; u < kPieces; u++) most[u] = now.largest(u), maxima[u] = fmaxf(maxima[u], most[u]);
@@ -357,6 +365,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void logprobs_kernel(LogArgs a) {
       if (own > held.bound) held.bound = own, held.last = entry_of(own, 0);  // equal ones that come later are not
       if (lane == 0) __hip_atomic_store(&bounds[wave], held.bound, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
     }
+    now = next;
   }
 
   // Statistics of the workgroup's wavefronts, then of the row's workgroups, one to a lane: all of them for the largest maximum.
@@ -445,13 +454,13 @@ __global__ __launch_bounds__(64 * WAVES, 4) void logprobs_kernel(LogArgs a) {
       if (lane == 0) row_stats = mine;
     }
     if (a.top > 0) {
-      if (n > 64) __syncthreads();
+      if (n > 256) __syncthreads();
 #pragma unroll
       for (int k = 0; k < kMaxRowParts * AMS_LOGPROBS_MAX_TOP / THREADS; k++) {
         const int i = k * THREADS + (int)threadIdx.x;
-        if (n > 64 && i < n && (i + 1) % a.top == 0 && theirs_best[k]) atomicMax((unsigned long long*)&least_entry, (unsigned long long)theirs_best[k]);
+        if (n > 256 && i < n && (i + 1) % a.top == 0 && theirs_best[k]) atomicMax((unsigned long long*)&least_entry, (unsigned long long)theirs_best[k]);
       }
-      if (n > 64) {
+      if (n > 256) {
         __syncthreads();
         bound = least_entry;
       }
@@ -490,7 +499,8 @@ __global__ __launch_bounds__(64 * WAVES, 4) void logprobs_kernel(LogArgs a) {
 
 bool load_logprobs() { return loaded((const void*)logprobs_kernel<float, 8>); }
 
-// Workgroups of a row.  Eight wavefronts to a workgroup up to as many as the chip holds, beyond that four.
+// Workgroups of a row.  Eight wavefronts to a workgroup up to as many as the chip holds at once, beyond that four, whose ends others cover (rows
+// of 50001, 8 tokens: 300 rows 27 us with eight, 31 with four; 500 29 and 34; 600 41 and 38; 2048 95 and 77).
 constexpr int64_t kWorkgroups = 512;
 struct LogPlan {
   int waves, parts, part_turns, part_bytes;
@@ -502,7 +512,9 @@ static LogPlan log_plan(int type, int64_t rows, int64_t vocab, int top, size_t w
   const LogPlan whole = {waves, 1, (int)((chunks + waves - 1) / waves), 0, 0};
   const int64_t turns = (chunks + kPartWaves - 1) / kPartWaves;
   const int64_t parts = std::min<int64_t>(std::min<int64_t>(turns, kMaxRowParts), rows > 0 ? kWorkgroups / rows : 1);
-  if (parts < 2) return whole;
+  // More than half as many rows as compute units: two parts have to be long to pay for their join (256 rows, 20 tokens, whole and in two: of 20000
+  // 13.7 us and 16.8, 50001 19.4 and 22.9, 128256 33.5 and 32.1; 128 rows of 50001 19.0, in four 17.2).
+  if (parts < 2 || (rows > 128 && turns < 4 * parts)) return whole;
   LogPlan p = {kPartWaves, 0, (int)((turns + parts - 1) / parts), (16 + 8 * top + 15) / 16 * 16, 0};
   p.parts = (int)((turns + p.part_turns - 1) / p.part_turns);
   p.workspace = kLogCountBytes + (size_t)(rows * p.parts) * p.part_bytes;

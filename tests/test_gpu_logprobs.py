@@ -83,6 +83,19 @@ def test_many_rows(workspace, rows):
     check(ams.ams_logprobs(x, tokens, top=7, workspace=workspace), x, tokens.tolist(), 7)
 
 
+@pytest.mark.parametrize("wide", [False, True])
+@pytest.mark.parametrize("rows,vocab", [(256, 17000), (257, 17000), (3, 32768), (3, 32769), (128, 50001), (129, 50001), (200, 70001), (512, 9000), (513, 9000), (600, 40000)])
+def test_every_split(workspace, rows, vocab, wide):
+    """Rows in parts, whole on eight wavefronts or sixteen, and of many on four."""
+    x, tokens = draw(rows, vocab, wide)
+    got = ams.ams_logprobs(x, tokens, top=11, workspace=workspace)
+    some = [0, 1, rows // 2, rows - 2, rows - 1]
+    check(ams.LogProbs(*(t[some] for t in got)), x[some], tokens[some].tolist(), 11)
+    alone = ams.ams_logprobs(x, tokens, top=11)
+    assert torch.equal(got.top_tokens, alone.top_tokens) and torch.equal(got.rank, alone.rank)
+    assert not workspace[: 64 << 10].any()
+
+
 @pytest.mark.parametrize("temperature", [0.1, 0.7, 1.5, 100.0])
 @pytest.mark.parametrize("wide", [False, True])
 def test_temperature(workspace, temperature, wide):
