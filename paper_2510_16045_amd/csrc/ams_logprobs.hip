@@ -16,9 +16,9 @@
 //
 // What bounds it.  Many rows: instruction issue beside memory: per value an exponential, four more operations and one for the rank, 2048 rows
 // of 128256 (525 MB) 91 us without tokens, 96 with, 102 with the most likely one, 125 with 20 (4.2 to 5.8 TB/s; a bare read takes 74).  Few rows: trips
-// that follow one another: 1 row 5.7 us, with 5 tokens 10, with 20 13.9; of 32 rows with 20 (15 us) 1 is loading, 1 bisection, 1.5 writing down,
-// 2.5 joining the wavefronts, 1.5 the way to memory and its count, 3 joining the parts.  Instructions that run once cost their way through
-// the instruction cache: the same kernel with 20 KB of code instead of 15 took a third longer wherever a list was asked for.
+// that follow one another: 1 row 5.7 us, with 5 tokens 10, with 20 13.9; of 32 rows with 20 (15 us) 1 is loading, 1.4 bisection, 1 writing down,
+// 1.5 waiting for the other wavefronts, 2.5 joining their lists, 1.4 the way to memory and its count, 3.3 joining the parts.  Instructions
+// that run once cost their way through the instruction cache: with 20 KB of code instead of 15 all that has a list took a third longer.
 #include <float.h>
 #include <limits.h>
 
