@@ -257,20 +257,29 @@ __global__ __launch_bounds__(64 * WAVES, 4) void logprobs_kernel(LogArgs a) {
   const T below_given = next_below(given);
   const bool ranked = has_token && a.rank;
 
-  // x's scaled distance from m.  In 32 bits x may be as large as that type's values are: the difference first.
-  auto scaled = [&](float v, float m) {
+  // x's scaled distance from m.  In 32 bits x may be as large as that type's values are: the difference first.  In 16 it is one operation
+  // with m's product, whose rounding moves all of a row's exponents alike, by half at most while that product is below 2^24.  Beyond, which
+  // needs a temperature of 0.0056 or less, the nearest smaller value lies 2^12 away, only m itself has a weight, and the factor's upper 13 bits
+  // do: their products with fp16 values are not rounded.
+  const bool cold = PER == 8 && a.scale2 >= 256;
+  const float short_factor = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, a.scale2) & 0xFFFFF800u);
+  auto is_far = [&](float m) { return fabsf(m) * a.scale2 >= 16777216.0f; };
+  auto factor_of = [&](float m) { return is_far(m) ? short_factor : a.scale2; };
+  auto scaled = [&](float v, float m, float factor) {
     if constexpr (PER == 4)
       return (v - m) * a.scale2;
     else
-      return __builtin_fmaf(v, a.scale2, -(m * a.scale2));
+      return __builtin_fmaf(v, factor, -(m * factor));
   };
   // What m instead of `before` makes of it: for fp16 the difference of the products as they were rounded.
   auto moved = [&](float before, float m) {
 #pragma clang fp contract(off)
     if constexpr (PER == 4) return (before - m) * a.scale2;
-    const float from = before * a.scale2, to = m * a.scale2;
+    float from = before * a.scale2, to = m * a.scale2;
+    if (cold) from = before * factor_of(before), to = m * factor_of(m);
     return from - to;
   };
+  float factor = a.scale2;
   float m = -INFINITY, sums[4] = {0, 0, 0, 0}, moments[4] = {0, 0, 0, 0}, maxima[kPieces];
 #pragma unroll
   for (int u = 0; u < kPieces; u++) maxima[u] = -INFINITY;
@@ -297,6 +306,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void logprobs_kernel(LogArgs a) {
     if (__ballot(top > m)) {
       const float before = m;
       m = max_over_wave(fmaxf(top, m));
+      if (cold) factor = factor_of(m);
       if (before != -INFINITY) {  // y becomes y + less
         const float less = moved(before, m), by = __builtin_amdgcn_exp2f(less);
 #pragma unroll
@@ -310,7 +320,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void logprobs_kernel(LogArgs a) {
       __builtin_amdgcn_sched_barrier(0);  // eight values at a time: more take registers
 #pragma unroll
       for (int j = 0; j < PER; j++) {
-        const float y = scaled((float)now.value(u, j), m_or_0), e = __builtin_amdgcn_exp2f(y);
+        const float y = scaled((float)now.value(u, j), m_or_0, factor), e = __builtin_amdgcn_exp2f(y);
         sums[j & 3] += e;
         moments[j & 3] = __builtin_fmaf(e, fmaxf(y, -256.0f), moments[j & 3]);  // 2^y is 0 far above: so that 0 times an infinity is not asked for
       }
@@ -478,7 +488,10 @@ __global__ __launch_bounds__(64 * WAVES, 4) void logprobs_kernel(LogArgs a) {
   }
   if (wave > 0) return;
   const float total = __log2f(mine.sum);
-  auto log_probability = [&](float v) { return v == -INFINITY && mine.sum == mine.sum ? -INFINITY : (scaled(v, mine.top) - total) * 0.69314718056f; };
+  auto log_probability = [&](float v) {
+    const float y = cold && is_far(mine.top) ? (v - mine.top) * a.scale2 : scaled(v, mine.top, a.scale2);
+    return v == -INFINITY && mine.sum == mine.sum ? -INFINITY : (y - total) * 0.69314718056f;
+  };
   if (lane == 0) {
     if (a.logprob) a.logprob[row] = has_token ? log_probability((float)given) : 0.0f;
     if (a.rank) a.rank[row] = has_token ? mine.ahead : -1;
