@@ -42,7 +42,7 @@ struct RopeArgs {
   int interleaved, transposed;
 };
 
-// The position of a row, the wavefront's own: false where no sequence has it.
+// The position of a row, the wavefront's own: false where no sequence has it.  Row starts count as in [0, rows], as the cache's calls take them.
 __device__ __forceinline__ bool row_position(const RopeArgs& a, int64_t row, int* position) {
   if (a.positions) {
     *position = a.positions[row];
@@ -55,7 +55,7 @@ __device__ __forceinline__ bool row_position(const RopeArgs& a, int64_t row, int
   }
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
     const int b = min(b0 + lane_id(), a.batch - 1);
-    const int first = a.starts[b], end = a.starts[b + 1], len = max(a.lens[b], 0);
+    const int first = a.starts[b], end = min(max(a.starts[b + 1], 0), (int)a.rows), len = max(a.lens[b], 0);
     const unsigned long long found = __ballot(first <= row && row < end);
     if (found) {
       *position = (int)((uint32_t)__builtin_amdgcn_readlane(len, __builtin_ctzll(found)) - (uint32_t)__builtin_amdgcn_readlane(end, __builtin_ctzll(found)) + (uint32_t)row);
