@@ -365,9 +365,11 @@ int ams_kv_attention(const ams_kv_cache* cache, const uint16_t* Q, uint16_t* O, 
  *   slopes       device, [heads] fp32, or NULL: then slopes[h] * |p - j| is taken off it
  *   prefix_lens  device, [batch], or NULL (causal only): every row of sequence b that has a position (p >= 0) sees the keys
  *                j < prefix_lens[b] of those that there are, also those behind it and those that its window has left behind
- * in this order; fp32, the hyperbolic tangent to 2^-22.  `scores` NULL, or one that asks for none of them, is ams_kv_attention.  The
- * workspace and what ams_kv_attention_plan says are the same for both.  Errors: as ams_kv_attention; SHAPE for a softcap below 0 or not
- * finite, or for prefix_lens without causal.
+ * in this order; fp32.  Capped scores are off by up to 2^-22 of the cap; of caps above 256, which take kernels of their own that are up to
+ * 1.4 times slower, by up to 2^-20 of the score.  `scores` NULL, or one that asks for none of them, is ams_kv_attention.  The workspace and
+ * what ams_kv_attention_plan says are the same for both: prefix_lens, which the host does not know, do not change the plan, so a long prefix
+ * behind a short window gets the workgroups that the window alone would get.  Errors: as ams_kv_attention; SHAPE for a softcap below 0, above
+ * 5.89e37 or not a number, one so small that 2.9 softmax_scale / softcap is no fp32 number, or for prefix_lens without causal.
  */
 typedef struct ams_kv_scores {
   const float* slopes;

@@ -2062,6 +2062,8 @@ bool load_scored_stream();
 bool load_scored_tile();
 bool load_prefix_stream();
 bool load_prefix_tile();
+bool load_large_cap_stream();
+bool load_large_cap_tile();
 bool load_rope();
 bool load_logprobs();
 }  // namespace ams_kv
@@ -2078,7 +2080,7 @@ int ams_init(void) {
   if (rc == AMS_OK) rc = prepare_format<FMT_FP5>();
   if (rc == AMS_OK) rc = prepare_format<FMT_FP4>();
   if (rc == AMS_OK) rc = prepare_format<FMT_FP16>();
-  if (rc == AMS_OK && !(ams_kv::load_cache() && ams_kv::load_stream() && ams_kv::load_tile() && ams_kv::load_scored_stream() && ams_kv::load_scored_tile() && ams_kv::load_prefix_stream() && ams_kv::load_prefix_tile() && ams_kv::load_rope() && ams_kv::load_logprobs())) rc = AMS_ERR_LAUNCH;
+  if (rc == AMS_OK && !(ams_kv::load_cache() && ams_kv::load_stream() && ams_kv::load_tile() && ams_kv::load_scored_stream() && ams_kv::load_scored_tile() && ams_kv::load_prefix_stream() && ams_kv::load_prefix_tile() && ams_kv::load_large_cap_stream() && ams_kv::load_large_cap_tile() && ams_kv::load_rope() && ams_kv::load_logprobs())) rc = AMS_ERR_LAUNCH;
   return rc;
 }
 

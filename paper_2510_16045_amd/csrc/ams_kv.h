@@ -245,6 +245,8 @@ bool load_scored_stream();
 bool load_scored_tile();
 bool load_prefix_stream();
 bool load_prefix_tile();
+bool load_large_cap_stream();
+bool load_large_cap_tile();
 bool load_rope();
 bool load_logprobs();
 

@@ -66,28 +66,48 @@ struct ScoredArgs : AttentionArgs {
 struct PrefixArgs : ScoredArgs {
   const int32_t* prefixes;  // [batch]
 };
+// Caps above kLargeCap, with or without prefixes (null): cap2 is 0.
+struct LargeCapArgs : PrefixArgs {
+  float cap_of;  // cap / softmax_scale
+};
+constexpr float kLargeCap = 256;
 template <typename Args>
 constexpr bool kScored = std::is_base_of_v<ScoredArgs, Args>;
 template <typename Args>
-constexpr bool kPrefix = std::is_same_v<Args, PrefixArgs>;
+constexpr bool kPrefix = std::is_base_of_v<PrefixArgs, Args>;
+template <typename Args>
+constexpr bool kIsLargeCap = std::is_same_v<Args, LargeCapArgs>;
 
 // Keys from the first on that every row with a position sees.
 __device__ __forceinline__ int prefix_of(const PrefixArgs& a, int b, int len) { return min(max(a.prefixes[b], 0), len); }
+__device__ __forceinline__ int prefix_of(const LargeCapArgs& a, int b, int len) { return a.prefixes ? min(max(a.prefixes[b], 0), len) : 0; }
 
 // Scores of N products s of a lane's row with keys, in place, in units of 1 / unit_of (log2): the i-th key lies `first` + key(i) from the
 // row; `behind`: none of them behind the row's position.
-//   cap tanh(x / cap) = cap - 2 cap / (exp(2 x / cap) + 1): off by 2^-22 of the cap, less by far than the rounding of a weight to fp16
-//   (2^-11), and right at both ends, where the exponential is 0 or infinite.  The first term, which all scores have, is left out: weights do
-//   not change with it, and log-sum-exps get it at the end (left_out).
+//   cap tanh(x / cap) = cap - 2 cap / (exp(2 x / cap) + 1): off by 2^-22 of the cap, so with caps up to kLargeCap by 2^-14 at most, an eighth
+//   of the rounding of a weight to fp16 (2^-11), and right at both ends, where the exponential is 0 or infinite.  The first term, which all
+//   scores have, is left out: weights do not change with it, and log-sum-exps get it at the end (left_out).
+//   Larger caps would lose scores that are small beside them.  Theirs are x (1 - (x / cap)^2 / 3 + ...), the series up to the ninth power, where
+//   |x| is below a quarter of the cap (the next term is below 1e-8 of x), and the exponential's form beyond: off by 2^-20 of the score.  Its
+//   sixteen operations have kernels of their own: beside the others they took their registers (64 channels: 60 bytes spilled, with them 96).  A cap of 300
+//   instead of 50: 2048 rows over 8192 keys, biased, 519 us instead of 380, one row each of 32 sequences of up to 8192 48 instead of 42.3.
 // Their issue is what they cost: 2048 rows over 8192 keys, 32 and 8 heads of 128 channels: plain 267 us, with a cap 325 (two transcendental
 // operations a score and two others), a bias 304 (two others), both 377; before the first term and a product were left out 341, 319 and 391.
 // One sequence's rows each of 32 sequences of up to 8192: 35, 37.5, 39.6, 42.5.
 __device__ __forceinline__ float scale_of(const ScoredArgs& a) { return a.cap2 > 0 ? 2 * a.cap2 : a.scale2; }
 __device__ __forceinline__ float unit_of(const ScoredArgs& a) { return a.slopes ? 1.0f : scale_of(a); }
 __device__ __forceinline__ float unit_of(const AttentionArgs& a) { return a.scale2; }
-template <int N, typename Key>
-__device__ __forceinline__ void score(const ScoredArgs& a, float (&s)[N], float slope, float first, bool behind, Key key) {
-  if (a.cap2 > 0) {
+template <int N, typename Args, typename Key>
+__device__ __forceinline__ void score(const Args& a, float (&s)[N], float slope, float first, bool behind, Key key) {
+  if constexpr (kIsLargeCap<Args>) {
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+      const float z = s[i] * a.to_cap, y = z * z * 0.120113253f;  // (x / cap)^2
+      const float near = __builtin_fmaf(s[i] * y, -1.0f / 3 + y * (2.0f / 15 + y * (-17.0f / 315 + y * (62.0f / 2835))), s[i]);
+      const float far = copysignf(a.cap_of, s[i]) * __builtin_fmaf(-2.0f, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(fabsf(z))), 1.0f);
+      s[i] = fabsf(z) < 0.721347520f ? near : far;
+    }
+  } else if (a.cap2 > 0) {
 #pragma unroll
     for (int i = 0; i < N; i++) s[i] = __builtin_amdgcn_rcpf(-1.0f - __builtin_amdgcn_exp2f(s[i] * a.to_cap));
   }
@@ -424,6 +444,10 @@ template <>
 void launch_stream<PrefixArgs>(const PrefixArgs&, int, int, int, int, unsigned, hipStream_t);
 template <>
 void launch_tile<PrefixArgs>(const PrefixArgs&, int, int, int, unsigned, hipStream_t);
+template <>
+void launch_stream<LargeCapArgs>(const LargeCapArgs&, int, int, int, int, unsigned, hipStream_t);
+template <>
+void launch_tile<LargeCapArgs>(const LargeCapArgs&, int, int, int, unsigned, hipStream_t);
 
 }  // namespace ams_kv
 #endif

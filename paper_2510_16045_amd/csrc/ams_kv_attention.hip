@@ -120,7 +120,7 @@ int ams_kv_attention(const ams_kv_cache* cache, const uint16_t* Q, uint16_t* O, 
 int ams_kv_attention_scored(const ams_kv_cache* cache, const ams_kv_scores* scores, const uint16_t* Q, uint16_t* O, float* lse, int64_t rows, int heads, int64_t q_stride,
                             int64_t q_head_stride, int64_t o_stride, int64_t o_head_stride, int64_t lse_stride, float softmax_scale, int causal, int64_t window, int64_t max_q_len,
                             void* workspace, size_t workspace_bytes, void* stream) {
-  PrefixArgs a;
+  LargeCapArgs a;
   if (const int rc = make_view(cache, rows, &a.v); rc != AMS_OK) return rc;
   if (rows > 0 && (!Q || !O)) return AMS_ERR_NULL;
   if (heads < 1 || heads % cache->kv_heads || heads > AMS_KV_MAX_HEADS || window < 0 || (window > 0 && !causal) || max_q_len < 0 || !(softmax_scale > 0) || !(softmax_scale <= FLT_MAX)) return AMS_ERR_SHAPE;
@@ -142,8 +142,11 @@ int ams_kv_attention_scored(const ams_kv_cache* cache, const ams_kv_scores* scor
   a.shares = (int)p.shares, a.cut = p.cut, a.row_tiles = (int)p.row_tiles, a.part_rows = p.part_rows;
   const int64_t grid = p.shares * cache->kv_heads;
   if (grid > 0x7FFFFFFF) return AMS_ERR_SHAPE;
-  if (x.prefix_lens)
+  if (x.softcap > kLargeCap) {
+    a.cap2 = 0, a.cap_of = x.softcap / softmax_scale;
     launch(a, p, cache, (unsigned)grid, (hipStream_t)stream);
+  } else if (x.prefix_lens)
+    launch<PrefixArgs>(a, p, cache, (unsigned)grid, (hipStream_t)stream);
   else if (x.softcap > 0 || x.slopes)
     launch<ScoredArgs>(a, p, cache, (unsigned)grid, (hipStream_t)stream);
   else

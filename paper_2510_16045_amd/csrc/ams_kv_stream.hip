@@ -15,7 +15,7 @@
 // 16 sequences of 3001 tokens, 64 and 8 heads, tiles of 40 rows: 57 MB in 27 us; 560 instructions a step, 11 us of them.
 #include "ams_kv_attention.h"
 
-#ifndef AMS_KV_SCORED  // 1: the kernels for capped and biased scores, 2: with prefixes, too
+#ifndef AMS_KV_SCORED  // 1: the kernels for capped and biased scores, 2: with prefixes, too, 3: for large caps
 #define AMS_KV_SCORED 0
 #endif
 
@@ -32,6 +32,8 @@ struct Steps<PrefixArgs> {
   int first, before, next;
   __device__ __forceinline__ int at(int i) const { return i < before ? first + i : next + i - before; }
 };
+template <>
+struct Steps<LargeCapArgs> : Steps<PrefixArgs> {};
 
 // The pages of 64 steps of a wavefront, one step to a lane: looked up together, read lane by lane.
 struct Pages {
@@ -429,7 +431,10 @@ __global__ __launch_bounds__(64 * WAVES, stream_groups(D, QT, WAVES) * WAVES / 4
   join_pending<D, 64 * WAVES, QT == 1 ? 1 : 4, QT == 1 ? 8 : 4>(a, pending, left_first, left_last, left, share, head, (float*)shared, all_there);
 }
 
-#if AMS_KV_SCORED == 2
+#if AMS_KV_SCORED == 3
+using Args = LargeCapArgs;
+bool load_large_cap_stream() { return loaded((const void*)stream_kernel<64, 32, 1, 4, Args>); }
+#elif AMS_KV_SCORED == 2
 using Args = PrefixArgs;
 bool load_prefix_stream() { return loaded((const void*)stream_kernel<64, 32, 1, 4, Args>); }
 #elif AMS_KV_SCORED == 1

@@ -12,7 +12,7 @@
 // tiles were joined through the workspace at 340 us.  With a window of 512, seven sequences of up to 1999 tokens, 16 heads of 64: 41 us.
 #include "ams_kv_attention.h"
 
-#ifndef AMS_KV_SCORED  // 1: the kernels for capped and biased scores, 2: with prefixes, too
+#ifndef AMS_KV_SCORED  // 1: the kernels for capped and biased scores, 2: with prefixes, too, 3: for large caps
 #define AMS_KV_SCORED 0
 #endif
 
@@ -363,7 +363,10 @@ __global__ __launch_bounds__(64 * WAVES, tile_waves(D, WAVES)) void tile_kernel(
   }
 }
 
-#if AMS_KV_SCORED == 2
+#if AMS_KV_SCORED == 3
+using Args = LargeCapArgs;
+bool load_large_cap_tile() { return loaded((const void*)tile_kernel<64, 32, 4, Args>); }
+#elif AMS_KV_SCORED == 2
 using Args = PrefixArgs;
 bool load_prefix_tile() { return loaded((const void*)tile_kernel<64, 32, 4, Args>); }
 #elif AMS_KV_SCORED == 1
