@@ -575,8 +575,22 @@ int ams_logprobs(const void* logits, int type, int64_t rows, int64_t vocab, int6
   a.counts = (uint32_t*)workspace, a.left = (uint8_t*)workspace + kLogCountBytes;
   a.vocab = (int)vocab, a.top = top, a.scale2 = (float)(1.4426950408889634 / temperature);
   a.part_turns = p.part_turns, a.part_bytes = p.part_bytes, a.left_bytes = (uint32_t)(p.workspace ? p.workspace - kLogCountBytes : 0), a.parts = divisor((uint32_t)p.parts), a.by_top = divisor((uint32_t)std::max(top, 1));
-  const unsigned grid = (unsigned)(rows * p.parts);
-  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * p.waves), 0, (hipStream_t)stream, a); };
+  // One launch has fewer than 2^32 threads (of more the runtime leaves out what passes that, with no error).
+  constexpr int64_t kLaunchRows = 1 << 23;  // of a workgroup each
+  static_assert(kLaunchRows >= kWorkgroups && kLaunchRows * 64 * kWholeWaves < (int64_t)1 << 32, "rows that are shared out are one launch's");
+  auto launch = [&](auto kernel) {
+    for (int64_t left = rows;;) {
+      const int64_t n = std::min(left, kLaunchRows);
+      hipLaunchKernelGGL(kernel, dim3((unsigned)(n * p.parts)), dim3(64 * p.waves), 0, (hipStream_t)stream, a);
+      if ((left -= n) == 0) return;
+      a.logits = (const uint8_t*)a.logits + n * stride * (type == AMS_TYPE_FP32 ? 4 : 2);
+      for (auto* t : {&a.logprob, &a.entropy})
+        if (*t) *t += n;
+      if (a.tokens) a.tokens += n;
+      if (a.rank) a.rank += n;
+      if (top > 0) a.top_logprobs += n * top, a.top_tokens += n * top;
+    }
+  };
   auto of_type = [&](auto zero) {
     typedef decltype(zero) T;
     if (p.waves == kWholeWaves) return launch(logprobs_kernel<T, kWholeWaves>);

@@ -31,7 +31,7 @@ struct RopeArgs {
   RopeTensor q, k;
   const uint64_t* turns;
   const int32_t *positions, *lens, *starts;
-  int64_t rows;
+  int64_t rows, first_row;  // first_row: of the launch
   float magnitude;
   int batch, heads, all_heads;  // heads: of q; all_heads: with k's behind them
   int pairs, rest;              // of a head: pairs, and channels behind them that are copied (0 where they are in place)
@@ -114,7 +114,8 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
   constexpr int PAIRS = INTERLEAVED && VEC > 1 ? VEC / 2 : VEC;
   const int lane = lane_id();
   const uint32_t unit = blockIdx.x * 4 + (uint32_t)__builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  const uint32_t row = a.by_parts.quotient(unit), part = unit - row * a.by_parts.by;
+  const uint32_t of_launch = a.by_parts.quotient(unit), part = unit - of_launch * a.by_parts.by;
+  const int64_t row = a.first_row + of_launch;
   if (row >= a.rows) return;
   int position;
   if (!row_position(a, row, &position)) return;
@@ -132,8 +133,8 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
       if (head >= a.all_heads) break;
       const RopeTensor& t = head < a.heads ? a.q : a.k;
       const int h = head < a.heads ? head : head - a.heads;
-      const uint16_t* const in = t.in + (int64_t)row * t.in_stride + (int64_t)h * t.in_head;
-      uint16_t* const out = t.out + (int64_t)row * t.out_stride + (int64_t)h * t.out_head;
+      const uint16_t* const in = t.in + row * t.in_stride + (int64_t)h * t.in_head;
+      uint16_t* const out = t.out + row * t.out_stride + (int64_t)h * t.out_head;
       Piece<VEC> x, y;
       if (chunk >= turned) {
         const int at = 2 * a.pairs + (chunk - turned) * VEC;
@@ -237,8 +238,13 @@ int ams_rope(const ams_rotation* rotation, const ams_rope_rows* Q, const ams_rop
   a.passes = (int)((turns + parts - 1) / parts);
   a.by_chunks = divisor((uint32_t)a.chunks), a.by_parts = divisor((uint32_t)((turns + a.passes - 1) / a.passes));
   a.interleaved = r.interleaved != 0, a.transposed = r.transposed != 0;
-  const unsigned grid = (unsigned)((rows * a.by_parts.by + 3) / 4);
-  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, (hipStream_t)stream, a); };
+  // One launch has fewer than 2^32 threads (of more the runtime leaves out what passes that, with no error).
+  constexpr int64_t kLaunchRows = 1 << 25;  // of a wavefront each
+  static_assert(kLaunchRows >= kWavefronts, "more rows have no parts");
+  auto launch = [&](auto kernel) {
+    for (a.first_row = 0; a.first_row < rows; a.first_row += kLaunchRows)
+      hipLaunchKernelGGL(kernel, dim3((unsigned)((std::min(rows - a.first_row, kLaunchRows) * a.by_parts.by + 3) / 4)), dim3(256), 0, (hipStream_t)stream, a);
+  };
   auto of_layout = [&](auto interleaved) {
     constexpr bool I = decltype(interleaved)::value;
     if (streamed) return launch(rope_kernel<8, I, true>);
