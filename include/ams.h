@@ -322,7 +322,8 @@ int ams_kv_block_bytes(int head_dim, int page_size, int scale_group, size_t* byt
  * ams_kv_read   the reverse: what the cache stands for at the rows' positions.
  * Any strides and any 2-byte alignment; 16-byte aligned rows are faster.  Two rows of a call that have the same place
  * race; nothing is written outside of the rows' own places, so writes of other tokens of a page may overlap in time.
- * Errors: NULL, SHAPE, ALIGN, DEVICE, LAUNCH.
+ * Errors: NULL, SHAPE (kv_heads times batch, with q_starts times (rows / 16 + 2 batch), from 2^26 on among them: more threads than one
+ * launch can have), ALIGN, DEVICE, LAUNCH.
  */
 int ams_kv_write(const ams_kv_cache* cache, const uint16_t* K, const uint16_t* V, int64_t rows, int64_t k_stride,
                  int64_t k_head_stride, int64_t v_stride, int64_t v_head_stride, void* stream);
@@ -343,7 +344,8 @@ int ams_kv_read(const ams_kv_cache* cache, uint16_t* K, uint16_t* V, int64_t row
  *                their parts through it.  ams_kv_attention_workspace_bytes says how much is used at most for such a call
  *                (never more than AMS_KV_WORKSPACE_BYTES); with less, fewer workgroups, but not much fewer than without one: where it is
  *                too small for that it is not used.  Calls that overlap in time must not share it.
- * Deterministic.  Errors: NULL, SHAPE (softmax_scale not above 0 or not finite among them), ALIGN, DEVICE, LAUNCH.
+ * Deterministic.  Errors: NULL, SHAPE (softmax_scale not above 0 or not finite among them; and 2^32 threads or more, by the workgroups and
+ * wavefronts that ams_kv_attention_plan tells), ALIGN, DEVICE, LAUNCH.
  */
 #define AMS_KV_WORKSPACE_BYTES (64 << 20)
 int ams_kv_attention_workspace_bytes(const ams_kv_cache* cache, int64_t rows, int heads, int64_t max_q_len, size_t* bytes);

@@ -231,6 +231,8 @@ void dispatch(int head_dim, int scale_group, Go go) {
 // Host: checks what the entry points share and fills in the view.
 int make_view(const ams_kv_cache* c, int64_t rows, View* v);
 bool aligned(const void* p, int bytes);
+// Threads that one launch can have are fewer than 2^32: of more the runtime starts those beyond, with no error.
+inline bool launchable(int64_t workgroups, int threads) { return workgroups * threads < (int64_t)1 << 32; }
 // AMS_OK on a gfx950 (ams_kernels.hip).
 int device_status();
 // Each file's kernels on the current device, so that a first call may be captured: one of a file brings in all of them.

@@ -130,18 +130,19 @@ int ams_kv_attention_scored(const ams_kv_cache* cache, const ams_kv_scores* scor
   a.slopes = x.slopes, a.prefixes = x.prefix_lens, a.cap2 = x.softcap * kLog2e, a.to_cap = x.softcap > 0 ? 2 * kLog2e * softmax_scale / x.softcap : 0;
   if (!(x.softcap >= 0) || !(a.cap2 <= FLT_MAX / 4) || !(a.to_cap <= FLT_MAX) || (x.prefix_lens && !causal)) return AMS_ERR_SHAPE;
   if (!aligned(Q, 2) || !aligned(O, 2) || !aligned(lse, 4) || !aligned(workspace, 16) || !aligned(x.slopes, 4) || !aligned(x.prefix_lens, 4)) return AMS_ERR_ALIGN;
+  const bool nothing = rows == 0 || cache->batch == 0;
+  const Plan p = nothing ? Plan{} : make_plan(cache, rows, heads, max_q_len, window, workspace ? workspace_bytes : 0);
+  const int64_t grid = p.shares * cache->kv_heads;
+  if (!launchable(grid, 64 * p.waves)) return AMS_ERR_SHAPE;
   if (const int rc = device_status(); rc != AMS_OK) return rc;
-  if (rows == 0 || cache->batch == 0) return AMS_OK;
+  if (nothing) return AMS_OK;
   a.q = Q, a.out = O, a.lse = lse, a.counts = (uint32_t*)workspace, a.parts = (float*)((uint8_t*)workspace + kCountBytes);
   a.q_stride = q_stride, a.q_head = q_head_stride, a.out_stride = o_stride, a.out_head = o_head_stride, a.lse_stride = lse_stride;
   a.scale2 = softmax_scale * kLog2e;
   a.group = heads / cache->kv_heads, a.by_group = divisor((uint32_t)a.group);
   a.causal = causal != 0, a.window = (int)std::min<int64_t>(window, 0x3FFFFFFF);
   a.vec = aligned(Q, 16) && aligned(O, 8) && (q_stride | q_head_stride) % 8 == 0 && (o_stride | o_head_stride) % 4 == 0;
-  const Plan p = make_plan(cache, rows, heads, max_q_len, window, workspace ? workspace_bytes : 0);
   a.shares = (int)p.shares, a.cut = p.cut, a.row_tiles = (int)p.row_tiles, a.part_rows = p.part_rows;
-  const int64_t grid = p.shares * cache->kv_heads;
-  if (grid > 0x7FFFFFFF) return AMS_ERR_SHAPE;
   if (x.softcap > kLargeCap) {
     a.cap2 = 0, a.cap_of = x.softcap / softmax_scale;
     launch(a, p, cache, (unsigned)grid, (hipStream_t)stream);

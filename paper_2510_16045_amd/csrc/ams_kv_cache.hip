@@ -251,12 +251,12 @@ int run_rows(const ams_kv_cache* cache, int64_t rows, uint16_t* k, uint16_t* v, 
   if (const int rc = make_view(cache, rows, &a.v); rc != AMS_OK) return rc;
   if (rows > 0 && (!k || !v)) return AMS_ERR_NULL;
   if (!aligned(k, 2) || !aligned(v, 2)) return AMS_ERR_ALIGN;
+  const int64_t units = (cache->q_starts ? rows / kTile + 2 * (int64_t)cache->batch : cache->batch) * cache->kv_heads, grid = (units + kWaves - 1) / kWaves;
+  if (rows > 0 && !launchable(grid, 64 * kWaves)) return AMS_ERR_SHAPE;
   if (const int rc = device_status(); rc != AMS_OK) return rc;
   if (rows == 0 || cache->batch == 0) return AMS_OK;
   a.k = k, a.v_rows = v, a.k_stride = k_stride, a.k_head = k_head, a.v_stride = v_stride, a.v_head = v_head;
   a.vec = aligned(k, 16) && aligned(v, 16) && (k_stride | k_head | v_stride | v_head) % 8 == 0;
-  const int64_t units = (cache->q_starts ? rows / kTile + 2 * (int64_t)cache->batch : cache->batch) * cache->kv_heads, grid = (units + kWaves - 1) / kWaves;
-  if (units > 0x7FFFFFFF - kWaves) return AMS_ERR_SHAPE;
   auto go = [&](auto d, auto g) {
     constexpr int D = decltype(d)::value, G = decltype(g)::value;
     if constexpr (WRITE)
