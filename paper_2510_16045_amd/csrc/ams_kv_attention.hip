@@ -63,7 +63,7 @@ Plan make_plan(const ams_kv_cache* c, int64_t rows, int heads, int64_t max_q_len
   if (!p.tile && p.qt == 1 && c->head_dim < 256 && (about <= kLoneTiles || (about <= kComputeUnits && capacity <= kShortKeys))) p.waves = 8;
   if (!p.tile && p.qt > 1 && c->head_dim == 128 && about <= kComputeUnits) p.waves = 8;
   const int64_t tile_steps = std::max<int64_t>((capacity + kStep - 1) / kStep, 1);
-  p.part_rows = (int)std::min<int64_t>(c->q_starts ? rows * R : R, p.rows);
+  p.part_rows = (int)std::min<int64_t>(c->q_starts ? std::max<int64_t>(rows, 1) * R : R, p.rows);
   const size_t part = (size_t)c->kv_heads * p.part_rows * (c->head_dim + 4) * sizeof(float);
   const size_t room = std::min<size_t>(workspace, AMS_KV_WORKSPACE_BYTES);
   const int64_t fit = std::max<int64_t>(stream_groups(c->head_dim, p.qt, p.waves) * kComputeUnits / c->kv_heads, 1);
@@ -71,7 +71,7 @@ Plan make_plan(const ams_kv_cache* c, int64_t rows, int heads, int64_t max_q_len
   // A workspace with room for few shares does not pay: whole tiles then, as without one.  From 7/8 of a share to a row tile on, as far as those
   // fit on the chip, equal shares gain more where lengths differ than they lose where they do not: 32 sequences, 32 query and 8 kv heads, of
   // 819 to 8192 tokens whole tiles 85 us, 3 shares 492, 24 74, 29 64, 32 59; all of 8192 whole tiles 90, 3 863, 24 123, 29 105, 32 90.
-  p.cut = !p.tile && p.shares > 1 && 8 * p.shares >= 7 * std::min(fit, p.row_tiles) && tile_steps > kUncutSteps && p.row_tiles * (tile_steps + kTileSteps) <= 0x7FFFFFFF;
+  p.cut = rows > 0 && !p.tile && p.shares > 1 && 8 * p.shares >= 7 * std::min(fit, p.row_tiles) && tile_steps > kUncutSteps && p.row_tiles * (tile_steps + kTileSteps) <= 0x7FFFFFFF;
   p.workspace = p.cut ? kCountBytes + 2 * (size_t)p.shares * part : 0;
   if (!p.cut) p.shares = p.row_tiles;
   return p;
