@@ -316,6 +316,13 @@ def _dev_ptr(t, dtype=None):
     return t.data_ptr()
 
 
+def _refuse_recorded(name, *tensors):
+    import torch
+
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        raise RuntimeError(f"{name} leaves no record for a gradient: call it under torch.no_grad(), in a torch.autograd.Function of your own, or on detached tensors")
+
+
 def _too_small(out, rows, columns):
     # the kernels write that many values (a buffer for a larger batch may be given)
     return ValueError(f"out must hold {rows} x {columns} values, it has {out.numel()}")
@@ -720,7 +727,9 @@ def ams_rope(q, k, turns, positions=None, kv_lens=None, q_starts=None, magnitude
 
     turns: of ams_rope_frequencies, on the GPU; the first 2 * len(turns) channels of a head are rotated, halves of them paired or
     (interleaved) neighbours.  positions: int32 [rows]; else the rows are the last ones of sequences of kv_lens tokens, as in
-    ams_kv_write, and rows that none has are left alone.  transposed: by the angles' negatives: takes a gradient back."""
+    ams_kv_write, and rows that none has are left alone.  transposed: by the angles' negatives: takes a gradient back.
+    torch's autograd gets no record of it: tensors that a gradient is asked of are refused unless gradients are switched off, as within a
+    torch.autograd.Function, whose two directions these are."""
     if out is not None and _rope_call(q, k, turns, positions, kv_lens, q_starts, magnitude, interleaved, transposed, *out):
         return out
     import torch
@@ -738,6 +747,7 @@ def ams_rope(q, k, turns, positions=None, kv_lens=None, q_starts=None, magnitude
         out = torch.empty(q.shape, dtype=torch.float16, device=q.device), None if k is None else torch.empty(k.shape, dtype=torch.float16, device=q.device)
     if (k is None) != (out[1] is None):
         raise ValueError("out must hold a tensor for each of q and k")
+    _refuse_recorded("ams_rope", q, k, *out)
     index = lambda t: None if t is None else _dev_ptr(t, torch.int32)  # noqa: E731
     rotation = _Rotation(_dev_ptr(turns, torch.int64), index(positions), index(kv_lens), index(q_starts), batch, 2 * turns.shape[0], int(interleaved), int(transposed), magnitude)
     rows = [None if x is None else ctypes.byref(_rope_rows(x, y, name)) for x, y, name in ((q, out[0], "q"), (k, out[1], "k"))]
@@ -773,12 +783,14 @@ def ams_logprobs(logits, tokens=None, top: int = 0, temperature: float = 1.0, wo
     tokens: int32 [rows], whose log probability and rank are asked for (None: both are None; a token outside of the vocabulary has 0 and
     -1).  top: how many of the most likely tokens (up to MAX_TOP).  temperature divides the logits.
     workspace: a uint8 CUDA tensor, zero-filled once, as ams_kv_attention's (it may be the same); without one each row is
-    one workgroup's.  out: a LogProbs of tensors to write; those that are None are not worked out."""
+    one workgroup's.  out: a LogProbs of tensors to write; those that are None are not worked out.  No gradient: logits that one is asked
+    of are refused unless gradients are switched off."""
     if out is not None and _logprobs_call(logits, tokens, top, temperature, workspace, *out):
         return out
     import torch
 
     kind, (rows, vocab) = _logits_type(logits), logits.shape
+    _refuse_recorded("ams_logprobs", logits, *(out or ()))
     if not logits.is_cuda or (vocab > 1 and logits.stride(1) != 1):
         raise ValueError("logits must be a CUDA tensor whose last dimension is contiguous")
     if _devices != 1:

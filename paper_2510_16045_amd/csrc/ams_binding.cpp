@@ -8,6 +8,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/PythonTorchFunctionTLS.h>
+#include <c10/core/GradMode.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/hip/HIPStream.h>
 
@@ -189,6 +190,9 @@ struct KvCall {
   void* st;
 };
 
+// Whether torch would record what happens to a tensor: rotations and log probabilities leave no record and are refused then.
+bool recorded(PyObject* o) { return THPVariable_CheckExact(o) && THPVariable_Unpack(o).requires_grad() && c10::GradMode::is_enabled(); }
+
 // A float, or a whole number (of fewer digits than a float has).
 bool real(PyObject* o, double* v) {
   if (PyFloat_CheckExact(o)) return *v = PyFloat_AS_DOUBLE(o), true;
@@ -323,7 +327,7 @@ bool rope_arguments(PyObject* const* a, Py_ssize_t n, RopeCall* c) try {
     const at::Tensor* const x = rows_of(in, 0, dim, dev, &r->in_stride);
     if (!x || x->size(1) > AMS_KV_MAX_HEADS) return nullptr;
     const at::Tensor* const y = rows_of(out, x->size(1), x->size(2), dev, &r->out_stride);
-    if (!y || y->size(0) != x->size(0)) return nullptr;
+    if (!y || y->size(0) != x->size(0) || recorded(in) || recorded(out)) return nullptr;
     r->in = (const uint16_t*)x->const_data_ptr(), r->out = (uint16_t*)y->data_ptr(), r->heads = (int32_t)x->size(1);
     return x;
   };
@@ -390,6 +394,8 @@ bool log_arguments(PyObject* const* a, Py_ssize_t n, LogCall* c) try {
   const at::Tensor* x = plain(a[0], at::kHalf, dev, false);
   if (!x) c->type = AMS_TYPE_FP32, x = plain(a[0], at::kFloat, dev, false);
   if (!x || x->dim() != 2 || (x->size(1) > 1 && x->stride(1) != 1)) return false;
+  for (const int i : {0, 5, 7, 8})  // logits and what there is of them in fp32
+    if (recorded(a[i])) return false;
   c->rows = x->size(0), c->vocab = x->size(1), c->stride = x->stride(0), c->top = (int)top, c->temperature = (float)temperature;
   void* tokens = nullptr;
   if (!values(a[1], at::kInt, c->rows, dev, &tokens)) return false;
