@@ -90,10 +90,10 @@ __device__ __forceinline__ int prefix_of(const LargeCapArgs& a, int b, int len) 
 //   Larger caps would lose scores that are small beside them.  Theirs are x (1 - (x / cap)^2 / 3 + ...), the series up to the ninth power, where
 //   |x| is below a quarter of the cap (the next term is below 1e-8 of x), and the exponential's form beyond: off by 2^-20 of the score.  Its
 //   sixteen operations have kernels of their own: beside the others they took their registers (64 channels: 60 bytes spilled, with them 96).  A cap of 300
-//   instead of 50: 2048 rows over 8192 keys, biased, 519 us instead of 380, one row each of 32 sequences of up to 8192 48 instead of 42.3.
-// Their issue is what they cost: 2048 rows over 8192 keys, 32 and 8 heads of 128 channels: plain 267 us, with a cap 325 (two transcendental
-// operations a score and two others), a bias 304 (two others), both 377; before the first term and a product were left out 341, 319 and 391.
-// One sequence's rows each of 32 sequences of up to 8192: 35, 37.5, 39.6, 42.5.
+//   instead of 50: 2048 rows over 8192 keys, biased, 520 us instead of 379, one row each of 32 sequences of up to 8192 48 instead of 42.3.
+// Their issue is what they cost: 2048 rows over 8192 keys, 32 and 8 heads of 128 channels: plain 260 us, with a cap 318 (two transcendental
+// operations a score and two others), a bias 301 (two others), both 379; leaving the first term and a product out took 12 to 16 us off each.
+// One row each of 32 sequences of up to 8192: 40.3, 42.3, 44, 46.7.
 __device__ __forceinline__ float scale_of(const ScoredArgs& a) { return a.cap2 > 0 ? 2 * a.cap2 : a.scale2; }
 __device__ __forceinline__ float unit_of(const ScoredArgs& a) { return a.slopes ? 1.0f : scale_of(a); }
 __device__ __forceinline__ float unit_of(const AttentionArgs& a) { return a.scale2; }

@@ -14,9 +14,9 @@
 // A row is shared out to several workgroups where rows do not fill the chip: each leaves its statistics and list in the workspace and
 // counts itself in; the last one joins them, always in the same order, and clears the count.  Nobody waits for anybody.
 //
-// What bounds it.  Many rows: instruction issue beside memory: per value an exponential, four more operations and one for the rank, 2048 rows
-// of 128256 (525 MB) 91 us without tokens, 96 with, 102 with the most likely one, 125 with 20 (4.2 to 5.8 TB/s; a bare read takes 74).  Few rows: trips
-// that follow one another: 1 row 5.7 us, with 5 tokens 10, with 20 13.9; of 32 rows with 20 (15 us) 1 is loading, 1.4 bisection, 1 writing down,
+// What bounds it.  Many rows: instruction issue beside memory: per value an exponential, four more operations and one for the rank, 9.7 with what
+// is around them, 2048 rows of 128256 (525 MB) 92 us without tokens, 96 with, 102 with the most likely one, 126 with 20 (4.2 to 5.7 TB/s; a bare
+// read takes 74).  Few rows: trips that follow one another: 1 row 5.6 us, with 5 tokens 10, with 20 13.9; of 32 rows with 20 (15 us) 1 is loading, 1.4 bisection, 1 writing down,
 // 1.5 waiting for the other wavefronts, 2.5 joining their lists, 1.4 the way to memory and its count, 3.3 joining the parts.  Instructions
 // that run once cost their way through the instruction cache: with 20 KB of code instead of 15 all that has a list took a third longer.
 #include <float.h>
@@ -518,7 +518,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void logprobs_kernel(LogArgs a) {
 bool load_logprobs() { return loaded((const void*)logprobs_kernel<float, 8, false>); }
 
 // Workgroups of a row.  Eight wavefronts to a workgroup up to as many as the chip holds at once, beyond that four, whose ends others cover (rows
-// of 50001, 8 tokens: 300 rows 27 us with eight, 31 with four; 500 29 and 34; 600 41 and 38; 2048 95 and 77).  Where sixteen have a chunk of the
+// of 50001, 8 tokens: 300 rows 20.5 us with eight, 23 with four; 500 22.4 and 24.3; 600 32 and 29; 2048 74 and 61).  Where sixteen have a chunk of the
 // row each, as of 32000 tokens in fp16, and every workgroup has a compute unit, they take it whole (rows of 20000 with 20 tokens: 1 row in two
 // parts 11.7 us, whole 9.8; 128 rows 13.8 and 12.3; 200 rows with eight 13.3, sixteen 12.8; 300 rows 16.4 and 21.6).
 constexpr int64_t kWorkgroups = 512;

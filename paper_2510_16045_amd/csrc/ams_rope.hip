@@ -4,9 +4,9 @@
 //
 // for pair i of a head's first `rotary_dim` channels: a, b = i, i + rotary_dim / 2, or 2 i, 2 i + 1 where they are interleaved.
 //
-// The angle.  w_i is given as a fraction of a turn in 64-bit fixed point; p times that modulo 2^64 is the angle modulo a turn, off by
-// p 2^-65 turns at most, where a product of 32-bit floats is off by 0.008 radians at p = 131072.  The upper 32 bits (1.5e-9 radians)
-// are reduced to an eighth of a turn on either side of a quarter, where sin and cos are polynomials: the Taylor series up to x^9 and
+// The angle.  w_i is given as a fraction of a turn in 64-bit fixed point, off by what the host's 53 bits leave (some 2^-54 turns for the fastest
+// pairs); p times that modulo 2^64 is the angle modulo a turn, off by p 2^-54 turns, at p = 131072 by 5e-11 radians, where a product of
+// 32-bit floats is off by 0.008.  Its upper 32 bits (to 1.5e-9 radians; the product's lowest word is left out) are reduced to an eighth of a turn on either side of a quarter, where sin and cos are polynomials: the Taylor series up to x^9 and
 // x^8, whose next terms are below 2e-9 and 3e-8.  So there is no table of cosines to read, and no longest position.
 //
 // What bounds it: memory, and a launch where there are few rows.  16384 rows of 72 heads of 128: 604 MB in 118 us, 5.1 TB/s, a copy's rate; in
